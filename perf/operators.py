@@ -227,7 +227,7 @@ def _framework(state):
     case = state["case"]
     if case["kind"] == "logprobs":
         rows, top = case["rows"], case["top"]
-        ws = _workspace(state, lambda: rk.token_logprobs_workspace_size(rows, case["vocab"], top))
+        ws = _workspace(state, lambda: rk.token_logprobs_workspace_size(rows, case["vocab"], top, case["dtype"]))
         rk.token_logprobs(state["logits"], state["tokens"], ws, logprob=state["logprob"], rank=state["rank"],
                           entropy=state["entropy"], top_ids=state["top_ids"] if top else None,
                           top_logprobs=state["top_logprobs"] if top else None)
