@@ -487,13 +487,146 @@ rk_status rk_policy_damage_group(const rk_model *m, const rk_batch *batch, int32
  * the mean rank; NaN when a profile is constant.  Host only, float64.          */
 rk_status rk_spearman(const double *x, const double *y, int32_t n, double *rho);
 
+/* ---------------------------------------------------------------- paged key-value cache */
+
+/* A key-value cache in pages, for decoding token by token: a whole cache, or one
+ * that rk_snapkv_compress cut to the layers' budgets and that grows again.  One
+ * rk_paged_cache is one layer's; the layers of a model may share one pool of pages.
+ *   k, v:       DEVICE [n_pages, n_kv_heads, page_size, head_dim] in dtype, the
+ *               rotated Keys and the Values;
+ *   key_bounds: DEVICE [n_pages, n_kv_heads, 2, head_dim] in dtype, or NULL: for
+ *               each page, KV head and channel the least and the largest value over
+ *               the Keys written to the page since its entry 0 was last written.
+ *               rk_paged_append keeps them, rk_paged_attention_selected reads them.
+ * page_size: a power of two, 16 .. 256.  head_dim: as in rk_model_config.  All
+ * buffers 16-byte aligned.                                                        */
+typedef struct {
+  void *k, *v;
+  void *key_bounds;
+  int64_t n_pages;
+  int32_t page_size, n_kv_heads, head_dim;
+  rk_dtype dtype;
+} rk_paged_cache;
+
+/* The sequences of a call.
+ *   pages:   DEVICE int32; entries [p * page_size, (p + 1) * page_size) of sequence
+ *            i lie on page pages[i * page_stride + p] of the cache, p < max_pages;
+ *            an id outside [0, n_pages) is no page: what would lie on it is neither
+ *            written nor seen.
+ *   lengths: DEVICE int32 [n_seqs]: entries of each sequence, after the append of
+ *            the step (one array serves both calls of a step).  0: an empty
+ *            sequence (a padded row of the batch).  Entries past max_pages *
+ *            page_size are neither written nor seen.
+ * Both are read by the kernels, so a captured call follows them from replay to
+ * replay.                                                                        */
+typedef struct {
+  const int32_t *pages;
+  const int32_t *lengths;
+  int64_t page_stride;
+  int32_t n_seqs, max_pages;
+} rk_paged_seqs;
+
+/* New rows.  offsets: HOST int64 [n_seqs + 1] as in rk_batch (sequence i brings rows
+ * offsets[i] .. offsets[i + 1] - 1, any number of them; n_seqs <=
+ * RK_MAX_BATCH_SEQS), or NULL: one row per sequence, row i to sequence i, any n_seqs.
+ *   k, v:      DEVICE, dtype of the cache, row r of KV head g at k + r *
+ *              k_row_stride + g * k_head_stride (elements), head_dim contiguous
+ *              values; 16-byte aligned, strides whole 16-byte pieces.  The columns
+ *              of a fused q|k|v row and the blocks of rk_snapkv_compress both fit.
+ *   q, q_out:  DEVICE or both NULL: n_heads contiguous heads per row, rotated into
+ *              q_out (the same address for in place).  k and v must not overlap what
+ *              is written.
+ *   positions: DEVICE int32 [rows]: rotary position of each row, or NULL: its entry.
+ *   rope_theta: rotary base, or 0: nothing is rotated (Keys that already are).    */
+typedef struct {
+  const int64_t *offsets;
+  const void *k, *v;
+  int64_t k_row_stride, k_head_stride, v_row_stride, v_head_stride;
+  const void *q;
+  void *q_out;
+  int64_t q_row_stride, q_out_row_stride;
+  int32_t n_heads;
+  float rope_theta;
+  const int32_t *positions;
+} rk_paged_rows;
+
+/* Writes the new Keys, rotated (rotate-half, as the model's projections), and Values
+ * to the entries lengths[i] - m_i .. lengths[i] - 1 of each sequence, m_i its number
+ * of rows, and updates the bounds of their pages.  Rows whose entry is negative or
+ * lies on no page are not written (their queries are still rotated).  No two
+ * sequences of a call may write to the same page.                               */
+rk_status rk_paged_append(const rk_paged_cache *cache, const rk_paged_seqs *seqs, const rk_paged_rows *rows,
+                          void *stream);
+
+/* Workspace bytes of rk_paged_attention (n_select = 0) or of both it and
+ * rk_paged_attention_selected with that many pages; 0 for invalid arguments.     */
+size_t rk_paged_workspace_size(const rk_paged_cache *cache, int32_t n_seqs, int32_t max_pages, int32_t n_heads,
+                               int32_t n_select);
+
+/* Attention of one new token of each sequence over its cache:
+ *   out_i,h = sum_u softmax_u(scale q_i,h . k_u) v_u,  u < lengths[i],
+ * query head h reading KV head h / (n_heads / n_kv_heads).
+ *   q, out: DEVICE, dtype of the cache, sequence i at q + i * q_row_stride elements,
+ *           n_heads contiguous heads; 16-byte aligned rows.
+ *   scale:  0 for 1 / sqrt(head_dim).
+ *   lse:    DEVICE fp32 [n_seqs, n_heads] or NULL: log sum_u e^(scale q . k_u).
+ * A sequence with nothing to see gets zeros and a log-sum-exp of -inf.  fp32
+ * softmax, sums and outputs, rounded once.                                       */
+rk_status rk_paged_attention(const rk_paged_cache *cache, const rk_paged_seqs *seqs, const void *q,
+                             int64_t q_row_stride, int32_t n_heads, float scale, void *out, int64_t out_row_stride,
+                             float *lse, void *workspace, size_t ws_bytes, void *stream);
+
+/* Which pages a query reads.  Per sequence and KV head: the first keep_first and the
+ * last keep_last pages of the sequence, and of the others those with the highest
+ *   sum_{query heads h of the KV head} sum_x max(q_hx lo_x, q_hx hi_x)
+ * (lo, hi the page's key_bounds, terms with q = 0 being 0: no key of the page has a
+ * larger summed product), n_select in all, ties to the lower page.  Scored in double
+ * precision; a NaN score counts as -inf.  n_select >= keep_first + keep_last.
+ *   selected: DEVICE int32 [n_seqs, n_kv_heads, n_select] or NULL: the pages chosen
+ *   (indexes within the sequence), increasing, then -1.                          */
+typedef struct {
+  int32_t n_select, keep_first, keep_last;
+  int32_t *selected;
+} rk_page_selection;
+
+/* rk_paged_attention over the pages that `selection` chooses. */
+rk_status rk_paged_attention_selected(const rk_paged_cache *cache, const rk_paged_seqs *seqs,
+                                      const rk_page_selection *selection, const void *q, int64_t q_row_stride,
+                                      int32_t n_heads, float scale, void *out, int64_t out_row_stride, float *lse,
+                                      void *workspace, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------- token log probabilities */
+
+/* Most alternatives of rk_token_logprobs. */
+#define RK_MAX_TOP 32
+
+/* Workspace bytes of rk_token_logprobs; 0 for invalid arguments. */
+size_t rk_token_logprobs_workspace_size(int64_t n_rows, int32_t vocab, rk_dtype dtype, int32_t n_top);
+
+/* Of each row of logits x (those of rk_profile_layer and rk_policy_damage, or any):
+ *   logprob[r] = x_tok - logsumexp(x), rank[r] = 1 + the number of entries that are
+ *     larger than x_tok, or as large at a lower index (tok = tokens[r]);
+ *   entropy[r] = -sum_v p_v log p_v, in nats;
+ *   top_ids, top_logprobs [n_rows, n_top]: the largest entries, falling, ties to the
+ *     lower index.
+ * logits: DEVICE, fp32 or bf16, row r at logits + r * row_stride elements, any
+ * alignment of the type.  tokens: DEVICE int32 [n_rows]; a token outside [0, vocab)
+ * (a padded row) has logprob 0 and rank 0.  Outputs may be NULL (logprob and rank
+ * without tokens must be).  0 <= n_top <= min(vocab, RK_MAX_TOP).
+ * Entries of -inf have probability 0.  A row whose largest entry is not finite, or
+ * with a NaN, has NaN logprob, entropy and top_logprobs; a NaN ranks as -inf.     */
+rk_status rk_token_logprobs(const void *logits, rk_dtype dtype, int64_t n_rows, int32_t vocab, int64_t row_stride,
+                            const int32_t *tokens, int32_t n_top, float *logprob, int32_t *rank, float *entropy,
+                            int32_t *top_ids, float *top_logprobs, void *workspace, size_t ws_bytes, void *stream);
+
 /* ---------------------------------------------------------------- diagnostics */
 
 /* Per-kernel timing for measurement: after rk_timing_begin(family) every launch
  * of that kernel family is bracketed by HIP events recorded on its launch stream
  * (families: "rmsnorm", "gemm_qkv", "noise", "attention", "gemm_o",
  * "gemm_gate_up", "gemm_down", "lm_lse", "lm_kl", "kl_logits", "lm_logits",
- * "local", "snap_scores", "snap_select").
+ * "local", "snap_scores", "snap_select", "paged_append", "paged_attention",
+ * "page_select", "token_logprobs").
  * rk_timing_end waits for the recorded events, returns the number of launches
  * and their summed duration in milliseconds, and stops recording.  Host-side
  * state is process-wide; not for concurrent use from several threads.          */

@@ -27,7 +27,8 @@ import numpy as np
 
 __all__ = ["RKError", "load", "Model", "Batch", "layer_budgets", "timing_begin", "timing_end", "LIB_PATH", "RK_FLAG_FULL_RECOMPUTE",
            "RK_FLAG_UNFUSED_KL", "RK_FLAG_CACHED_WINDOW", "RK_FLAG_GRAPH", "RK_FLAG_LOCAL_SIGNAL", "RK_FLAG_CHECK_STATE", "RK_WS_CLEAN_STATE", "RK_MAX_BATCH_SEQS", "RK_MAX_GROUP",
-           "RK_POOL_MAX", "RK_POOL_AVG", "RK_SNAPKV_MAX_PREFIX", "RK_STATIC_SCRATCH_BYTES", "snapkv_layout", "spearman"]
+           "RK_POOL_MAX", "RK_POOL_AVG", "RK_SNAPKV_MAX_PREFIX", "RK_STATIC_SCRATCH_BYTES", "snapkv_layout", "spearman",
+           "PagedCache", "PagedSeqs", "token_logprobs", "token_logprobs_workspace_size", "RK_MAX_TOP"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "librk.so")
 
@@ -47,6 +48,7 @@ RK_POOL_MAX = 0
 RK_POOL_AVG = 1
 RK_SNAPKV_MAX_PREFIX = 36864
 RK_STATIC_SCRATCH_BYTES = 128 << 20
+RK_MAX_TOP = 32
 
 _STATUS = {0: "RK_OK", -1: "RK_ERR_ARG", -2: "RK_ERR_SHAPE", -3: "RK_ERR_WORKSPACE", -4: "RK_ERR_HIP",
            -5: "RK_ERR_UNSUPPORTED", -6: "RK_ERR_STATE"}
@@ -86,6 +88,30 @@ class _Params(ctypes.Structure):
 
 class _SnapParams(ctypes.Structure):
     _fields_ = [("obs_window", ctypes.c_int32), ("pool_kernel", ctypes.c_int32), ("pooling", ctypes.c_int)]
+
+
+class _PagedCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("key_bounds", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int)]
+
+
+class _PagedSeqs(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("page_stride", ctypes.c_int64),
+                ("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
+
+
+class _PagedRows(ctypes.Structure):
+    _fields_ = [("offsets", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("k_row_stride", ctypes.c_int64), ("k_head_stride", ctypes.c_int64),
+                ("v_row_stride", ctypes.c_int64), ("v_head_stride", ctypes.c_int64), ("q", ctypes.c_void_p),
+                ("q_out", ctypes.c_void_p), ("q_row_stride", ctypes.c_int64), ("q_out_row_stride", ctypes.c_int64),
+                ("n_heads", ctypes.c_int32), ("rope_theta", ctypes.c_float), ("positions", ctypes.c_void_p)]
+
+
+class _PageSelection(ctypes.Structure):
+    _fields_ = [("n_select", ctypes.c_int32), ("keep_first", ctypes.c_int32), ("keep_last", ctypes.c_int32),
+                ("selected", ctypes.c_void_p)]
 
 
 _lib = None
@@ -138,6 +164,16 @@ def load() -> ctypes.CDLL:
         "rk_snapkv_layout": (i64, [ctypes.POINTER(_Batch), i32, ctypes.POINTER(i64), ctypes.POINTER(i64)]),
         "rk_snapkv_compress": (st, [vp, ctypes.POINTER(_Batch), ctypes.POINTER(_SnapParams), ctypes.POINTER(i64), vp,
                                     sz, vp, vp, vp, vp, vp, sz, vp]),
+        "rk_paged_append": (st, [ctypes.POINTER(_PagedCache), ctypes.POINTER(_PagedSeqs), ctypes.POINTER(_PagedRows),
+                                 vp]),
+        "rk_paged_workspace_size": (sz, [ctypes.POINTER(_PagedCache), i32, i32, i32, i32]),
+        "rk_paged_attention": (st, [ctypes.POINTER(_PagedCache), ctypes.POINTER(_PagedSeqs), vp, i64, i32, f32, vp,
+                                    i64, vp, vp, sz, vp]),
+        "rk_paged_attention_selected": (st, [ctypes.POINTER(_PagedCache), ctypes.POINTER(_PagedSeqs),
+                                             ctypes.POINTER(_PageSelection), vp, i64, i32, f32, vp, i64, vp, vp, sz,
+                                             vp]),
+        "rk_token_logprobs_workspace_size": (sz, [i64, i32, st, i32]),
+        "rk_token_logprobs": (st, [vp, st, i64, i32, i64, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -358,6 +394,196 @@ class Model:
         p = _params(seed, 0, protect_head, protect_tail, 0)
         _check(load().rk_perturb_values(self._h, ctypes.byref(batch._c), int(layer), float(alpha), ctypes.byref(p),
                                         _ptr(v), int(row_stride), _stream(stream)))
+
+
+# ----------------------------------------------------------------------------- paged cache, token log probabilities
+def _dtype_id(t, what: str) -> int:
+    import torch
+    if t.dtype == torch.bfloat16:
+        return RK_BF16
+    if t.dtype == torch.float32:
+        return RK_F32
+    raise ValueError(f"{what}: bfloat16 or float32, not {t.dtype}")
+
+
+def _need(t, what: str, like, dtype, shape=None, contiguous: bool = True):
+    """Checks a tensor of a call (``like``: a tensor that names the device): None passes through."""
+    if t is None:
+        return None
+    if t.device != like.device:
+        raise ValueError(f"{what}: on {t.device}, not on {like.device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{what}: {t.dtype}, not {dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, not {tuple(shape)}")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{what}: must be contiguous")
+    return t
+
+
+def _need_rows(t, what: str, like, n_rows: int, n_heads: int, head_dim: int):
+    """[n_rows, n_heads, head_dim] with heads one after the other in a row: its row stride."""
+    _need(t, what, like, like.dtype, (n_rows, n_heads, head_dim), contiguous=False)
+    _, sh, sd = t.stride()
+    if sd != 1 or (n_heads > 1 and sh != head_dim):
+        raise ValueError(f"{what}: the heads of a row must be contiguous")
+    return t.stride(0) if n_rows > 1 else max(t.stride(0), n_heads * head_dim)
+
+
+def _on_device(tensor, stream, call):
+    """``call(stream)`` with the tensors' device current: on ``stream``, or on that device's current stream."""
+    import torch
+    if tensor.device.index == torch.cuda.current_device():
+        return _check(call(_stream(stream)))
+    with torch.cuda.device(tensor.device):
+        return _check(call(_stream(stream)))
+
+
+def _need_cuda(t, what: str):
+    if t.device.type != "cuda":
+        raise ValueError(f"{what}: must be on the GPU")
+
+
+def _bytes(t) -> int:
+    return t.numel() * t.element_size()
+
+
+class PagedSeqs:
+    """rk_paged_seqs.  ``pages``: int32 [n_seqs, max_pages] (rows may be strided); ``lengths``: int32 [n_seqs],
+    entries of each sequence with the step's new rows counted.  Both stay the caller's and are read by the kernels:
+    updating them in place is how a sequence grows."""
+
+    def __init__(self, pages, lengths):
+        import torch
+        _need_cuda(pages, "pages")
+        if pages.dim() != 2 or pages.shape[0] < 1 or pages.shape[1] < 1:
+            raise ValueError("pages: [n_seqs, max_pages], neither 0")
+        _need(pages, "pages", pages, torch.int32, contiguous=False)
+        n, width = pages.shape
+        if (width > 1 and pages.stride(1) != 1) or pages.stride(0) < 0:
+            raise ValueError("pages: a row must be contiguous")
+        _need(lengths, "lengths", pages, torch.int32, (n,))
+        self.pages, self.lengths, self.n_seqs, self.max_pages = pages, lengths, n, width
+        stride = pages.stride(0) if n > 1 else max(pages.stride(0), width)
+        self._c = _PagedSeqs(pages.data_ptr(), lengths.data_ptr(), stride, n, width)
+
+
+class PagedCache:
+    """rk_paged_cache over the caller's tensors: ``k``, ``v`` [n_pages, n_kv_heads, page_size, head_dim] in bfloat16 or
+    float32, ``key_bounds`` [n_pages, n_kv_heads, 2, head_dim] or None."""
+
+    def __init__(self, k, v, key_bounds=None):
+        _need_cuda(k, "k")
+        if k.dim() != 4:
+            raise ValueError("k: [n_pages, n_kv_heads, page_size, head_dim]")
+        dtype = _dtype_id(k, "k")
+        _need(k, "k", k, k.dtype)
+        _need(v, "v", k, k.dtype, k.shape)
+        n_pages, n_kv, page, d = k.shape
+        _need(key_bounds, "key_bounds", k, k.dtype, (n_pages, n_kv, 2, d))
+        self.k, self.v, self.key_bounds = k, v, key_bounds
+        self.n_kv_heads, self.page_size, self.head_dim = n_kv, page, d
+        self._c = _PagedCache(k.data_ptr(), v.data_ptr(), _ptr(key_bounds), n_pages, page, n_kv, d, dtype)
+
+    def workspace_size(self, n_seqs: int, max_pages: int, n_heads: int, n_select: int = 0) -> int:
+        return int(load().rk_paged_workspace_size(ctypes.byref(self._c), int(n_seqs), int(max_pages), int(n_heads),
+                                                  int(n_select)))
+
+    def append(self, seqs: PagedSeqs, k, v, row_offsets: Optional[Sequence[int]] = None, q=None, q_out=None,
+               positions=None, rope_theta: float = 0.0, stream=None):
+        """rk_paged_append.  k, v: [rows, n_kv_heads, head_dim], any strides of whole 16-byte pieces; row_offsets:
+        host offsets of the sequences' rows, or None for one row each; q, q_out: [rows, n_heads, head_dim]."""
+        import torch
+        _need(seqs.pages, "seqs", self.k, torch.int32, contiguous=False)
+        offsets = None
+        n_rows = seqs.n_seqs
+        if row_offsets is not None:
+            offsets = np.ascontiguousarray(np.asarray(row_offsets, dtype=np.int64))
+            if offsets.shape != (seqs.n_seqs + 1,):
+                raise ValueError(f"row_offsets: {seqs.n_seqs + 1} entries")
+            n_rows = int(offsets[-1])
+        shape = (n_rows, self.n_kv_heads, self.head_dim)
+        for t, what in ((k, "k"), (v, "v")):
+            _need(t, what, self.k, self.k.dtype, shape, contiguous=False)
+            if n_rows and t.stride(2) != 1:
+                raise ValueError(f"{what}: a head's values must be contiguous")
+        n_heads = q_stride = qo_stride = 0
+        if (q is None) != (q_out is None):
+            raise ValueError("q and q_out go together")
+        if q is not None:
+            n_heads = q.shape[1]
+            q_stride = _need_rows(q, "q", self.k, n_rows, n_heads, self.head_dim)
+            qo_stride = _need_rows(q_out, "q_out", self.k, n_rows, n_heads, self.head_dim)
+        _need(positions, "positions", self.k, torch.int32, (n_rows,))
+        if n_rows == 0 and (offsets is None or not offsets.any()):
+            return
+        rows = _PagedRows(None if offsets is None else offsets.ctypes.data, k.data_ptr(), v.data_ptr(), k.stride(0),
+                          k.stride(1), v.stride(0), v.stride(1), _ptr(q), _ptr(q_out), q_stride, qo_stride, n_heads,
+                          rope_theta, _ptr(positions))
+        _on_device(self.k, stream, lambda s: load().rk_paged_append(ctypes.byref(self._c), ctypes.byref(seqs._c),
+                                                                    ctypes.byref(rows), s))
+
+    def _attention_args(self, seqs, q, out, lse, workspace):
+        import torch
+        _need(seqs.pages, "seqs", self.k, torch.int32, contiguous=False)
+        if q.dim() != 3:
+            raise ValueError("q: [n_seqs, n_heads, head_dim]")
+        n_heads = q.shape[1]
+        q_stride = _need_rows(q, "q", self.k, seqs.n_seqs, n_heads, self.head_dim)
+        out_stride = _need_rows(out, "out", self.k, seqs.n_seqs, n_heads, self.head_dim)
+        _need(lse, "lse", self.k, torch.float32, (seqs.n_seqs, n_heads))
+        _need(workspace, "workspace", self.k, workspace.dtype)
+        return n_heads, q_stride, out_stride
+
+    def attention(self, seqs: PagedSeqs, q, out, workspace, scale: float = 0.0, lse=None, stream=None):
+        """rk_paged_attention: q, out [n_seqs, n_heads, head_dim], lse float32 [n_seqs, n_heads]."""
+        n_heads, qs, os_ = self._attention_args(seqs, q, out, lse, workspace)
+        _on_device(self.k, stream, lambda s: load().rk_paged_attention(
+            ctypes.byref(self._c), ctypes.byref(seqs._c), q.data_ptr(), qs, n_heads, scale, out.data_ptr(), os_,
+            _ptr(lse), workspace.data_ptr(), _bytes(workspace), s))
+
+    def attention_selected(self, seqs: PagedSeqs, q, out, workspace, n_select: int, keep_first: int = 1,
+                           keep_last: int = 1, scale: float = 0.0, lse=None, selected=None, stream=None):
+        """rk_paged_attention_selected: selected int32 [n_seqs, n_kv_heads, n_select] or None."""
+        import torch
+        n_heads, qs, os_ = self._attention_args(seqs, q, out, lse, workspace)
+        _need(selected, "selected", self.k, torch.int32, (seqs.n_seqs, self.n_kv_heads, n_select))
+        sel = _PageSelection(n_select, keep_first, keep_last, _ptr(selected))
+        _on_device(self.k, stream, lambda s: load().rk_paged_attention_selected(
+            ctypes.byref(self._c), ctypes.byref(seqs._c), ctypes.byref(sel), q.data_ptr(), qs, n_heads, scale,
+            out.data_ptr(), os_, _ptr(lse), workspace.data_ptr(), _bytes(workspace), s))
+
+
+def token_logprobs_workspace_size(n_rows: int, vocab: int, n_top: int = 0, dtype: str = "f32") -> int:
+    """rk_token_logprobs_workspace_size; dtype "f32" or "bf16"."""
+    return int(load().rk_token_logprobs_workspace_size(int(n_rows), int(vocab), RK_BF16 if dtype == "bf16" else RK_F32,
+                                                       int(n_top)))
+
+
+def token_logprobs(logits, tokens, workspace, logprob=None, rank=None, entropy=None, top_ids=None, top_logprobs=None,
+                   stream=None):
+    """rk_token_logprobs.  logits: [rows, vocab] float32 or bfloat16, rows may be strided; tokens: int32 [rows] or
+    None; logprob, entropy: float32 [rows]; rank: int32 [rows]; top_ids int32 and top_logprobs float32 [rows, n_top]."""
+    import torch
+    _need_cuda(logits, "logits")
+    if logits.dim() != 2:
+        raise ValueError("logits: [rows, vocab]")
+    dtype = _dtype_id(logits, "logits")
+    n, vocab = logits.shape
+    if n and vocab > 1 and logits.stride(1) != 1:
+        raise ValueError("logits: a row must be contiguous")
+    top = next((t.shape[-1] for t in (top_ids, top_logprobs) if t is not None), 0)
+    _need(tokens, "tokens", logits, torch.int32, (n,))
+    _need(logprob, "logprob", logits, torch.float32, (n,))
+    _need(entropy, "entropy", logits, torch.float32, (n,))
+    _need(rank, "rank", logits, torch.int32, (n,))
+    _need(top_ids, "top_ids", logits, torch.int32, (n, top))
+    _need(top_logprobs, "top_logprobs", logits, torch.float32, (n, top))
+    _need(workspace, "workspace", logits, workspace.dtype)
+    stride = logits.stride(0) if n > 1 else max(logits.stride(0), vocab)
+    _on_device(logits, stream, lambda s: load().rk_token_logprobs(
+        logits.data_ptr(), dtype, n, vocab, stride, _ptr(tokens), top, _ptr(logprob), _ptr(rank), _ptr(entropy),
+        _ptr(top_ids), _ptr(top_logprobs), workspace.data_ptr(), _bytes(workspace), s))
 
 
 def spearman(x: Sequence[float], y: Sequence[float]) -> float:

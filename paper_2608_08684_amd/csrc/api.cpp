@@ -223,28 +223,22 @@ struct Timing {
 };
 static Timing g_timing;
 
-class Timed {
- public:
-  Timed(const char* family, hipStream_t s) : s_(s) {
-    if (!g_timing.on || g_timing.family != family) return;
-    if (g_timing.used == g_timing.start.size()) {
-      hipEvent_t a, b;
-      if (hipEventCreate(&a) != hipSuccess) return;
-      if (hipEventCreate(&b) != hipSuccess) { (void)hipEventDestroy(a); return; }
-      g_timing.start.push_back(a);
-      g_timing.stop.push_back(b);
-    }
-    idx_ = (long)g_timing.used++;
-    (void)hipEventRecord(g_timing.start[idx_], s_);
+Timed::Timed(const char* family, hipStream_t s) : s_(s) {
+  if (!g_timing.on || g_timing.family != family) return;
+  if (g_timing.used == g_timing.start.size()) {
+    hipEvent_t a, b;
+    if (hipEventCreate(&a) != hipSuccess) return;
+    if (hipEventCreate(&b) != hipSuccess) { (void)hipEventDestroy(a); return; }
+    g_timing.start.push_back(a);
+    g_timing.stop.push_back(b);
   }
-  ~Timed() {
-    if (idx_ >= 0) (void)hipEventRecord(g_timing.stop[idx_], s_);
-  }
+  idx_ = (long)g_timing.used++;
+  (void)hipEventRecord(g_timing.start[idx_], s_);
+}
 
- private:
-  hipStream_t s_;
-  long idx_ = -1;
-};
+Timed::~Timed() {
+  if (idx_ >= 0) (void)hipEventRecord(g_timing.stop[idx_], s_);
+}
 
 // ----------------------------------------------------------------------------- passes
 #define RK_TRY(expr)                                                       \

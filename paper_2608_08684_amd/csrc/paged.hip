@@ -1,0 +1,780 @@
+// Paged key-value cache: append with the rotary embedding on the way, attention of one
+// new token of each sequence over its pages, and the same over the pages that a bound
+// on their keys' products ranks highest.
+//
+// Cache layout: k and v [n_pages, n_kv_heads, page_size, head_dim], so a page of one
+// head is one contiguous block; bounds [n_pages, n_kv_heads, 2, head_dim], the least
+// and the largest value of each channel over the page's keys.
+#include <math.h>
+
+#include <algorithm>
+
+#include "rk_internal.h"
+
+namespace rk {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4;
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// 16 bytes of cache elements as floats and back (one rounding to nearest even)
+template <typename T> struct Pack;
+template <> struct Pack<bf16_t> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void get(v4u u, float* f) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(u[i] << 16);
+      f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ v4u put(const float* f) {
+    v4u u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = (uint32_t)f2bf(f[2 * i]) | ((uint32_t)f2bf(f[2 * i + 1]) << 16);
+    return u;
+  }
+};
+template <> struct Pack<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void get(v4u u, float* f) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(u[i]);
+  }
+  static __device__ __forceinline__ v4u put(const float* f) {
+    v4u u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(f[i]);
+    return u;
+  }
+};
+
+// e^x of a difference to a running maximum.  The difference is formed before the factor
+// log2(e): scaling the scores themselves would put that factor's rounding, times a
+// score of 50, into the weights.
+__device__ __forceinline__ float exp_diff(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+
+__device__ __forceinline__ int min_i(int a, int b) { return a < b ? a : b; }
+__device__ __forceinline__ int max_i(int a, int b) { return a > b ? a : b; }
+
+// --------------------------------------------------------------------------- append
+// New row r = off[i] + j of sequence i (m_i of them) is entry lengths[i] - m_i + j of
+// the sequence.  With pos its rotary position and x < d / 2,
+//   y[x]         = k[x] cos a - k[x + d/2] sin a
+//   y[x + d/2]   = k[x + d/2] cos a + k[x] sin a,   a = pos theta^(-2x/d);
+// the angle is formed in turns and reduced in double precision (a position of 10^6
+// would leave fp32 four digits of the angle), its sine and cosine in fp32.  One
+// workgroup owns all new rows of a page, so the page's bounds take them in a fixed
+// order without atomics.  Bound: memory (each value read once, written once); a single
+// row: the latency of one pass.
+constexpr int kAppendThreads = 256, kAppendRows = 16;
+
+template <int DH>
+__device__ __forceinline__ float2 turn(const AppendArgs& a, int pos, int x) {
+  if (!a.rotate) return make_float2(1.f, 0.f);
+  const double t = (double)pos * a.freq[x];   // turns
+  float s, c;
+  sincospif((float)(2.0 * (t - rint(t))), &s, &c);
+  return make_float2(c, s);
+}
+
+template <typename T, int DH>
+__global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedView cache, PagedTable tab, AppendArgs a,
+                                                                SeqTable st, int kv_blocks, int q_rows) {
+  constexpr int VE = Pack<T>::N, HALF = DH / 2, UPH = HALF / VE, NT = kAppendThreads;
+  __shared__ float2 cs[kAppendRows][HALF];
+  __shared__ float red[NT][2 * VE];
+  const int tid = threadIdx.x;
+  if ((int)blockIdx.x >= kv_blocks) {
+    // ---- queries of q_rows rows
+    const int r0 = ((int)blockIdx.x - kv_blocks) * q_rows, n = min_i(q_rows, a.n_rows - r0);
+    for (int i = tid; i < n * HALF; i += NT) {
+      const int r = r0 + i / HALF;
+      int pos;
+      if (a.positions) {
+        pos = a.positions[r];
+      } else if (a.one_row) {
+        pos = (int)((uint32_t)tab.lengths[r] - 1u);
+      } else {
+        const int s = seq_of_row(st, r);
+        pos = tab.lengths[s] - (st.off[s + 1] - st.off[s]) + (r - st.off[s]);
+      }
+      cs[i / HALF][i % HALF] = turn<DH>(a, pos, i % HALF);
+    }
+    __syncthreads();
+    const int U = a.n_heads * UPH;
+    for (int i = tid; i < n * U; i += NT) {
+      const int rr = i / U, u = i - rr * U, h = u / UPH, x = (u % UPH) * VE;
+      const T* src = (const T*)a.q + (int64_t)(r0 + rr) * a.q_rs + (int64_t)h * DH + x;
+      T* dst = (T*)a.q_out + (int64_t)(r0 + rr) * a.qo_rs + (int64_t)h * DH + x;
+      float lo[VE], hi[VE], y0[VE], y1[VE];
+      Pack<T>::get(*(const v4u*)src, lo);
+      Pack<T>::get(*(const v4u*)(src + HALF), hi);
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        const float2 c = cs[rr][x + e];
+        y0[e] = lo[e] * c.x - hi[e] * c.y;
+        y1[e] = hi[e] * c.x + lo[e] * c.y;
+      }
+      *(v4u*)dst = Pack<T>::put(y0);
+      *(v4u*)(dst + HALF) = Pack<T>::put(y1);
+    }
+    return;
+  }
+  // ---- keys and values of one page
+  int s, j = 0, row0, m;
+  if (a.one_row) {
+    s = blockIdx.x;
+    row0 = s;
+    m = 1;
+  } else {
+    int lo = 0, hi = st.n - 1;
+    while (lo < hi) {   // the sequence whose page blocks hold this one
+      const int mid = (lo + hi + 1) >> 1;
+      if (a.block0[mid] <= (int)blockIdx.x) lo = mid; else hi = mid - 1;
+    }
+    s = lo;
+    j = (int)blockIdx.x - a.block0[s];
+    row0 = st.off[s];
+    m = st.off[s + 1] - row0;
+  }
+  const int len = tab.lengths[s], first = (int)((uint32_t)len - (uint32_t)m);   // entries first .. len - 1
+  const int p = (max_i(first, 0) >> cache.page_shift) + j;
+  if (p >= tab.max_pages) return;
+  const int e0 = max_i(max_i(first, 0), p << cache.page_shift), e1 = min_i(len, (p + 1) << cache.page_shift);
+  if (e0 >= e1) return;
+  const int page = tab.pages[(int64_t)s * tab.stride + p];
+  if (page < 0 || page >= cache.n_pages) return;
+  const int in_page = e0 & ((1 << cache.page_shift) - 1), n = e1 - e0, r0 = row0 + (e0 - first);
+  const int G = cache.n_kv, ps = 1 << cache.page_shift;
+  const int64_t page_at = (int64_t)page * G * ps * DH;
+  T* kc = (T*)cache.k + page_at;
+  T* vc = (T*)cache.v + page_at;
+  const int U = G * UPH, upt = min_i(U, NT), RP = NT / upt, rp = tid / upt;
+  for (int u0 = 0; u0 < U; u0 += upt) {
+    const int u = u0 + tid % upt, h = u / UPH, x = (u % UPH) * VE;
+    const bool mine = rp < RP && u < U;
+    float bl[2 * VE], bh[2 * VE];
+#pragma unroll
+    for (int e = 0; e < 2 * VE; ++e) { bl[e] = INFINITY; bh[e] = -INFINITY; }
+    for (int b = 0; b < n; b += kAppendRows) {
+      const int nb = min_i(kAppendRows, n - b);
+      __syncthreads();
+      for (int i = tid; i < nb * HALF; i += NT) {
+        const int rr = b + i / HALF;
+        cs[i / HALF][i % HALF] = turn<DH>(a, a.positions ? a.positions[r0 + rr] : e0 + rr, i % HALF);
+      }
+      __syncthreads();
+      if (mine)
+        for (int rr = rp; rr < nb; rr += RP) {
+          const T* src = (const T*)a.k + (int64_t)(r0 + b + rr) * a.k_rs + (int64_t)h * a.k_hs + x;
+          T* dst = kc + ((int64_t)h * ps + in_page + b + rr) * DH + x;
+          float lo[VE], hi[VE], y[2 * VE];
+          Pack<T>::get(*(const v4u*)src, lo);
+          Pack<T>::get(*(const v4u*)(src + HALF), hi);
+#pragma unroll
+          for (int e = 0; e < VE; ++e) {
+            const float2 c = cs[rr][x + e];
+            y[e] = lo[e] * c.x - hi[e] * c.y;
+            y[VE + e] = hi[e] * c.x + lo[e] * c.y;
+          }
+          const v4u w0 = Pack<T>::put(y), w1 = Pack<T>::put(y + VE);
+          *(v4u*)dst = w0;
+          *(v4u*)(dst + HALF) = w1;
+          if (cache.bounds) {   // of the keys as stored
+            Pack<T>::get(w0, y);
+            Pack<T>::get(w1, y + VE);
+#pragma unroll
+            for (int e = 0; e < 2 * VE; ++e) {
+              bl[e] = fminf(bl[e], y[e]);
+              bh[e] = fmaxf(bh[e], y[e]);
+            }
+          }
+        }
+    }
+    if (cache.bounds) {
+      T* bp = (T*)cache.bounds + ((int64_t)page * G + h) * 2 * DH + x;
+#pragma unroll
+      for (int side = 0; side < 2; ++side) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 2 * VE; ++e) red[tid][e] = side ? bh[e] : bl[e];
+        __syncthreads();
+        if (mine && rp == 0) {
+          float y[2 * VE];
+          if (in_page == 0) {   // the page starts here
+#pragma unroll
+            for (int e = 0; e < 2 * VE; ++e) y[e] = red[tid][e];
+          } else {
+            Pack<T>::get(*(const v4u*)(bp + side * DH), y);
+            Pack<T>::get(*(const v4u*)(bp + side * DH + HALF), y + VE);
+#pragma unroll
+            for (int e = 0; e < 2 * VE; ++e) y[e] = side ? fmaxf(y[e], red[tid][e]) : fminf(y[e], red[tid][e]);
+          }
+          for (int q = 1; q < RP; ++q)
+#pragma unroll
+            for (int e = 0; e < 2 * VE; ++e) {
+              const float z = red[tid + q * upt][e];
+              y[e] = side ? fmaxf(y[e], z) : fminf(y[e], z);
+            }
+          *(v4u*)(bp + side * DH) = Pack<T>::put(y);
+          *(v4u*)(bp + side * DH + HALF) = Pack<T>::put(y + VE);
+        }
+      }
+    }
+  }
+  const int CPR = G * (DH / VE);   // 16-byte pieces of a row's values
+  for (int i = tid; i < n * CPR; i += NT) {
+    const int rr = i / CPR, c = i - rr * CPR, h = c / (DH / VE), x = (c % (DH / VE)) * VE;
+    *(v4u*)(vc + ((int64_t)h * ps + in_page + rr) * DH + x) =
+        *(const v4u*)((const T*)a.v + (int64_t)(r0 + rr) * a.v_rs + (int64_t)h * a.v_hs + x);
+  }
+}
+
+// Dispatch on the cache's element type and head size.
+#define RK_PAGED_DISPATCH(bf16, dh, CALL)                                 \
+  do {                                                                    \
+    if (bf16) {                                                           \
+      if (dh == 64) { CALL(bf16_t, 64); } else { CALL(bf16_t, 128); }     \
+    } else {                                                              \
+      if (dh == 32) { CALL(float, 32); }                                  \
+      else if (dh == 64) { CALL(float, 64); }                             \
+      else { CALL(float, 128); }                                          \
+    }                                                                     \
+  } while (0)
+
+hipError_t launch_append(const PagedView& cache, const PagedTable& tab, AppendArgs a, const SeqTable& st,
+                         hipStream_t s) {
+  if (a.n_rows <= 0) return hipSuccess;
+  const int ps = 1 << cache.page_shift;
+  int kv_blocks = 0;
+  if (a.one_row) {
+    kv_blocks = tab.n_seqs;
+  } else {
+    for (int i = 0; i < st.n; ++i) {   // m rows touch at most (m + ps - 2) / ps + 1 pages
+      a.block0[i] = kv_blocks;
+      const int m = st.off[i + 1] - st.off[i];
+      if (m > 0) kv_blocks += (int)(((int64_t)m + ps - 2) / ps) + 1;
+    }
+  }
+  const int q_rows = std::max(1, std::min(kAppendRows, a.n_rows / 1024));
+  const int q_blocks = a.q ? (a.n_rows + q_rows - 1) / q_rows : 0;
+#define RK_APPEND(T, DH) \
+  append_kernel<T, DH><<<kv_blocks + q_blocks, kAppendThreads, 0, s>>>(cache, tab, a, st, kv_blocks, q_rows)
+  RK_PAGED_DISPATCH(cache.bf16, cache.head_dim, RK_APPEND);
+#undef RK_APPEND
+  return hipGetLastError();
+}
+
+// --------------------------------------------------------------------------- attention of one new token
+// o_h = sum_u softmax_u(scale q_h . k_u) v_u over the entries u < length of the
+// sequence; query head h reads KV head h / (H / H_kv).  One pass over the cache with a
+// running maximum m, sum l and output o per wave.  A workgroup = 4 waves serves one
+// (sequence, KV head, part of the length) and up to 16 of the query heads that share
+// the KV head; its waves take the part's 32-entry tiles in turn and are joined through
+// LDS, the parts by a second kernel.
+//   scores  S^T[entry, head] = K Q^T: the cache's rows are the A operand as they lie
+//           in memory, so K goes from memory to the matrix unit's registers directly;
+//   output  O^T[d, head] = V^T P^T: a lane's scores are already the B operand of that
+//           product (entries 4 g + i of its 16-lane group g), and V^T comes out of a
+//           row-major LDS tile with transposing reads (bf16) or from memory with d
+//           spread over the product's rows (fp32).
+// bf16: a weight p is split into bf16(p) + bf16(p - bf16(p)), 16 bits in all: the
+// matrix unit has the time (a tile's 16 KB take longer to arrive than 20 MFMAs), and
+// the output then carries only its own rounding.
+// Entries on pages outside the cache and entries past the length weigh nothing; their
+// scores are replaced by -inf and their values by 0, whatever memory holds there.
+constexpr int kDecodeWaves = 4, kTile = 32;
+
+template <typename T, int DH> struct DecodeTile;
+
+template <int DH> struct DecodeTile<bf16_t, DH> {
+  static constexpr int CH = DH / 8;          // 16-byte pieces of a row
+  static constexpr int NC = DH / 32;         // k-steps of the scores
+  static constexpr int NV = kTile * CH / 64; // 16-byte loads of V per lane
+  static constexpr int ND = DH / 16;         // 16-row blocks of O^T
+  static constexpr int LDS = kTile * DH * 2; // bytes per wave
+  bf16x8_t q[NC];
+  v4u k[2][NC], v[NV];
+
+  // the 32-byte pair of pieces that ds_read_b64_tr_b16 takes from a row, placed so
+  // that eight consecutive rows use all 64 banks
+  static __device__ __forceinline__ int swz(int row) { return DH == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1; }
+
+  __device__ __forceinline__ void load_q(const bf16_t* qp, int lane) {   // row of this lane's head
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      q[c] = __builtin_bit_cast(bf16x8_t, *(const v4u*)(qp + c * 32 + (lane >> 4) * 8));
+  }
+  // rows of the tile's two 16-entry halves
+  __device__ __forceinline__ void load(const bf16_t* k0, const bf16_t* k1, const bf16_t* v0, const bf16_t* v1,
+                                       int lane) {
+    const int at = (lane & 15) * DH + (lane >> 4) * 8;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      k[0][c] = *(const v4u*)(k0 + at + c * 32);
+      k[1][c] = *(const v4u*)(k1 + at + c * 32);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int slot = i * 64 + lane, row = slot / CH;
+      v[i] = *(const v4u*)((row < 16 ? v0 : v1) + (row & 15) * DH + (slot % CH) * 8);
+    }
+  }
+  __device__ __forceinline__ void clear_values(uint32_t seen, int lane) {   // bit r: row r counts
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (!(seen >> ((i * 64 + lane) / CH) & 1)) v[i] = v4u{0, 0, 0, 0};
+  }
+  __device__ __forceinline__ void scores(f32x4_t s[2]) const {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k[t][c]), q[c], s[t], 0, 0, 0);
+    }
+  }
+  __device__ __forceinline__ void values(const f32x4_t p[2], f32x4_t* o, char* lds, int lane) const {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int slot = i * 64 + lane, row = slot / CH, ch = slot % CH;
+      *(v4u*)(lds + (row * CH + (ch ^ swz(row))) * 16) = v[i];
+    }
+    bf16x8_t hi, lo;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float x = p[e >> 2][e & 3];
+      hi[e] = (__bf16)x;
+      lo[e] = (__bf16)(x - (float)hi[e]);
+    }
+    __builtin_amdgcn_wave_barrier();
+    const int g = lane >> 4, jj = lane & 15, r = 4 * g + (jj >> 2);
+#pragma unroll
+    for (int b = 0; b < ND; ++b) {
+      const int ch = 2 * b + ((jj & 3) >> 1);
+      const char* at = lds + (r * CH + (ch ^ swz(r))) * 16 + (jj & 1) * 8;   // swz(r + 16) = swz(r)
+      const s16x4_t a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+      const s16x4_t a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * CH * 16));
+      const v4u a = {__builtin_bit_cast(v2u, a0)[0], __builtin_bit_cast(v2u, a0)[1], __builtin_bit_cast(v2u, a1)[0],
+                     __builtin_bit_cast(v2u, a1)[1]};
+      o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), hi, o[b], 0, 0, 0);
+      o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), lo, o[b], 0, 0, 0);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+  // channel of element i of output block b in 16-lane group g
+  static __device__ __forceinline__ int channel(int b, int g, int i) { return b * 16 + 4 * g + i; }
+};
+
+template <int DH> struct DecodeTile<float, DH> {
+  static constexpr int NC = DH / 16;
+  static constexpr int VEC = DH >= 64 ? 4 : 2;   // channels per lane and load of V
+  static constexpr int NP = DH / (16 * VEC);     // loads per entry
+  static constexpr int ND = DH / 16;
+  static constexpr int LDS = 0;
+  typedef float vecf __attribute__((ext_vector_type(VEC)));
+  f32x4_t q[NC], k[2][NC];
+  vecf v[2][4][NP];
+
+  __device__ __forceinline__ void load_q(const float* qp, int lane) {
+#pragma unroll
+    for (int c = 0; c < NC; ++c) q[c] = *(const f32x4_t*)(qp + c * 16 + (lane >> 4) * 4);
+  }
+  __device__ __forceinline__ void load(const float* k0, const float* k1, const float* v0, const float* v1, int lane) {
+    const int l = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      k[0][c] = *(const f32x4_t*)(k0 + l * DH + c * 16 + g * 4);
+      k[1][c] = *(const f32x4_t*)(k1 + l * DH + c * 16 + g * 4);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < NP; ++c) {
+        v[0][i][c] = *(const vecf*)(v0 + (4 * g + i) * DH + c * 16 * VEC + l * VEC);
+        v[1][i][c] = *(const vecf*)(v1 + (4 * g + i) * DH + c * 16 * VEC + l * VEC);
+      }
+  }
+  __device__ __forceinline__ void clear_values(uint32_t seen, int lane) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (!(seen >> (t * 16 + 4 * (lane >> 4) + i) & 1))
+#pragma unroll
+          for (int c = 0; c < NP; ++c)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) v[t][i][c][e] = 0.f;
+  }
+  __device__ __forceinline__ void scores(f32x4_t s[2]) const {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[t][c][e], q[c][e], s[t], 0, 0, 0);
+    }
+  }
+  __device__ __forceinline__ void values(const f32x4_t p[2], f32x4_t* o, char*, int) const {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < NP; ++c)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e)
+            o[c * VEC + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[t][i][c][e], p[t][i], o[c * VEC + e], 0, 0, 0);
+  }
+  static __device__ __forceinline__ int channel(int b, int g, int i) {
+    return (b / VEC) * 16 * VEC + VEC * (4 * g + i) + b % VEC;
+  }
+};
+
+// Entries of one part of a length: whole tiles for every wave, at most n_parts parts.
+__device__ __forceinline__ int part_entries(int len, int n_parts) {
+  constexpr int unit = kTile * kDecodeWaves;
+  const int per = (len + n_parts - 1) / n_parts;
+  return max_i((per + unit - 1) / unit, 1) * unit;
+}
+
+__device__ __forceinline__ int table_length(const PagedTable& tab, int row, int page_shift) {
+  return max_i(0, (int)min((int64_t)tab.lengths[row], (int64_t)tab.max_pages << page_shift));
+}
+
+template <typename T, int DH>
+__global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cache, PagedTable tab, DecodeArgs a) {
+  using Tile = DecodeTile<T, DH>;
+  constexpr int NW = kDecodeWaves, SP = DH + 4;
+  constexpr int AREA = Tile::LDS * NW > NW * 16 * SP * 4 ? Tile::LDS * NW : NW * 16 * SP * 4;
+  __shared__ __attribute__((aligned(16))) char area[AREA];
+  __shared__ float sm[NW][16], sl[NW][16];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = cache.n_kv, grp = a.n_heads / G, tiles_h = (grp + 15) / 16;
+  // block = ((sequence * G + KV head) * head tiles + head tile) * parts + part
+  int b = blockIdx.x;
+  const int part = b % a.n_parts; b /= a.n_parts;
+  const int ht = b % tiles_h; b /= tiles_h;
+  const int hk = b % G, seq = b / G;
+  const int row = tab.per_head ? seq * G + hk : seq;
+  const int len = table_length(tab, row, cache.page_shift);
+  const int per = part_entries(len, a.n_parts);
+  const int start = part * per, end = min_i(len, start + per);
+  if (part > 0 && start >= len) return;   // the joining kernel knows; part 0 of an empty sequence stays
+  const int nh = min_i(16, grp - ht * 16), h0 = hk * grp + ht * 16;
+  const int32_t* pages = tab.pages + (int64_t)row * tab.stride;
+  const int shift = cache.page_shift, in_mask = (1 << shift) - 1;
+  const int64_t head_at = (int64_t)hk << shift, page_rows = (int64_t)G << shift;
+
+  Tile tile;
+  const int col = lane & 15, g = lane >> 4;
+  tile.load_q((const T*)a.q + (int64_t)seq * a.q_rs + (int64_t)(h0 + min_i(col, nh - 1)) * DH, lane);
+  f32x4_t o[Tile::ND];
+#pragma unroll
+  for (int i = 0; i < Tile::ND; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  for (int k0 = start + w * kTile; k0 < end; k0 += NW * kTile) {
+    const int k1 = k0 + 16;
+    const int p0 = pages[k0 >> shift], p1 = k1 < end ? pages[k1 >> shift] : -1;
+    const bool ok0 = p0 >= 0 && p0 < cache.n_pages, ok1 = p1 >= 0 && p1 < cache.n_pages;
+    // rows of a page that holds nothing are read from page 0 and not used
+    const int64_t at0 = ((ok0 ? p0 : 0) * page_rows + head_at + (k0 & in_mask)) * DH;
+    const int64_t at1 = ((ok1 ? p1 : 0) * page_rows + head_at + (k1 & in_mask)) * DH;
+    tile.load((const T*)cache.k + at0, (const T*)cache.k + at1, (const T*)cache.v + at0, (const T*)cache.v + at1,
+              lane);
+    uint32_t seen = (ok0 ? 0xffffu : 0u) | (ok1 ? 0xffff0000u : 0u);
+    if (end - k0 < 32) seen &= (1u << (end - k0)) - 1u;
+    f32x4_t s[2];
+    tile.scores(s);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[t][i] *= a.scale;
+    if (seen != 0xffffffffu) {
+      tile.clear_values(seen, lane);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!(seen >> (t * 16 + 4 * g + i) & 1)) s[t][i] = -INFINITY;
+    }
+    float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                     fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.f : m_new;
+    const float corr = exp_diff(m - ref);
+    m = m_new;
+    l *= corr;
+#pragma unroll
+    for (int i = 0; i < Tile::ND; ++i) o[i] *= corr;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[t][i] = exp_diff(s[t][i] - ref);
+        l += s[t][i];
+      }
+    tile.values(s, o, area + w * Tile::LDS, lane);
+  }
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  __syncthreads();   // the tiles are done with: their area takes the waves' outputs
+  float* so = (float*)area;
+  if (g == 0) { sm[w][col] = m; sl[w][col] = l; }
+#pragma unroll
+  for (int i = 0; i < Tile::ND; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) so[(w * 16 + col) * SP + Tile::channel(i, g, e)] = o[i][e];
+  __syncthreads();
+  for (int i = tid; i < nh * DH; i += 64 * NW) {
+    const int h = i / DH, x = i % DH;
+    float M = sm[0][h];
+#pragma unroll
+    for (int q = 1; q < NW; ++q) M = fmaxf(M, sm[q][h]);
+    const float ref = M == -INFINITY ? 0.f : M;
+    float L = 0.f, v = 0.f;
+#pragma unroll
+    for (int q = 0; q < NW; ++q) {
+      const float c = exp_diff(sm[q][h] - ref);
+      L += sl[q][h] * c;
+      v += so[(q * 16 + h) * SP + x] * c;
+    }
+    // nothing seen: 0, with a log-sum-exp of -inf (a NaN sum stays NaN)
+    v = L == 0.f ? 0.f : v / L;
+    const float lse = L == 0.f ? -INFINITY : ref + logf(L);
+    const int64_t at = (int64_t)seq * a.n_heads + h0 + h;
+    if (a.n_parts == 1) {
+      Act<T>::store((T*)a.out + (int64_t)seq * a.out_rs + (int64_t)(h0 + h) * DH + x, v);
+      if (a.lse && x == 0) a.lse[at] = lse;
+    } else {
+      a.part_o[(at * a.n_parts + part) * DH + x] = v;
+      if (x == 0) a.part_lse[at * a.n_parts + part] = lse;
+    }
+  }
+}
+
+// Joins the parts of one (sequence, query head): o = sum_s e^(lse_s - M) o_s / sum_s e^(lse_s - M).
+template <typename T, int DH>
+__global__ __launch_bounds__(DH) void decode_join_kernel(PagedTable tab, DecodeArgs a, int n_kv, int page_shift) {
+  const int x = threadIdx.x, seq = blockIdx.x / a.n_heads, h = blockIdx.x % a.n_heads;
+  const int row = tab.per_head ? seq * n_kv + h / (a.n_heads / n_kv) : seq;
+  const int len = table_length(tab, row, page_shift);
+  const int per = part_entries(len, a.n_parts), n = max_i(1, (len + per - 1) / per);
+  const int64_t at = (int64_t)blockIdx.x * a.n_parts;
+  float M = -INFINITY;
+  for (int p = 0; p < n; ++p) M = fmaxf(M, a.part_lse[at + p]);
+  const float ref = M == -INFINITY ? 0.f : M;
+  float L = 0.f, v = 0.f;
+  for (int p = 0; p < n; ++p) {
+    const float c = exp_diff(a.part_lse[at + p] - ref);
+    L += c;
+    v += c * a.part_o[(at + p) * DH + x];
+  }
+  Act<T>::store((T*)a.out + (int64_t)seq * a.out_rs + (int64_t)h * DH + x, L == 0.f ? 0.f : v / L);
+  if (a.lse && x == 0) a.lse[blockIdx.x] = L == 0.f ? -INFINITY : ref + logf(L);
+}
+
+// Parts per (sequence, KV head): enough workgroups for four on each of the 256 CUs, no
+// part shorter than 256 entries.
+int decode_parts(int n_seqs, int n_heads, int n_kv, int64_t max_entries) {
+  const int64_t rows = (int64_t)n_seqs * n_kv * ((n_heads / n_kv + 15) / 16);
+  const int64_t want = (1024 + rows - 1) / rows, most = std::max<int64_t>(1, max_entries / 256);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), 256));
+}
+
+hipError_t launch_decode(const PagedView& cache, const PagedTable& tab, const DecodeArgs& a, hipStream_t s) {
+  const int64_t blocks =
+      (int64_t)tab.n_seqs * cache.n_kv * ((a.n_heads / cache.n_kv + 15) / 16) * a.n_parts;
+#define RK_DECODE(T, DH)                                                                                        \
+  do {                                                                                                          \
+    decode_kernel<T, DH><<<(uint32_t)blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, a);                         \
+    if (a.n_parts > 1)                                                                                          \
+      decode_join_kernel<T, DH><<<tab.n_seqs * a.n_heads, DH, 0, s>>>(tab, a, cache.n_kv, cache.page_shift);    \
+  } while (0)
+  RK_PAGED_DISPATCH(cache.bf16, cache.head_dim, RK_DECODE);
+#undef RK_DECODE
+  return hipGetLastError();
+}
+
+// --------------------------------------------------------------------------- page selection
+// Score of a page for one KV head: sum over the query heads h that share it of
+// sum_x max(q_hx lo_x, q_hx hi_x), an upper bound of the summed products with any key
+// of the page.  The heads can be summed first: sum_x hi_x Q+_x + lo_x Q-_x with
+// Q+ = sum_h max(q_h, 0), Q- = sum_h min(q_h, 0).  In double precision throughout, so
+// the choice does not hang on the order of a sum.  Bound: memory, the bounds of every
+// page read once.
+//
+// A score becomes a whole number that orders the same way: larger for a larger score;
+// the largest of all for pages that are always kept, 0 for pages that hold nothing (a
+// NaN score counts as -inf).
+__device__ __forceinline__ uint64_t score_key(double x) {
+  if (x != x) x = -INFINITY;
+  const uint64_t u = (uint64_t)__double_as_longlong(x + 0.0);   // -0 and 0 are one score
+  return u >> 63 ? ~u : u | 0x8000000000000000ull;
+}
+
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void page_scores_kernel(PagedView cache, PagedTable tab, SelectArgs a, int chunks) {
+  constexpr int VE = Pack<T>::N, LPP = 2 * DH / VE;   // lanes per page: its lower bounds, then its upper
+  __shared__ double qs[2][DH];                        // Q-, Q+
+  const int G = cache.n_kv, grp = a.n_heads / G;
+  const int chunk = blockIdx.x % chunks, sh = blockIdx.x / chunks, seq = sh / G, hk = sh % G;
+  const int len = table_length(tab, seq, cache.page_shift);
+  const int count = (len + (1 << cache.page_shift) - 1) >> cache.page_shift;
+  const int per = (tab.max_pages + chunks - 1) / chunks, first = chunk * per, last = min_i(count, first + per);
+  if (first >= last) return;
+  for (int x = threadIdx.x; x < DH; x += 256) {
+    double lo = 0.0, hi = 0.0;
+    const T* qp = (const T*)a.q + (int64_t)seq * a.q_rs + (int64_t)hk * grp * DH + x;
+    for (int h = 0; h < grp; ++h) {
+      const double v = (double)Act<T>::load(qp + (int64_t)h * DH);
+      lo += v < 0.0 ? v : 0.0;
+      hi += v < 0.0 ? 0.0 : v;
+    }
+    qs[0][x] = lo;
+    qs[1][x] = hi;
+  }
+  __syncthreads();
+  const int sub = threadIdx.x % LPP, x0 = (sub * VE) % DH, side = sub * VE / DH;
+  double q[VE];
+#pragma unroll
+  for (int e = 0; e < VE; ++e) q[e] = qs[side][x0 + e];
+  for (int p = first + threadIdx.x / LPP; p < last; p += 256 / LPP) {
+    const int page = tab.pages[(int64_t)seq * tab.stride + p];
+    const bool ok = page >= 0 && page < cache.n_pages;
+    float f[VE];
+    Pack<T>::get(*(const v4u*)((const T*)cache.bounds + ((int64_t)(ok ? page : 0) * G + hk) * 2 * DH + sub * VE), f);
+    double s = 0.0;
+#pragma unroll
+    for (int e = 0; e < VE; ++e) s += q[e] * (q[e] != 0.0 ? (double)f[e] : 0.0);   // an infinite bound of 0 counts 0
+#pragma unroll
+    for (int d = LPP / 2; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
+    if (sub == 0) {
+      uint64_t key = score_key(s);
+      if (p < a.keep_first || p >= count - a.keep_last) key = ~0ull;
+      a.keys[(int64_t)sh * tab.max_pages + p] = ok ? key : 0ull;
+    }
+  }
+}
+
+constexpr int kSelectThreads = 256;
+
+// One workgroup per (sequence, KV head): the n_select largest keys, ties to the lower
+// page, by the digits of the key from the top, 8 bits a step; the search ends as soon
+// as the pages at or above the digits found are exactly those wanted.
+__global__ __launch_bounds__(kSelectThreads) void page_select_kernel(PagedView cache, PagedTable tab, SelectArgs a) {
+  constexpr int NT = kSelectThreads;
+  static_assert(NT == 256, "a thread per digit");
+  __shared__ int hist[256], scan[NT / 64], found[3], has_last;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, sh = blockIdx.x, seq = sh / cache.n_kv;
+  const int len = table_length(tab, seq, cache.page_shift), ps = 1 << cache.page_shift;
+  const int count = (len + ps - 1) >> cache.page_shift;
+  const uint64_t* keys = a.keys + (int64_t)sh * tab.max_pages;
+  const int32_t* pages = tab.pages + (int64_t)seq * tab.stride;
+  // keys with the digits of `prefix` above `shift` bits: want of them are still to be chosen
+  uint64_t prefix = 0;
+  int want = a.n_select, shift = 64;
+  bool exact = false;   // every key at or above prefix is taken
+  if (count <= a.n_select) {
+    prefix = 1;         // all pages that hold something
+    shift = 0;
+    exact = true;
+  }
+  while (!exact && shift > 0) {
+    shift -= 8;
+    for (int i = tid; i < 256; i += NT) hist[i] = 0;
+    __syncthreads();
+    for (int p = tid; p < count; p += NT) {
+      const uint64_t k = keys[p];
+      if (shift == 56 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1);
+    }
+    __syncthreads();
+    // thread t holds digit 255 - t: the digit at which the counts from the top reach `want`
+    const int c = hist[255 - tid];
+    int sum = c;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(sum, d, 64);
+      if (lane >= d) sum += o;
+    }
+    if (lane == 63) scan[w] = sum;
+    __syncthreads();
+    for (int i = 0; i < w; ++i) sum += scan[i];
+    if (sum >= want && sum - c < want) {
+      found[0] = 255 - tid;
+      found[1] = sum - c;
+      found[2] = c;
+    }
+    __syncthreads();
+    prefix |= (uint64_t)found[0] << shift;
+    want -= found[1];
+    exact = found[2] == want;
+    __syncthreads();
+  }
+  // keys above the prefix, and of those equal to it (all digits used) the first `want`;
+  // keys of 0 hold nothing and are never taken
+  int taken = 0, equal = 0;
+  if (tid == 0) has_last = 0;
+  for (int p0 = 0; p0 < count; p0 += NT) {
+    const int p = p0 + tid;
+    const uint64_t k = p < count ? (count <= a.n_select ? (uint64_t)(pages[p] >= 0 && pages[p] < cache.n_pages) : keys[p])
+                                 : 0ull;
+    bool eq = false, take = false;
+    if (k != 0) {
+      if (exact) take = k >= prefix;
+      else if (k > prefix) take = true;
+      else eq = k == prefix;
+    }
+    // ranks among the equal keys, then among the taken ones, in page order
+    const uint64_t be = __ballot(eq);
+    if (lane == 0) scan[w] = __popcll(be);
+    __syncthreads();
+    int before = equal, all = 0;
+    for (int i = 0; i < NT / 64; ++i) { before += i < w ? scan[i] : 0; all += scan[i]; }
+    __syncthreads();
+    if (eq && before + __popcll(be & ((1ull << lane) - 1)) < want) take = true;
+    equal += all;
+    const uint64_t bt = __ballot(take);
+    if (lane == 0) scan[w] = __popcll(bt);
+    __syncthreads();
+    before = taken;
+    all = 0;
+    for (int i = 0; i < NT / 64; ++i) { before += i < w ? scan[i] : 0; all += scan[i]; }
+    __syncthreads();
+    if (take) {
+      const int at = before + __popcll(bt & ((1ull << lane) - 1));
+      a.list[(int64_t)sh * a.n_select + at] = pages[p];
+      if (a.selected) a.selected[(int64_t)sh * a.n_select + at] = p;
+      if (p == count - 1) has_last = 1;
+    }
+    taken += all;
+  }
+  for (int i = taken + tid; i < a.n_select; i += NT) {
+    a.list[(int64_t)sh * a.n_select + i] = -1;
+    if (a.selected) a.selected[(int64_t)sh * a.n_select + i] = -1;
+  }
+  __syncthreads();
+  // entries of the chosen pages: whole pages, but for the sequence's last one, which comes last
+  if (tid == 0) a.list_len[sh] = taken * ps - (has_last ? count * ps - len : 0);
+}
+
+hipError_t launch_page_select(const PagedView& cache, const PagedTable& tab, const SelectArgs& a, hipStream_t s) {
+  const int rows = tab.n_seqs * cache.n_kv;
+  // a workgroup's fill of 256 threads four times over, split further while CUs are idle
+  const int per_pass = 256 * 16 / (2 * cache.head_dim * (cache.bf16 ? 2 : 4));
+  const int chunks = std::max(1, std::min((tab.max_pages + per_pass - 1) / per_pass, std::max(1, 2048 / rows)));
+#define RK_SCORES(T, DH) page_scores_kernel<T, DH><<<(uint32_t)rows * chunks, 256, 0, s>>>(cache, tab, a, chunks)
+  RK_PAGED_DISPATCH(cache.bf16, cache.head_dim, RK_SCORES);
+#undef RK_SCORES
+  page_select_kernel<<<rows, kSelectThreads, 0, s>>>(cache, tab, a);
+  return hipGetLastError();
+}
+
+}  // namespace rk

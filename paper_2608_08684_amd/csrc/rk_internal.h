@@ -211,7 +211,90 @@ hipError_t launch_snap_select(const float* votes, int64_t prefix_rows, const voi
                               int pool_kernel, bool pool_avg, int n_items, const int16_t* seq, const int16_t* layer,
                               const int32_t* keep, const int64_t* entry0, int32_t* positions, void* k_out, void* v_out,
                               float* scores, hipStream_t s);
+// --------------------------------------------------------------------------- paged cache
+struct PagedView {
+  void *k, *v, *bounds;   // [n_pages, n_kv, 1 << page_shift, head_dim]; bounds [n_pages, n_kv, 2, head_dim] or NULL
+  int64_t n_pages;
+  int page_shift, n_kv, head_dim;
+  bool bf16;
+};
+// Pages and entries of each sequence, or (per_head) of each (sequence, KV head).
+struct PagedTable {
+  const int32_t* pages;     // row i: pages[i * stride ..), max_pages of them
+  const int32_t* lengths;
+  int64_t stride;
+  int n_seqs, max_pages;
+  bool per_head;
+};
+struct AppendArgs {
+  const void *k, *v, *q;
+  void* q_out;
+  int64_t k_rs, k_hs, v_rs, v_hs, q_rs, qo_rs;   // elements
+  const int32_t* positions;
+  int n_rows, n_heads;
+  bool one_row;             // one new row per sequence; otherwise the rows of a SeqTable
+  bool rotate;
+  double freq[64];          // turns per position of channel pair x
+  int block0[RK_MAX_BATCH_SEQS];
+};
+hipError_t launch_append(const PagedView& cache, const PagedTable& tab, AppendArgs a, const SeqTable& st,
+                         hipStream_t s);
+struct DecodeArgs {
+  const void* q;
+  void* out;
+  float* lse;
+  int64_t q_rs, out_rs;     // elements
+  int n_heads, n_parts;
+  float scale;              // of the scores
+  float* part_o;            // [n_seqs * n_heads, n_parts, head_dim], n_parts > 1 only
+  float* part_lse;          // [n_seqs * n_heads, n_parts]
+};
+// Parts that the length is split into (the workspace is sized by it).
+int decode_parts(int n_seqs, int n_heads, int n_kv, int64_t max_entries);
+hipError_t launch_decode(const PagedView& cache, const PagedTable& tab, const DecodeArgs& a, hipStream_t s);
+struct SelectArgs {
+  const void* q;
+  int64_t q_rs;
+  int n_heads, n_select, keep_first, keep_last;
+  uint64_t* keys;           // [n_seqs * n_kv, max_pages]
+  int32_t* list;            // [n_seqs * n_kv, n_select] pages of the cache, then -1
+  int32_t* list_len;        // [n_seqs * n_kv] entries
+  int32_t* selected;        // [n_seqs * n_kv, n_select] pages of the sequence, then -1; or NULL
+};
+hipError_t launch_page_select(const PagedView& cache, const PagedTable& tab, const SelectArgs& a, hipStream_t s);
+
+// --------------------------------------------------------------------------- token log probabilities
+struct LogprobArgs {
+  const void* logits;
+  int64_t row_stride;       // elements
+  int64_t n_rows;
+  int vocab, n_top, chunks, chunk_groups;
+  const int32_t* tokens;
+  float *logprob, *entropy, *top_logprobs;
+  int32_t *rank, *top_ids;
+  float4* part;             // [n_rows, chunks]: max, sum, weighted sum, count (bits)
+  float* group_max;         // [n_rows, groups]
+};
+int logprob_groups(int vocab, bool bf16);
+void logprob_chunks(int64_t n_rows, int vocab, bool bf16, int* chunks, int* chunk_groups);
+hipError_t launch_logprobs(const LogprobArgs& a, bool bf16, hipStream_t s);
+
 hipError_t launch_finalize(const double* s_acc, int n, double inv_n, float* s_out, hipStream_t s);
 hipError_t launch_zero_f64(double* p, int n, hipStream_t s);
+
+// --------------------------------------------------------------------------- host
+// Message of rk_last_error().
+void set_error(const char* fmt, ...);
+
+// Events around the launches of its scope, when their family is being timed.
+class Timed {
+ public:
+  Timed(const char* family, hipStream_t s);
+  ~Timed();
+
+ private:
+  hipStream_t s_;
+  long idx_ = -1;
+};
 
 }  // namespace rk

@@ -1,0 +1,215 @@
+"""Log probabilities of given tokens, ranks, entropies and alternatives against float64."""
+import numpy as np
+import pytest
+
+import paper_2608_08684_amd as rk
+from oracle import paged as OP
+
+from paged_helpers import f64, torch_dtype
+
+pytestmark = pytest.mark.gpu
+
+
+def run(x, tokens, n_top, want=("logprob", "rank", "entropy", "top_ids", "top_logprobs"), **kw):
+    import torch
+    n, vocab = x.shape
+    size = rk.token_logprobs_workspace_size(n, vocab, n_top, "bf16" if x.dtype == torch.bfloat16 else "f32")
+    ws = torch.full((max(size, 1),), 0xFF, dtype=torch.uint8, device="cuda")
+    f = lambda *s: torch.full(s, -77.0, device="cuda")
+    i = lambda *s: torch.full(s, -77, dtype=torch.int32, device="cuda")
+    out = dict(logprob=f(n), rank=i(n), entropy=f(n))
+    if n_top:
+        out.update(top_ids=i(n, n_top), top_logprobs=f(n, n_top))
+    out = {k: v for k, v in out.items() if k in want}
+    rk.token_logprobs(x, tokens, ws, **out, **kw)
+    return out
+
+
+def check(x, tokens, n_top, out):
+    """fp32 sums of n terms, at most n / 256 + 64 in a chain, and exponentials good to 2^-21: S and T are off by at
+    most rel of their absolute terms; a logit's own difference to the maximum by a rounding."""
+    x, tok = f64(x), None if tokens is None else tokens.cpu().numpy()
+    rel = (x.shape[1] / 256 + 64) * 2.0 ** -24 + 2.0 ** -21
+    for r in range(len(x)):
+        lp, rank, h, ids, top = OP.logprobs(x[r], None if tok is None else int(tok[r]), n_top)
+        if "rank" in out:
+            assert int(out["rank"][r]) == rank, r
+        if "top_ids" in out:
+            assert out["top_ids"][r].tolist() == ids, r
+        near = lambda got, want, tol: (np.isnan(got) and np.isnan(want)) or got == want or abs(got - want) <= tol
+        step = lambda v: rel + 2.0 ** -22 * (abs(v) if np.isfinite(v) else 0.0)
+        if "logprob" in out:
+            assert near(float(out["logprob"][r]), lp, step(lp)), (r, float(out["logprob"][r]), lp)
+        if "entropy" in out:    # log S - T / S; |T| / S <= the entropy plus log S <= 2 log n
+            assert near(float(out["entropy"][r]), h, 4 * rel * (1 + np.log(x.shape[1]))), (r, float(out["entropy"][r]), h)
+        if "top_logprobs" in out:
+            for a, b in zip(out["top_logprobs"][r].tolist(), top):
+                assert near(a, b, step(b)), (r, a, b)
+
+
+def logits(rows, vocab, dtype, seed, pad=0, shift=0):
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(rows, vocab, generator=g) * 3
+    x[torch.arange(rows), torch.randint(0, vocab, (rows,), generator=g)] += 12
+    buf = torch.full((rows * (vocab + pad) + shift,), float("nan"), dtype=torch_dtype(dtype), device="cuda")
+    view = buf[shift:].view(rows, vocab + pad)[:, :vocab]
+    view.copy_(x)
+    tok = torch.randint(0, vocab, (rows,), generator=g).to(torch.int32).cuda()
+    return view, tok
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows, vocab, n_top", [
+    (1, 1, 1), (3, 2, 2), (2, 7, 0), (2, 33, 32), (5, 64, 5), (4, 65, 1), (3, 127, 20), (3, 1000, 32), (2, 4099, 7),
+    (1, 32000, 5), (2, 50257, 20), (1, 128256, 32), (40, 777, 3),
+])
+def test_sizes(dtype, rows, vocab, n_top):
+    x, tok = logits(rows, vocab, dtype, vocab + n_top)
+    check(x, tok, n_top, run(x, tok, n_top))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pad, shift", [(0, 1), (1, 0), (3, 5), (7, 3), (64, 0)])
+def test_rows_at_any_address(dtype, pad, shift):
+    """Rows that start anywhere; what surrounds them is NaN."""
+    x, tok = logits(9, 333, dtype, 1, pad, shift)
+    check(x, tok, 6, run(x, tok, 6))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_rows(dtype):
+    x, tok = logits(1500, 300, dtype, 2)
+    check(x, tok, 4, run(x, tok, 4))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n_top", [1, 5, 32])
+def test_ties(dtype, n_top):
+    """Few distinct values, a constant row, largest logits at the ends, signed zeros, falling and rising rows."""
+    import torch
+    g = torch.Generator().manual_seed(3)
+    x = torch.randint(-2, 3, (8, 2500), generator=g).float()
+    x[1] = 1.5
+    x[2] = 0.0
+    x[2, ::3] = -0.0
+    x[3] = torch.arange(2500) * -0.25
+    x[4] = torch.arange(2500) * 0.25
+    x[5, [0, 63, 64, 2499]] = 9.0
+    x = x.to(torch_dtype(dtype)).cuda()
+    tok = torch.tensor([0, 2499, 1, 17, 2499, 2499, 1200, 64], dtype=torch.int32).cuda()
+    check(x, tok, n_top, run(x, tok, n_top))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_masked_and_non_finite(dtype):
+    """-inf entries have no probability; the type's lowest value has none beside others; rows that have no
+    distribution say so, and leave the rows beside them alone."""
+    import torch
+    x, tok = logits(12, 700, dtype, 4)
+    low = torch.finfo(x.dtype).min
+    x[0, :600] = -float("inf")
+    tok[0] = 3                      # a token that is masked
+    x[1] = -float("inf")
+    x[1, 650] = -2.0
+    tok[1] = 650
+    x[2] = -float("inf")
+    x[3, 5] = float("inf")
+    x[4, 5] = float("nan")
+    x[5] = low
+    x[6, 100:] = low
+    x[7] = -float("inf")
+    x[7, 3] = float("nan")
+    tok[7] = 3
+    x[8] = 1.0e4
+    x[9, 0] = 1.0e30
+    x[9, 1] = -1.0e30
+    x[10] = float("inf")
+    check(x, tok, 20, run(x, tok, 20))
+
+
+def test_tokens_outside_the_vocabulary():
+    import torch
+    x, tok = logits(5, 400, "f32", 5)
+    tok.copy_(torch.tensor([-1, 400, -2 ** 31, 2 ** 31 - 1, 399], dtype=torch.int32))
+    out = run(x, tok, 2)
+    check(x, tok, 2, out)
+    assert out["logprob"][:4].tolist() == [0.0] * 4 and out["rank"][:4].tolist() == [0] * 4
+
+
+@pytest.mark.parametrize("want", [("logprob",), ("rank",), ("entropy",), ("top_ids",), ("top_logprobs",),
+                                  ("logprob", "entropy")])
+def test_outputs_one_by_one(want):
+    x, tok = logits(3, 1300, "f32", 6)
+    n_top = 4 if "top" in want[0] else 0
+    out = run(x, tok if want[0] in ("logprob", "rank") else None, n_top, want)
+    assert set(out) == set(want)
+    check(x, tok, n_top, out)
+
+
+def test_no_rows():
+    x, tok = logits(1, 50, "f32", 7)
+    run(x[:0], tok[:0], 3)
+
+
+def test_a_confident_row_keeps_its_digits():
+    """One logit far above the others: log p and the entropy are as small as they are, not as the logits are."""
+    import torch
+    x = torch.zeros(1, 1000, device="cuda")
+    x[0, 3] = 30.0
+    tok = torch.tensor([3], dtype=torch.int32, device="cuda")
+    out = run(x, tok, 1)
+    assert abs(float(out["logprob"][0])) < 2.0 ** -23 and abs(float(out["entropy"][0])) < 2.0 ** -20
+
+
+def test_beyond_32_bit_offsets():
+    """Rows whose byte offsets need more than 32 bits."""
+    import torch
+    vocab, rows = 128256, 9000
+    buf = torch.empty(rows, vocab, device="cuda")
+    x, tok = logits(3, vocab, "f32", 8)
+    far = buf[rows - 1 - 2 * 4000::4000]
+    far.copy_(x)
+    a, b = run(far, tok, 8), run(x, tok, 8)
+    assert all(torch.equal(a[k], b[k]) for k in a)
+    check(x, tok, 8, b)
+
+
+def test_streams_and_graphs():
+    import torch
+    x, tok = logits(20, 5000, "bf16", 9)
+    ref = run(x, tok, 5)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        other = run(x, tok, 5)
+    s.synchronize()
+    assert all(torch.equal(ref[k], other[k]) for k in ref)
+    ws = torch.empty(rk.token_logprobs_workspace_size(20, 5000, 5, "bf16"), dtype=torch.uint8, device="cuda")
+    out = {k: torch.empty_like(v) for k, v in ref.items()}
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        rk.token_logprobs(x, tok, ws, **out)
+    for k in range(4):
+        g.replay()
+        torch.cuda.synchronize()
+        eager = run(x, tok, 5)
+        assert all(torch.equal(eager[name], out[name]) for name in out)
+        x.copy_(x.roll(101 * (k + 1), 1))
+
+
+def test_binding_refusals():
+    import torch
+    x, tok = logits(4, 100, "f32", 10)
+    ws = torch.empty(1 << 16, dtype=torch.uint8, device="cuda")
+    f, i = torch.empty(4, device="cuda"), torch.empty(4, dtype=torch.int32, device="cuda")
+    for args, kw in (((x.half(), tok, ws), dict(logprob=f)), ((x, tok.long(), ws), dict(logprob=f)),
+                     ((x, tok[:3], ws), dict(logprob=f)), ((x, tok, ws), dict(logprob=f[:3])),
+                     ((x, tok, ws), dict(logprob=f.double())), ((x, tok, ws), dict(rank=f)),
+                     ((x, tok, ws.cpu()), dict(logprob=f)), ((x.T, tok, ws), dict(logprob=f)), ((x, tok, ws), {}),
+                     ((x, None, ws), dict(rank=i)), ((x, tok, ws[:64]), dict(logprob=f)),
+                     ((x, tok, ws), dict(top_ids=torch.empty(4, 33, dtype=torch.int32, device="cuda"))),
+                     ((x, tok, ws), dict(top_ids=torch.empty(4, 2, dtype=torch.int32, device="cuda"),
+                                         top_logprobs=torch.empty(4, 3, device="cuda")))):
+        with pytest.raises((ValueError, rk.RKError)):
+            rk.token_logprobs(*args, **kw)
