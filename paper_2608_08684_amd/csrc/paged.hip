@@ -352,7 +352,7 @@ template <int DH> struct DecodeTile<bf16_t, DH> {
       hi[e] = (__bf16)x;
       lo[e] = (__bf16)(x - (float)hi[e]);
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_sync();
     const int g = lane >> 4, jj = lane & 15, r = 4 * g + (jj >> 2);
 #pragma unroll
     for (int b = 0; b < ND; ++b) {
@@ -365,7 +365,7 @@ template <int DH> struct DecodeTile<bf16_t, DH> {
       o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), hi, o[b], 0, 0, 0);
       o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), lo, o[b], 0, 0, 0);
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_sync();
   }
   // channel of element i of output block b in 16-lane group g
   static __device__ __forceinline__ int channel(int b, int g, int i) { return b * 16 + 4 * g + i; }

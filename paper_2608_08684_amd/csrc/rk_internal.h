@@ -40,6 +40,14 @@ __device__ __forceinline__ float bf2f(bf16_t b) { return __uint_as_float(((uint3
 // fp32 -> bf16, round to nearest even (gfx950 v_cvt_pk_bf16_f32; NaN stays NaN).
 __device__ __forceinline__ bf16_t f2bf(float f) { return __builtin_bit_cast(bf16_t, (__bf16)f); }
 
+// Orders a wave's LDS accesses across its lanes: what any lane wrote before, every lane
+// reads after.  (The hardware keeps them in order; this keeps the compiler to it.)
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 __device__ __forceinline__ int seq_of_row(const SeqTable& st, int r) {
   int lo = 0, hi = st.n - 1;
   while (lo < hi) {  // largest k with off[k] <= r
@@ -272,8 +280,8 @@ struct LogprobArgs {
   const int32_t* tokens;
   float *logprob, *entropy, *top_logprobs;
   int32_t *rank, *top_ids;
-  float4* part;             // [n_rows, chunks]: max, sum, weighted sum, count (bits)
-  float* group_max;         // [n_rows, groups]
+  float4* part;             // [n_rows, chunks]: reference, sum, weighted sum, count (bits)
+  uint32_t* group_keys;     // [n_rows, groups] order of the groups' largest logits
 };
 int logprob_groups(int vocab, bool bf16);
 void logprob_chunks(int64_t n_rows, int vocab, bool bf16, int* chunks, int* chunk_groups);

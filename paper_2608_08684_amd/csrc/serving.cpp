@@ -290,7 +290,7 @@ rk_status rk_token_logprobs(const void *logits, rk_dtype dtype, int64_t n_rows, 
   a.logits = logits; a.row_stride = row_stride; a.n_rows = n_rows; a.vocab = vocab; a.n_top = n_top;
   a.tokens = tokens; a.logprob = logprob; a.rank = rank; a.entropy = entropy;
   a.top_ids = top_ids; a.top_logprobs = top_logprobs;
-  a.part = (float4*)workspace; a.group_max = (float*)((char*)workspace + gmax);
+  a.part = (float4*)workspace; a.group_keys = (uint32_t*)((char*)workspace + gmax);
   Timed timed("token_logprobs", s);
   return hip_status("token log probabilities", launch_logprobs(a, dtype == RK_BF16, s));
 }
