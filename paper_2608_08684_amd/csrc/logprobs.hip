@@ -10,26 +10,34 @@
 // its digits next to 0).  The difference is formed before the factor log2(e) of the
 // exponential: x log2(e) would overflow at the type's lowest value, a common mask.
 //
-// Each logit is read once: a running (c, S, T) per thread, joined in a fixed order.
-// The alternatives come out of the same pass by groups of consecutive logits (16 lanes
-// times one 16-byte load): the n best logits, ordered by value and then by lower index,
-// lie in the n groups whose largest logits come first in that order (each of those
-// groups holds at least one logit that precedes any logit of another group), so only
-// those groups are looked at again, by one wave.
+// A workgroup reads each logit of a row (of a part of a long row, where rows are few)
+// once: a running (c, S, T) per thread, joined in a fixed order.  The alternatives come
+// out of the same pass by groups of 16 vectors (4 lanes, 4 passes): if n groups have a
+// logit that reaches a bound, the n best logits lie in the groups whose largest logit
+// reaches it.  Only those are looked at again, shared out over the waves.  Where equal
+// logits make them too many (a constant row, a mask that leaves fewer than n), the bound
+// is the n-th largest of the groups' largest logits: the logits above it come from the
+// groups above it, and the rest are the first logits of the row that equal it.
+//
+// Bound: memory for many rows, the chain of dependent steps for few.
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "rk_internal.h"
 
 namespace rk {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kLpThreads = 256;
 
 template <typename T> struct Logit;
 template <> struct Logit<float> {
   static constexpr int N = 4;
+  static __device__ __forceinline__ v4u none() { return v4u{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u}; }
+  static __device__ __forceinline__ v4u put(const float* f) {
+    return v4u{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+  }
   static __device__ __forceinline__ void get(v4u u, float* f) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(u[i]);
@@ -37,6 +45,13 @@ template <> struct Logit<float> {
 };
 template <> struct Logit<bf16_t> {
   static constexpr int N = 8;
+  static __device__ __forceinline__ v4u none() { return v4u{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u}; }
+  static __device__ __forceinline__ v4u put(const float* f) {
+    v4u u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = (uint32_t)f2bf(f[2 * i]) | ((uint32_t)f2bf(f[2 * i + 1]) << 16);
+    return u;
+  }
   static __device__ __forceinline__ void get(v4u u, float* f) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -59,31 +74,19 @@ struct Sums {
     s *= f;
     c = c2;
   }
-  __device__ __forceinline__ void join(Sums o) {
-    const float m = fmaxf(c, o.c);
-    if (m == -INFINITY) {   // nothing but -inf so far; a NaN has left its mark on the sums
-      s += o.s;
-      t += o.t;
-      return;
-    }
-    raise(m);
-    o.raise(m);
-    s += o.s;
-    t += o.t;
-  }
 };
 
-// A row seen as 16-byte vectors: vector v holds logits v N - shift .. of the row.
+// A row, or a part of one, as 16-byte vectors: vector v holds logits v N - shift .. of it.
 template <typename T> struct RowView {
   static constexpr int N = Logit<T>::N;
   const T* row;
   const v4u* base;   // aligned address at or below the row's first logit
   int shift, vocab, n_vec;
-  __device__ __forceinline__ RowView(const LogprobArgs& a, int64_t r) {
-    row = (const T*)a.logits + r * a.row_stride;
+  __device__ __forceinline__ RowView(const T* first, int n) {
+    row = first;
     shift = (int)(((uintptr_t)row & 15) / sizeof(T));
-    base = (const v4u*)((uintptr_t)row & ~(uintptr_t)15);
-    vocab = a.vocab;
+    base = (const v4u*)(row - shift);
+    vocab = n;
     n_vec = (int)(((int64_t)shift + vocab + N - 1) / N);
   }
   // vectors v .. v + n - 1 lie whole within the row
@@ -91,14 +94,15 @@ template <typename T> struct RowView {
     return v * N >= shift && (int64_t)(v + n) * N - shift <= vocab;
   }
   // vectors that reach outside the row are read logit by logit; what is outside is -inf
-  __device__ __forceinline__ void load(int v, float* f) const {
+  __device__ __forceinline__ v4u load(int v) const {
+    if (inside(v, 1)) return base[v];
     const int id = v * N - shift;
-    if (id >= 0 && id <= vocab - N) {
-      Logit<T>::get(base[v], f);
-    } else {
+    float f[N];
 #pragma unroll
-      for (int e = 0; e < N; ++e) f[e] = id + e >= 0 && id + e < vocab ? Act<T>::load(row + id + e) : -INFINITY;
-    }
+    for (int e = 0; e < N; ++e) f[e] = Act<T>::load(row + min(max(id + e, 0), vocab - 1));
+#pragma unroll
+    for (int e = 0; e < N; ++e) f[e] = id + e >= 0 && id + e < vocab ? f[e] : -INFINITY;
+    return Logit<T>::put(f);
   }
 };
 
@@ -109,21 +113,32 @@ __device__ __forceinline__ uint32_t order_bits(float x) {
   return u >> 31 ? ~u : u | 0x80000000u;
 }
 
-// Largest of a value over the wave (unsigned), by row shifts and broadcasts.
-__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
-#define RK_STEP(ctrl, rows) \
-  { const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, false); x = o > x ? o : x; }
+// Folds a value over the wave by row shifts and broadcasts; every lane gets the result.
+template <typename F>
+__device__ __forceinline__ uint32_t wave_fold(uint32_t x, F f) {   // 0 is the identity of f
+#define RK_STEP(ctrl, rows) x = f(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, false));
   RK_STEP(0x111, 0xf) RK_STEP(0x112, 0xf) RK_STEP(0x114, 0xf) RK_STEP(0x118, 0xf)   // row_shr 1, 2, 4, 8
   RK_STEP(0x142, 0xa) RK_STEP(0x143, 0xc)                                           // row_bcast 15, 31
 #undef RK_STEP
   return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
 }
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  return wave_fold(x, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+__device__ __forceinline__ int wave_count(int x) {
+  return (int)wave_fold((uint32_t)x, [](uint32_t a, uint32_t b) { return a + b; });
+}
+__device__ __forceinline__ float wave_total(float x) {
+  return __uint_as_float(wave_fold(__float_as_uint(x), [](uint32_t a, uint32_t b) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }));
+}
 
-// Largest over the 16 lanes of a row, in every one of them.
-__device__ __forceinline__ float row_max(float x) {
+// Largest over each four lanes, in every one of them.
+__device__ __forceinline__ uint32_t quad_max(uint32_t x) {
 #define RK_STEP(ctrl) \
-  x = fmaxf(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), ctrl, 0xf, 0xf, false)));
-  RK_STEP(0x128) RK_STEP(0x124) RK_STEP(0x122) RK_STEP(0x121)   // row_ror 8, 4, 2, 1
+  { const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, 0xf, 0xf, false); x = o > x ? o : x; }
+  RK_STEP(0xb1) RK_STEP(0x4e)   // quad_perm 1 0 3 2, 2 3 0 1
 #undef RK_STEP
   return x;
 }
@@ -131,155 +146,166 @@ __device__ __forceinline__ float row_max(float x) {
 // The float of order_bits.
 __device__ __forceinline__ float from_order(uint32_t k) { return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k); }
 
-constexpr int kTopGroups = 4096;   // group keys held in LDS
-constexpr int kTopList = 256;      // candidates held in LDS
-
-struct TopShared {
-  v4u keys[kTopGroups / 4];
-  uint64_t list[kTopList];
-  int chosen[RK_MAX_TOP];
-  int n_chosen, count;
-};
-
-// One wave: groups of the n largest keys (ties to the lower group) into sh.chosen; the
-// smallest key taken.  A search between the least of the lanes' best keys and the best
-// of all: about ten steps of counting, whatever n is.  KEYS(i): keys 4 i .. 4 i + 3, 0
-// past the last group.
-template <typename Keys>
-__device__ __forceinline__ uint32_t choose_groups(int n_groups, int n, TopShared& sh, Keys keys) {
-  const int lane = threadIdx.x & 63, its = (n_groups + 255) / 256;
-  uint32_t best = 0;
-  for (int it = 0; it < its; ++it) {
-    const v4u k = keys(it * 64 + lane);
-    best = max(max(max(best, k[0]), max(k[1], k[2])), k[3]);
-  }
-  // n <= 64 lanes: at least n keys reach the least of the lanes' best
-  uint32_t hi = wave_max(best), lo = max(~wave_max(~best), 1u);
-  int above = 0;
-  bool exact = false;
-  if (n_groups == n) { lo = 1; exact = true; }
-  while (!exact && lo < hi) {
-    const uint32_t mid = lo + (hi - lo + 1) / 2;
-    int c = 0;
-    for (int it = 0; it < its; ++it) {
-      const v4u k = keys(it * 64 + lane);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) c += __popcll(__ballot(k[e] >= mid));
-    }
-    if (c >= n) lo = mid; else hi = mid - 1;
-    exact = c == n;
-  }
-  // keys above lo, and of those equal to it the first that are still wanted
-  if (lane == 0) sh.n_chosen = 0;
-  wave_sync();
-  if (!exact)
-    for (int it = 0; it < its; ++it) {
-      const v4u k = keys(it * 64 + lane);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) above += __popcll(__ballot(k[e] > lo));
-    }
-  int want = n - above;
-  for (int it = 0; it < its; ++it) {
-    const v4u k = keys(it * 64 + lane);
-    int equal = 0, before = 0, all = 0;
-    if (!exact) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint64_t b = __ballot(k[e] == lo);
-        before += __popcll(b & ((1ull << lane) - 1));
-        all += __popcll(b);
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const bool tie = !exact && k[e] == lo;
-      if (tie ? before + equal < want : k[e] >= lo && k[e] != 0) sh.chosen[atomicAdd(&sh.n_chosen, 1)] = (it * 64 + lane) * 4 + e;
-      equal += tie;
-    }
-    want -= all;
-  }
-  wave_sync();
-  return lo;
+// The wave's sums, all moved to the largest reference.  (A lane that has met a NaN or an
+// infinity holds a NaN sum, and that stays.)
+__device__ __forceinline__ Sums wave_sums(Sums q) {
+  const float m = from_order(wave_max(order_bits(q.c)));
+  if (m > -INFINITY) q.raise(m);
+  return Sums{m, wave_total(q.s), wave_total(q.t)};
 }
 
-// One wave: the n_top best logits of row r, given the groups' keys, c and log S.
-template <typename T>
-__device__ __forceinline__ void top_of_row(const LogprobArgs& a, const RowView<T>& x, int64_t r,
-                                           const uint32_t* group_keys, float c, float log_s, TopShared& sh) {
-  constexpr int N = Logit<T>::N, PASSES = RK_MAX_TOP / 4;
-  const int lane = threadIdx.x & 63;
-  const int n_groups = (x.n_vec + 15) / 16, n_ch = min(n_groups, a.n_top);
-  const auto load_keys = [&](int i) {   // rows of keys are padded to whole vectors
-    v4u k = v4u{0, 0, 0, 0};
-    if (4 * i < n_groups) {
-      k = reinterpret_cast<const v4u*>(group_keys)[i];
+constexpr int kPasses = 4;         // vectors in flight per lane
+constexpr int kTopGroups = 4096;   // groups of a row or part: 65536 vectors
+constexpr int kTopLook = 128;      // groups looked at again
+constexpr int kTopList = 256;      // candidates held in LDS
+constexpr int kMaxParts = 64;
+
+template <int NT> struct TopShared {
+  v4u keys[kTopGroups / 4];        // order of each group's largest logit, 0 for a group without logits
+  uint32_t best[NT / 4];           // the largest key of each four lanes
+  uint64_t list[kTopList];
+  int chosen[kTopLook], n_chosen, n_list;
+  uint32_t tau;                    // of the search over every key:
+  int n_look, all;
+};
+
+// The workgroup: the n best logits of x, given the groups' keys; put(i, order, id) takes
+// the i-th.  An earlier barrier has made keys and best visible and n_chosen, n_list 0.
+template <typename T, int NT, typename Put>
+__device__ __forceinline__ void top_logits(const RowView<T>& x, int n, int n_groups, TopShared<NT>& sh, Put put) {
+  constexpr int N = Logit<T>::N, NW = NT / 64, NB = NT / 256;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint64_t lower = (1ull << lane) - 1;
+  // ---- a bound that n or a few more of the best keys reach, by halving an interval (1:
+  // there are no n of them, every logit is a candidate); the same in every wave
+  uint32_t bound = 1;
+  {
+    uint32_t best[NB], top = 0;
 #pragma unroll
-      for (int e = 1; e < 4; ++e) k[e] = 4 * i + e < n_groups ? k[e] : 0u;
+    for (int i = 0; i < NB; ++i) {
+      best[i] = sh.best[i * 64 + lane];
+      top = max(top, best[i]);
     }
-    return k;
+    // every lane's largest reaches the least of them: 64 keys, if no lane is without one
+    uint32_t hi = wave_max(top);
+    bound = max(~wave_max(~top), 1u);
+    while (bound < hi) {
+      const uint32_t mid = bound + (hi - bound + 1) / 2;
+      int c = 0;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) c += __popcll(__ballot(best[i] >= mid));
+      if (c >= n) bound = mid; else hi = mid - 1;
+      if (c >= n && c <= n + n / 8 + 1) break;
+    }
+  }
+  for (int i0 = w * 64; i0 < n_groups / 4; i0 += NT) {
+    const int i = i0 + lane;
+    const v4u k = i < n_groups / 4 ? sh.keys[i] : v4u{0, 0, 0, 0};
+    int mine = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) mine += k[e] >= bound;
+    if (__ballot(mine > 0) == 0) continue;
+    if (mine) {
+      int at = atomicAdd(&sh.n_chosen, mine);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (k[e] >= bound) {
+          if (at < kTopLook) sh.chosen[at] = 4 * i + e;
+          ++at;
+        }
+    }
+  }
+  __syncthreads();
+  int n_ch = sh.n_chosen;
+  bool all = true;   // the chosen groups have every logit of at least the bound, or else every one above it
+  if (n_ch > kTopLook) {
+    // ---- the n-th largest key itself, and the groups above it, with those equal to it if they fit
+    if (w == 0) {
+      const auto reaching = [&](uint32_t b) {
+        int c = 0;
+        for (int i = lane; i < n_groups / 4; i += 64) {
+          const v4u k = sh.keys[i];
+          c += (k[0] >= b) + (k[1] >= b) + (k[2] >= b) + (k[3] >= b);
+        }
+        return wave_count(c);
+      };
+      uint32_t lo = bound, hi = ~0u;
+      while (lo < hi) {
+        const uint32_t mid = lo + (hi - lo) / 2 + 1;
+        if (reaching(mid) >= n) lo = mid; else hi = mid - 1;
+      }
+      const bool fits = reaching(lo) <= kTopLook;
+      const uint32_t from = fits ? lo : lo + 1;
+      int taken = 0;
+      for (int i0 = 0; i0 < n_groups / 4; i0 += 64) {
+        const int i = i0 + lane;
+        const v4u k = i < n_groups / 4 ? sh.keys[i] : v4u{0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint64_t b = __ballot(k[e] >= from);
+          if (k[e] >= from) sh.chosen[taken + __popcll(b & lower)] = 4 * i + e;
+          taken += __popcll(b);
+        }
+      }
+      if (lane == 0) { sh.n_look = taken; sh.tau = lo; sh.all = fits; }
+    }
+    __syncthreads();
+    n_ch = sh.n_look;
+    bound = sh.tau;
+    all = sh.all;
+  }
+  const uint32_t from = all ? bound : bound + 1;
+  // vector l of chosen group i
+  const auto vector_of = [&](int i, int l) {
+    const int g = sh.chosen[i], wave = g / 16;
+    return wave / NW * (NT * kPasses) + (l / 4) * NT + wave % NW * 64 + g % 16 * 4 + l % 4;
   };
-  uint32_t tau;
-  if (n_groups <= kTopGroups) {
-    const int its = (n_groups + 255) / 256;
-#pragma unroll 4
-    for (int it = 0; it < its; ++it) sh.keys[it * 64 + lane] = load_keys(it * 64 + lane);
-    wave_sync();
-    tau = choose_groups(n_groups, n_ch, sh, [&](int i) { return sh.keys[i]; });
-  } else {
-    tau = choose_groups(n_groups, n_ch, sh, load_keys);
-  }
-  if (lane == 0) sh.count = 0;
-  wave_sync();
-  // ---- logits of those groups at or above the last group's best: n_top of them or more
-  v4u raw[PASSES];
-#pragma unroll
-  for (int p = 0; p < PASSES; ++p) {
-    const int i = p * 4 + lane / 16, v = i < n_ch ? sh.chosen[i] * 16 + (lane & 15) : -1;
-    if (v >= 0 && x.inside(v, 1)) raw[p] = x.base[v];
-  }
-  if (n_ch < a.n_top) tau = 1;   // every logit counts
-#pragma unroll
-  for (int p = 0; p < PASSES; ++p) {
-    const int i = p * 4 + lane / 16, v = i < n_ch ? sh.chosen[i] * 16 + (lane & 15) : x.n_vec;
+  // ---- the chosen groups' logits at or above `from`, four groups a step and wave
+#pragma unroll 1
+  for (int p = w; p * 4 < n_ch; p += NW) {
+    const int i = p * 4 + lane / 16, v = i < n_ch ? vector_of(i, lane & 15) : x.n_vec;
     if (v < x.n_vec) {
       float f[N];
-      if (x.inside(v, 1)) Logit<T>::get(raw[p], f); else x.load(v, f);
+      Logit<T>::get(x.load(v), f);
+      uint32_t hits = 0;
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         const int id = v * N - x.shift + e;
-        const uint32_t k = order_bits(f[e]);
-        if (k >= tau && id >= 0 && id < x.vocab) {
-          const int n = atomicAdd(&sh.count, 1);
-          if (n < kTopList) sh.list[n] = (uint64_t)k << 32 | (uint32_t)~id;
-        }
+        if (order_bits(f[e]) >= from && id >= 0 && id < x.vocab) hits |= 1u << e;
+      }
+      if (hits) {
+        int at = atomicAdd(&sh.n_list, __popc(hits));
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (hits >> e & 1) {
+            if (at < kTopList) sh.list[at] = (uint64_t)order_bits(f[e]) << 32 | (uint32_t)~(v * N - x.shift + e);
+            ++at;
+          }
       }
     }
   }
-  wave_sync();
-  const int count = sh.count;
-  auto put = [&](int i, uint64_t key) {
-    if (a.top_ids) a.top_ids[r * a.n_top + i] = (int)~(uint32_t)key;
-    if (a.top_logprobs) a.top_logprobs[r * a.n_top + i] = (from_order((uint32_t)(key >> 32)) - c) - log_s;
-  };
-  if (count <= kTopList) {
+  __syncthreads();
+  const int n_list = sh.n_list;
+  if (n_list <= kTopList) {
     // a candidate's place is the number of candidates before it
-    for (int i = lane; i < count; i += 64) {
-      const uint64_t mine = sh.list[i];
+    if (tid < n_list) {
+      const uint64_t mine = sh.list[tid];
       int before = 0;
-#pragma unroll 8
-      for (int j = 0; j < count; ++j) before += sh.list[j] > mine;
-      if (before < a.n_top) put(before, mine);
+#pragma unroll 4
+      for (int j = 0; j < n_list; ++j) before += sh.list[j] > mine;
+      if (before < n) put(before, (uint32_t)(mine >> 32), (int)~(uint32_t)mine);
     }
-  } else {
-    // runs of large or equal logits: n_top times the next in order, over all of them
+  } else if (w == 0) {
+    // runs of large logits: n times the next in order, over all of the groups
     uint64_t prev = ~0ull;
-    for (int i = 0; i < a.n_top; ++i) {
+    for (int i = 0; i < min(n_list, n); ++i) {
       uint64_t next = 0;
       for (int q = lane; q < n_ch * 16 * N; q += 64) {
-        const int id = sh.chosen[q / (16 * N)] * (16 * N) + q % (16 * N) - x.shift;
+        const int id = vector_of(q / (16 * N), q / N % 16) * N + q % N - x.shift;
         if (id < 0 || id >= x.vocab) continue;
-        const uint64_t k = (uint64_t)order_bits(Act<T>::load(x.row + id)) << 32 | (uint32_t)~id;
-        if (k < prev && k > next) next = k;
+        const uint32_t o = order_bits(Act<T>::load(x.row + id));
+        const uint64_t k = (uint64_t)o << 32 | (uint32_t)~id;
+        if (o >= from && k < prev && k > next) next = k;
       }
 #pragma unroll
       for (int d = 32; d >= 1; d >>= 1) {
@@ -287,88 +313,115 @@ __device__ __forceinline__ void top_of_row(const LogprobArgs& a, const RowView<T
         next = o > next ? o : next;
       }
       prev = next;
-      if (lane == 0) put(i, next);
+      if (lane == 0) put(i, (uint32_t)(next >> 32), (int)~(uint32_t)next);
     }
   }
-}
-
-// The outputs of a row from its sums (wave-uniform), by one wave.
-template <typename T>
-__device__ __forceinline__ void finish_row(const LogprobArgs& a, const RowView<T>& x, int64_t r, const Sums& q,
-                                           int count, uint32_t* group_keys, TopShared* sh) {
-  const float c = q.ref();
-  // without a finite largest logit the row has no distribution: S is 0 or NaN
-  const float log_s = q.s > 0.f ? logf(q.s) : NAN;
-  if ((threadIdx.x & 63) == 0) {
-    const int tok = a.tokens ? a.tokens[r] : -1;
-    const bool has = tok >= 0 && tok < x.vocab;
-    if (a.logprob) a.logprob[r] = has ? (Act<T>::load(x.row + tok) - c) - log_s : 0.f;
-    if (a.rank) a.rank[r] = has ? 1 + count : 0;
-    if (a.entropy) a.entropy[r] = log_s - q.t / q.s;
+  // ---- the first logits of the row that equal the bound, until there are n
+  if (all || w != 0) return;
+  int count = n_list;
+  for (int v0 = 0; count < n && v0 < x.n_vec; v0 += 64) {
+    const int v = v0 + lane;
+    float f[N];
+    Logit<T>::get(x.load(min(v, x.n_vec - 1)), f);
+    uint64_t b[N];
+    int at = count;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const int id = v * N - x.shift + e;
+      b[e] = __ballot(v < x.n_vec && id >= 0 && id < x.vocab && order_bits(f[e]) == bound);
+      at += __popcll(b[e] & lower);
+      count += __popcll(b[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (b[e] >> lane & 1) {
+        if (at < n) put(at, bound, v * N - x.shift + e);
+        ++at;
+      }
   }
-  if (sh) top_of_row<T>(a, x, r, group_keys, c, log_s, *sh);
 }
 
-// One workgroup per (row, run of groups).  FUSED: the run is the whole row, whose
-// outputs the workgroup's first wave then forms while the other workgroups of the CU
-// read on; otherwise the runs' sums go to the joining kernel.
-template <typename T, bool TOP, bool FUSED>
-__global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobArgs a, int groups) {
-  constexpr int N = Logit<T>::N, NW = kLpThreads / 64, U = 4;
+// Outputs of a row from its sums.
+struct RowResult {
+  float c, log_s, logprob, entropy;
+  int rank;
+  __device__ __forceinline__ RowResult(const LogprobArgs& a, int64_t r, Sums q, int count, bool has, float x_tok) {
+    c = q.ref();
+    // without a finite largest logit the row has no distribution: S is 0 or NaN
+    log_s = q.s > 0.f ? logf(q.s) : NAN;
+    logprob = has ? (x_tok - c) - log_s : 0.f;
+    entropy = log_s - q.t / q.s;
+    rank = has ? 1 + count : 0;
+  }
+  __device__ __forceinline__ void write(const LogprobArgs& a, int64_t r) const {
+    if (a.logprob) a.logprob[r] = logprob;
+    if (a.rank) a.rank[r] = rank;
+    if (a.entropy) a.entropy[r] = entropy;
+  }
+  __device__ __forceinline__ void put(const LogprobArgs& a, int64_t r, int i, uint32_t k, int id) const {
+    if (a.top_ids) a.top_ids[r * a.n_top + i] = id;
+    if (a.top_logprobs) a.top_logprobs[r * a.n_top + i] = (from_order(k) - c) - log_s;
+  }
+};
+
+template <typename T, int NT, bool TOP>
+__global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
+  constexpr int N = Logit<T>::N, NW = NT / 64, U = kPasses;
   __shared__ Sums sums[NW];
   __shared__ int counts[NW];
+  __shared__ std::conditional_t<TOP, TopShared<NT>, int> sh;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int64_t r = FUSED ? blockIdx.x : blockIdx.x / a.chunks;
-  const int chunk = FUSED ? 0 : (int)(blockIdx.x - r * a.chunks);
-  const RowView<T> x(a, r);
-  const int tok = a.tokens ? a.tokens[r] : -1;
-  const bool has = tok >= 0 && tok < x.vocab;
+  const int64_t r = blockIdx.x / a.parts;
+  const int part = (int)(blockIdx.x - r * a.parts), first = part * a.part_logits;
+  const T* row = (const T*)a.logits + r * a.row_stride;
+  const RowView<T> x(row + first, min(a.part_logits, a.vocab - first));
+  int tok = a.tokens ? a.tokens[r] : -1;
+  const bool has = tok >= 0 && tok < a.vocab;
   float xt = INFINITY;   // no token: nothing is counted
-  if (has) {
-    xt = Act<T>::load(x.row + tok);
-    if (xt != xt) xt = -INFINITY;
-  }
+  if (has) xt = Act<T>::load(row + tok);
+  const float x_tok = xt;
+  if (xt != xt) xt = -INFINITY;
+  tok -= first;          // of the part, maybe outside it
   // x >= xt is x > below, the next float down (xt = -inf is counted index by index)
   const int bits = __float_as_int(xt);
   const float below = xt == 0.f ? __int_as_float((int)0x80000001) : __int_as_float(bits < 0 ? bits + 1 : bits - 1);
   Sums q{-INFINITY, 0.f, 0.f};
-  float largest = -INFINITY;
-  int count = 0;   // wave-uniform
-  const int v0 = chunk * a.chunk_groups * 16, v1 = min(x.n_vec, v0 + a.chunk_groups * 16);
-  uint32_t* group_keys = a.group_keys + r * groups;
-  for (int b = v0 + w * 64; b < v1; b += kLpThreads * U) {   // the wave's first vector of U passes
-    float f[U][N];
-    if (b + (U - 1) * kLpThreads + 64 <= v1 && x.inside(b, (U - 1) * kLpThreads + 64)) {
-      v4u raw[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) raw[u] = x.base[b + u * kLpThreads + lane];
-#pragma unroll
-      for (int u = 0; u < U; ++u) Logit<T>::get(raw[u], f[u]);
-    } else {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int v = b + u * kLpThreads + lane;
-        if (v < v1) {
-          x.load(v, f[u]);
-        } else {
-#pragma unroll
-          for (int e = 0; e < N; ++e) f[u][e] = -INFINITY;
-        }
-      }
-    }
+  float largest = -INFINITY, c = 0.f;   // c: q.ref()
+  int count = 0;                        // wave-uniform
+  uint32_t best_key = 0;
+  const auto load = [&](v4u* raw, int b) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int vb = b + u * kLpThreads, v = vb + lane;
-      if (vb >= v1) break;
-      float vm = f[u][0];
+      const int vb = b + u * NT;
+      if (x.inside(vb, 64)) raw[u] = x.base[vb + lane];
+      else if (vb + lane < x.n_vec) raw[u] = x.load(vb + lane);
+      else raw[u] = Logit<T>::none();
+    }
+  };
+  // the next passes' loads are out while these are added up
+  v4u raw[U], next[U];
+  load(raw, w * 64);
+  for (int b0 = 0; b0 < x.n_vec; b0 += NT * U) {   // the first vector of U passes
+    const int b = b0 + w * 64;                     // .. of this wave's
+    if (b0 + NT * U < x.n_vec) load(next, b + NT * U);
+    float best = -INFINITY;
 #pragma unroll
-      for (int e = 1; e < N; ++e) vm = fmaxf(vm, f[u][e]);
-      largest = fmaxf(largest, vm);
-      if (vm > q.c + kLazy) q.raise(vm);
-      const float c = q.ref();
+    for (int u = 0; u < U; ++u) {
+      const int vb = b + u * NT;
+      if (vb >= x.n_vec) break;
+      float f[N];
+      Logit<T>::get(raw[u], f);
+      float vm = f[0];
+#pragma unroll
+      for (int e = 1; e < N; ++e) vm = fmaxf(vm, f[e]);
+      best = fmaxf(best, vm);
+      if (vm > q.c + kLazy) {
+        q.raise(vm);
+        c = q.ref();
+      }
 #pragma unroll
       for (int e = 0; e < N; ++e) {
-        const float d = f[u][e] - c, p = __builtin_amdgcn_exp2f(d * kLog2e);
+        const float d = f[e] - c, p = __builtin_amdgcn_exp2f(d * kLog2e);
         q.s += p;
         q.t = fmaf(p, fmaxf(d, -1.0e4f), q.t);
       }
@@ -377,97 +430,98 @@ __global__ __launch_bounds__(kLpThreads) void logprob_kernel(LogprobArgs a, int 
         if (xt != -INFINITY && (id0 > tok || id0 + 64 * N <= tok)) {
           const float thr = id0 > tok ? xt : below;
 #pragma unroll
-          for (int e = 0; e < N; ++e) count += __popcll(__ballot(f[u][e] > thr));
+          for (int e = 0; e < N; ++e) count += __popcll(__ballot(f[e] > thr));
         } else {
-          const int id = v * N - x.shift;
+          const int id = (vb + lane) * N - x.shift;
 #pragma unroll
           for (int e = 0; e < N; ++e)
-            count += __popcll(__ballot(id + e >= 0 && v < v1 &&
-                                       (f[u][e] > xt || (id + e < tok && (f[u][e] == xt || xt == -INFINITY)))));
+            count += __popcll(__ballot(id + e >= 0 && id + e < x.vocab &&
+                                       (f[e] > xt || (id + e < tok && (f[e] == xt || xt == -INFINITY)))));
         }
       }
-      if (TOP) {
-        const float g = row_max(fmaxf(vm, -INFINITY));
-        if ((lane & 15) == 0 && v < v1) group_keys[v / 16] = order_bits(g);
-      }
     }
+    largest = fmaxf(largest, best);
+    if constexpr (TOP) {
+      // a group holds logits if its first vector does
+      uint32_t key = quad_max(order_bits(best));
+      if ((b + lane) - lane % 4 >= x.n_vec) key = 0;
+      best_key = max(best_key, key);
+      if (lane % 4 == 0) reinterpret_cast<uint32_t*>(sh.keys)[b0 / 16 + w * 16 + lane / 4] = key;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) raw[u] = next[u];
   }
   if (largest > q.c) q.raise(largest);
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1)
-    q.join(Sums{__shfl_xor(q.c, d, 64), __shfl_xor(q.s, d, 64), __shfl_xor(q.t, d, 64)});
+  q = wave_sums(q);
   if (lane == 0) { sums[w] = q; counts[w] = count; }
-  __syncthreads();
-  if (w != 0) return;
-  q = sums[0];
-  count = counts[0];
-#pragma unroll
-  for (int i = 1; i < NW; ++i) { q.join(sums[i]); count += counts[i]; }
-  if constexpr (FUSED) {
-    if constexpr (TOP) {
-      __shared__ TopShared sh;
-      finish_row<T>(a, x, r, q, count, group_keys, &sh);
-    } else {
-      finish_row<T>(a, x, r, q, count, group_keys, nullptr);
-    }
-  } else if (lane == 0) {
-    a.part[r * a.chunks + chunk] = make_float4(q.c, q.s, q.t, __int_as_float(count));
-  }
-}
-
-// One wave per row: joins the sums of its runs and forms its outputs.
-template <typename T, bool TOP>
-__global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a, int groups) {
-  const int64_t r = blockIdx.x;
-  const int lane = threadIdx.x;
-  const RowView<T> x(a, r);
-  Sums q{-INFINITY, 0.f, 0.f};
-  int count = 0;
-  if (lane < a.chunks) {   // at most 64
-    const float4 p = a.part[r * a.chunks + lane];
-    q = Sums{p.x, p.y, p.z};
-    count = __float_as_int(p.w);
-  }
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) {
-    q.join(Sums{__shfl_xor(q.c, d, 64), __shfl_xor(q.s, d, 64), __shfl_xor(q.t, d, 64)});
-    count += __shfl_xor(count, d, 64);
-  }
   if constexpr (TOP) {
-    __shared__ TopShared sh;
-    finish_row<T>(a, x, r, q, count, a.group_keys + r * groups, &sh);
-  } else {
-    finish_row<T>(a, x, r, q, count, nullptr, nullptr);
+    if (lane % 4 == 0) sh.best[w * 16 + lane / 4] = best_key;
+    if (tid == 0) { sh.n_chosen = 0; sh.n_list = 0; }
+  }
+  __syncthreads();
+  q = wave_sums(lane < NW ? sums[lane] : Sums{-INFINITY, 0.f, 0.f});
+  count = wave_count(lane < NW ? counts[lane] : 0);
+  if (a.parts > 1) {
+    if (tid == 0) a.part[r * a.parts + part] = make_float4(q.c, q.s, q.t, __int_as_float(count));
+    if constexpr (TOP)
+      top_logits<T, NT>(x, a.n_top, (x.n_vec + NT * U - 1) / (NT * U) * (NT / 4), sh, [&](int i, uint32_t k, int id) {
+        a.part_top[(r * a.parts + part) * a.n_top + i] = (uint64_t)k << 32 | (uint32_t)~(id + first);
+      });
+    return;
+  }
+  const RowResult res(a, r, q, count, has, x_tok);
+  if (tid == 0) res.write(a, r);
+  if constexpr (TOP)
+    top_logits<T, NT>(x, a.n_top, (x.n_vec + NT * U - 1) / (NT * U) * (NT / 4), sh,
+                      [&](int i, uint32_t k, int id) { res.put(a, r, i, k, id); });
+}
+
+// Joins the parts of a row: their sums, and the first n_top of their n_top best logits each.
+template <typename T>
+__global__ __launch_bounds__(256) void logprob_join_kernel(LogprobArgs a) {
+  __shared__ uint64_t list[kMaxParts * RK_MAX_TOP];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int64_t r = blockIdx.x;
+  const int n = a.parts * a.n_top;
+  for (int i = tid; i < n; i += 256) list[i] = a.part_top[r * n + i];
+  const float4 p = lane < a.parts ? a.part[r * a.parts + lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+  const int tok = a.tokens ? a.tokens[r] : -1;
+  const bool has = tok >= 0 && tok < a.vocab;
+  const float x_tok = has ? Act<T>::load((const T*)a.logits + r * a.row_stride + tok) : 0.f;
+  const Sums q = wave_sums(Sums{p.x, p.y, p.z});
+  const RowResult res(a, r, q, wave_count(__float_as_int(p.w)), has, x_tok);
+  if (tid == 0) res.write(a, r);
+  __syncthreads();
+  for (int i = tid; i < n; i += 256) {
+    const uint64_t mine = list[i];
+    int before = 0;
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) before += list[j] > mine;
+    if (before < a.n_top) res.put(a, r, before, (uint32_t)(mine >> 32), (int)~(uint32_t)mine);
   }
 }
 
-// Groups of a row, wherever it starts, in whole vectors of keys.
-int logprob_groups(int vocab, bool bf16) {
+// Parts of a row of about 8 passes of a 1024-thread workgroup, while CUs are idle.
+void logprob_parts(int64_t n_rows, int vocab, bool bf16, int* parts, int* part_logits) {
   const int n = bf16 ? 8 : 4;
-  return (int)(((int64_t)vocab + n - 1 + 16 * n - 1) / (16 * n) + 3) / 4 * 4;
+  const int64_t vectors = ((int64_t)vocab + n - 1) / n;
+  const int64_t room = 256 / std::max<int64_t>(n_rows, 1), must = (vectors + kTopGroups * 16 - 2) / (kTopGroups * 16 - 1);
+  const int64_t want = std::max(must, std::min(room, vectors / (8 * 1024)));
+  *parts = (int)std::max<int64_t>(1, std::min<int64_t>(want, kMaxParts));
+  *part_logits = (int)((vectors + *parts - 1) / *parts * n);
 }
 
-// Workgroups per row: about 1024 in all, none with less than four loads per thread.
-void logprob_chunks(int64_t n_rows, int vocab, bool bf16, int* chunks, int* chunk_groups) {
-  const int groups = logprob_groups(vocab, bf16);
-  const int64_t want = std::max<int64_t>(1, 1024 / std::max<int64_t>(n_rows, 1));
-  const int64_t n = std::min<int64_t>(std::min<int64_t>(want, 64), (groups + 63) / 64);
-  *chunk_groups = (int)((groups + n - 1) / n);
-  *chunks = (groups + *chunk_groups - 1) / *chunk_groups;
-}
-
+// Threads per row: the widest workgroups for few rows, so that every CU of 256 has 16
+// waves with four loads each in flight.
 hipError_t launch_logprobs(const LogprobArgs& a, bool bf16, hipStream_t s) {
   if (a.n_rows <= 0) return hipSuccess;
-  const int groups = logprob_groups(a.vocab, bf16);
-  const uint32_t blocks = (uint32_t)(a.n_rows * a.chunks);
-#define RK_LOGPROBS(T, TOP)                                                                   \
-  do {                                                                                        \
-    if (a.chunks == 1) {                                                                      \
-      logprob_kernel<T, TOP, true><<<blocks, kLpThreads, 0, s>>>(a, groups);                  \
-    } else {                                                                                  \
-      logprob_kernel<T, TOP, false><<<blocks, kLpThreads, 0, s>>>(a, groups);                 \
-      logprob_join_kernel<T, TOP><<<(uint32_t)a.n_rows, 64, 0, s>>>(a, groups);               \
-    }                                                                                         \
+  const int64_t blocks = a.n_rows * a.parts;
+#define RK_LOGPROBS(T, TOP)                                                                     \
+  do {                                                                                          \
+    if (blocks <= 256) logprob_kernel<T, 1024, TOP><<<(uint32_t)blocks, 1024, 0, s>>>(a);       \
+    else if (blocks <= 512) logprob_kernel<T, 512, TOP><<<(uint32_t)blocks, 512, 0, s>>>(a);    \
+    else logprob_kernel<T, 256, TOP><<<(uint32_t)blocks, 256, 0, s>>>(a);                       \
+    if (a.parts > 1) logprob_join_kernel<T><<<(uint32_t)a.n_rows, 256, 0, s>>>(a);              \
   } while (0)
   if (bf16) { if (a.n_top) RK_LOGPROBS(bf16_t, true); else RK_LOGPROBS(bf16_t, false); }
   else { if (a.n_top) RK_LOGPROBS(float, true); else RK_LOGPROBS(float, false); }

@@ -276,15 +276,16 @@ struct LogprobArgs {
   const void* logits;
   int64_t row_stride;       // elements
   int64_t n_rows;
-  int vocab, n_top, chunks, chunk_groups;
+  int vocab, n_top;
+  int parts, part_logits;   // workgroups per row, logits of each
   const int32_t* tokens;
   float *logprob, *entropy, *top_logprobs;
   int32_t *rank, *top_ids;
-  float4* part;             // [n_rows, chunks]: reference, sum, weighted sum, count (bits)
-  uint32_t* group_keys;     // [n_rows, groups] order of the groups' largest logits
+  float4* part;             // parts > 1: [n_rows, parts] reference, sum, weighted sum, count (bits)
+  uint64_t* part_top;       // parts > 1: [n_rows, parts, n_top] order and complement of the index
 };
-int logprob_groups(int vocab, bool bf16);
-void logprob_chunks(int64_t n_rows, int vocab, bool bf16, int* chunks, int* chunk_groups);
+constexpr int kMaxVocab = 1 << 22;
+void logprob_parts(int64_t n_rows, int vocab, bool bf16, int* parts, int* part_logits);
 hipError_t launch_logprobs(const LogprobArgs& a, bool bf16, hipStream_t s);
 
 hipError_t launch_finalize(const double* s_acc, int n, double inv_n, float* s_out, hipStream_t s);

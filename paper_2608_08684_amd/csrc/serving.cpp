@@ -247,32 +247,35 @@ rk_status rk_paged_attention_selected(const rk_paged_cache* cache, const rk_page
                    ws_bytes, stream);
 }
 
-static bool logprob_plan(int64_t n_rows, int32_t vocab, rk_dtype dtype, int32_t n_top, LogprobArgs* a, size_t* gmax,
-                         size_t* total) {
-  if (n_rows < 0 || vocab < 1 || vocab > (1 << 30) || n_top < 0 || n_top > RK_MAX_TOP || n_top > vocab) return false;
-  if (dtype != RK_F32 && dtype != RK_BF16) return false;
-  const bool bf16 = dtype == RK_BF16;
-  if (n_rows > kMaxGrid / 64) return false;
-  logprob_chunks(n_rows, vocab, bf16, &a->chunks, &a->chunk_groups);
-  *gmax = align256((size_t)n_rows * a->chunks * 16);
-  *total = std::max<size_t>(256, *gmax + (n_top ? align256((size_t)n_rows * logprob_groups(vocab, bf16) * 4) : 0));
-  return true;
+// Workspace: the parts' sums and best logits, where rows are split; 0 for invalid sizes.
+struct LogprobPlan {
+  int parts, part_logits;
+  size_t top, total;
+};
+
+static LogprobPlan logprob_plan(int64_t n_rows, int32_t vocab, rk_dtype dtype, int32_t n_top) {
+  LogprobPlan p{};
+  if (n_rows < 0 || n_rows > kMaxGrid / 64 || vocab < 1 || vocab > kMaxVocab) return p;
+  if (n_top < 0 || n_top > RK_MAX_TOP || n_top > vocab || (dtype != RK_F32 && dtype != RK_BF16)) return p;
+  logprob_parts(n_rows, vocab, dtype == RK_BF16, &p.parts, &p.part_logits);
+  const size_t parts = p.parts > 1 ? (size_t)n_rows * p.parts : 0;
+  p.top = align256(parts * sizeof(float4));
+  p.total = std::max<size_t>(256, p.top + align256(parts * n_top * 8));
+  return p;
 }
 
 size_t rk_token_logprobs_workspace_size(int64_t n_rows, int32_t vocab, rk_dtype dtype, int32_t n_top) {
-  LogprobArgs a{};
-  size_t gmax, total;
-  return logprob_plan(n_rows, vocab, dtype, n_top, &a, &gmax, &total) ? total : 0;
+  return logprob_plan(n_rows, vocab, dtype, n_top).total;
 }
 
 rk_status rk_token_logprobs(const void *logits, rk_dtype dtype, int64_t n_rows, int32_t vocab, int64_t row_stride,
                             const int32_t* tokens, int32_t n_top, float* logprob, int32_t* rank, float* entropy,
                             int32_t* top_ids, float* top_logprobs, void* workspace, size_t ws_bytes, void* stream) {
   LogprobArgs a{};
-  size_t gmax, total;
   if (dtype != RK_F32 && dtype != RK_BF16) return bad(RK_ERR_ARG, "unknown dtype");
-  if (!logprob_plan(n_rows, vocab, dtype, n_top, &a, &gmax, &total)) {
-    set_error("n_rows must be in [0, 2^25), vocab in [1, 2^30], n_top in [0, min(vocab, %d)]", RK_MAX_TOP);
+  const LogprobPlan p = logprob_plan(n_rows, vocab, dtype, n_top);
+  if (p.total == 0) {
+    set_error("n_rows must be in [0, 2^25), vocab in [1, 2^22], n_top in [0, min(vocab, %d)]", RK_MAX_TOP);
     return RK_ERR_ARG;
   }
   if (row_stride < vocab) return bad(RK_ERR_ARG, "row_stride below vocab");
@@ -283,14 +286,15 @@ rk_status rk_token_logprobs(const void *logits, rk_dtype dtype, int64_t n_rows, 
   if (!logits || !workspace) return bad(RK_ERR_ARG, "null logits or workspace");
   if (((uintptr_t)logits & (dtype == RK_BF16 ? 1 : 3)) || misaligned(workspace))
     return bad(RK_ERR_ARG, "logits must be aligned to their type and the workspace to 16 bytes");
-  if (ws_bytes < total) { set_error("workspace too small (%zu < %zu)", ws_bytes, total); return RK_ERR_WORKSPACE; }
+  if (ws_bytes < p.total) { set_error("workspace too small (%zu < %zu)", ws_bytes, p.total); return RK_ERR_WORKSPACE; }
   hipStream_t s = (hipStream_t)stream;
   rk_status e;
   if ((e = check_stream(s)) != RK_OK) return e;
   a.logits = logits; a.row_stride = row_stride; a.n_rows = n_rows; a.vocab = vocab; a.n_top = n_top;
   a.tokens = tokens; a.logprob = logprob; a.rank = rank; a.entropy = entropy;
   a.top_ids = top_ids; a.top_logprobs = top_logprobs;
-  a.part = (float4*)workspace; a.group_keys = (uint32_t*)((char*)workspace + gmax);
+  a.parts = p.parts; a.part_logits = p.part_logits;
+  a.part = (float4*)workspace; a.part_top = (uint64_t*)((char*)workspace + p.top);
   Timed timed("token_logprobs", s);
   return hip_status("token log probabilities", launch_logprobs(a, dtype == RK_BF16, s));
 }

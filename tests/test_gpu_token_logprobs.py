@@ -41,7 +41,8 @@ def check(x, tokens, n_top, out):
         if "logprob" in out:
             assert near(float(out["logprob"][r]), lp, step(lp)), (r, float(out["logprob"][r]), lp)
         if "entropy" in out:    # log S - T / S; |T| / S <= the entropy plus log S <= 2 log n
-            assert near(float(out["entropy"][r]), h, 4 * rel * (1 + np.log(x.shape[1]))), (r, float(out["entropy"][r]), h)
+            got = float(out["entropy"][r])
+            assert near(got, h, 4 * rel * (1 + np.log(x.shape[1]))), (r, got, h)
         if "top_logprobs" in out:
             for a, b in zip(out["top_logprobs"][r].tolist(), top):
                 assert near(a, b, step(b)), (r, a, b)
@@ -63,6 +64,8 @@ def logits(rows, vocab, dtype, seed, pad=0, shift=0):
 @pytest.mark.parametrize("rows, vocab, n_top", [
     (1, 1, 1), (3, 2, 2), (2, 7, 0), (2, 33, 32), (5, 64, 5), (4, 65, 1), (3, 127, 20), (3, 1000, 32), (2, 4099, 7),
     (1, 32000, 5), (2, 50257, 20), (1, 128256, 32), (40, 777, 3),
+    (1, 262144, 5), (2, 262150, 32), (1, 600011, 20), (300, 2222, 4), (1, 1100003, 32), (20, 140003, 9),
+    (1, 1 << 22, 3),
 ])
 def test_sizes(dtype, rows, vocab, n_top):
     x, tok = logits(rows, vocab, dtype, vocab + n_top)
@@ -96,6 +99,10 @@ def test_ties(dtype, n_top):
     x[3] = torch.arange(2500) * -0.25
     x[4] = torch.arange(2500) * 0.25
     x[5, [0, 63, 64, 2499]] = 9.0
+    x[6, 700:1400] = 2.5 + torch.rand(700, generator=g)     # more large logits than a list holds
+    x[6, 1100] = 9.0
+    x[7] = -float("inf")                                    # fewer that count than are asked for
+    x[7, [64, 1999, 3]] = torch.tensor([1.0, 1.0, 0.5])
     x = x.to(torch_dtype(dtype)).cuda()
     tok = torch.tensor([0, 2499, 1, 17, 2499, 2499, 1200, 64], dtype=torch.int32).cuda()
     check(x, tok, n_top, run(x, tok, n_top))

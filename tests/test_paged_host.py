@@ -109,7 +109,7 @@ def test_workspace_sizes():
     for bad in (dict(n=0), dict(pages=0), dict(heads=3), dict(select=-1), dict(page_size=20), dict(pages=1 << 27)):
         assert size(**bad) == 0
     sz = rk.token_logprobs_workspace_size
-    assert sz(16, 32000, 5) > sz(16, 32000, 0) > 0
+    assert sz(16, 10 ** 6, 5) > sz(16, 10 ** 6, 0) > sz(16, 32000, 5) > 0 and sz(1, 1 << 22, 32) > 0
     assert sz(-1, 10, 0) == sz(1, 0, 0) == sz(1, 10, 11) == sz(1, 100, rk.RK_MAX_TOP + 1) == sz(1, 10, -1) == 0
 
 
@@ -121,6 +121,7 @@ def logprobs(logits=AT, dtype=rk.RK_F32, rows=2, vocab=100, stride=100, tokens=A
 
 @pytest.mark.parametrize("status, kw", [
     (A, dict(logits=None)), (A, dict(dtype=2)), (A, dict(rows=-1)), (A, dict(rows=1 << 25)), (A, dict(vocab=0)),
+    (A, dict(vocab=(1 << 22) + 1, stride=1 << 23)),
     (A, dict(stride=99)), (A, dict(tokens=None)), (A, dict(tokens=None, lp=None, rank=AT)), (A, dict(lp=None)),
     (A, dict(n_top=-1, ids=AT)), (A, dict(n_top=33, ids=AT)), (A, dict(n_top=5)), (A, dict(ids=AT)),
     (A, dict(n_top=5, vocab=4, ids=AT)), (A, dict(ws=None)), (A, dict(ws=AT + 4)), (A, dict(logits=AT + 2)),
