@@ -27,7 +27,9 @@ ARCH = "gfx950"
 # ordinary VGPRs: its softmax reads and rescales them every tile, and the AGPR
 # form would copy them across register files around every MFMA.  Its scores are
 # never NaN (masked keys are -inf), so max reductions need no NaN canonicalising.
-EXTRA = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"]}
+# The paged attention does the same with its own.
+EXTRA = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"],
+         "paged.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def hipcc() -> str:

@@ -311,19 +311,19 @@ template <int DH> struct DecodeTile<bf16_t, DH> {
       q[c] = __builtin_bit_cast(bf16x8_t, *(const v4u*)(qp + c * 32 + (lane >> 4) * 8));
   }
   // rows of the tile's two 16-entry halves
-  __device__ __forceinline__ void load(const bf16_t* k0, const bf16_t* k1, const bf16_t* v0, const bf16_t* v1,
-                                       int lane) {
-    const int at = (lane & 15) * DH + (lane >> 4) * 8;
+  __device__ __forceinline__ void load_k(const bf16_t* k0, const bf16_t* k1, int lane) {
+    const uint32_t at = (lane & 15) * DH + (lane >> 4) * 8;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       k[0][c] = *(const v4u*)(k0 + at + c * 32);
       k[1][c] = *(const v4u*)(k1 + at + c * 32);
     }
+  }
+  __device__ __forceinline__ void load_v(const bf16_t* v0, const bf16_t* v1, int lane) {
+    // a load covers 64 / CH rows, all of one half
+    const uint32_t at = lane * 8;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int slot = i * 64 + lane, row = slot / CH;
-      v[i] = *(const v4u*)((row < 16 ? v0 : v1) + (row & 15) * DH + (slot % CH) * 8);
-    }
+    for (int i = 0; i < NV; ++i) v[i] = *(const v4u*)((i < NV / 2 ? v0 : v1) + at + i % (NV / 2) * 512);
   }
   __device__ __forceinline__ void clear_values(uint32_t seen, int lane) {   // bit r: row r counts
 #pragma unroll
@@ -339,12 +339,17 @@ template <int DH> struct DecodeTile<bf16_t, DH> {
         s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k[t][c]), q[c], s[t], 0, 0, 0);
     }
   }
-  __device__ __forceinline__ void values(const f32x4_t p[2], f32x4_t* o, char* lds, int lane) const {
+  // the values' registers are free after stage_v
+  __device__ __forceinline__ void stage_v(char* lds, int lane) const {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int slot = i * 64 + lane, row = slot / CH, ch = slot % CH;
       *(v4u*)(lds + (row * CH + (ch ^ swz(row))) * 16) = v[i];
     }
+    wave_sync();
+  }
+  static constexpr bool kStaged = true;
+  __device__ __forceinline__ void values(const f32x4_t p[2], f32x4_t* o, char* lds, int lane) const {
     bf16x8_t hi, lo;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -352,7 +357,6 @@ template <int DH> struct DecodeTile<bf16_t, DH> {
       hi[e] = (__bf16)x;
       lo[e] = (__bf16)(x - (float)hi[e]);
     }
-    wave_sync();
     const int g = lane >> 4, jj = lane & 15, r = 4 * g + (jj >> 2);
 #pragma unroll
     for (int b = 0; b < ND; ++b) {
@@ -385,21 +389,26 @@ template <int DH> struct DecodeTile<float, DH> {
 #pragma unroll
     for (int c = 0; c < NC; ++c) q[c] = *(const f32x4_t*)(qp + c * 16 + (lane >> 4) * 4);
   }
-  __device__ __forceinline__ void load(const float* k0, const float* k1, const float* v0, const float* v1, int lane) {
-    const int l = lane & 15, g = lane >> 4;
+  __device__ __forceinline__ void load_k(const float* k0, const float* k1, int lane) {
+    const uint32_t at = (lane & 15) * DH + (lane >> 4) * 4;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-      k[0][c] = *(const f32x4_t*)(k0 + l * DH + c * 16 + g * 4);
-      k[1][c] = *(const f32x4_t*)(k1 + l * DH + c * 16 + g * 4);
+      k[0][c] = *(const f32x4_t*)(k0 + at + c * 16);
+      k[1][c] = *(const f32x4_t*)(k1 + at + c * 16);
     }
+  }
+  __device__ __forceinline__ void load_v(const float* v0, const float* v1, int lane) {
+    const uint32_t at = (lane >> 4) * 4 * DH + (lane & 15) * VEC;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int c = 0; c < NP; ++c) {
-        v[0][i][c] = *(const vecf*)(v0 + (4 * g + i) * DH + c * 16 * VEC + l * VEC);
-        v[1][i][c] = *(const vecf*)(v1 + (4 * g + i) * DH + c * 16 * VEC + l * VEC);
+        v[0][i][c] = *(const vecf*)(v0 + at + i * DH + c * 16 * VEC);
+        v[1][i][c] = *(const vecf*)(v1 + at + i * DH + c * 16 * VEC);
       }
   }
+  static constexpr bool kStaged = false;
+  __device__ __forceinline__ void stage_v(char*, int) const {}
   __device__ __forceinline__ void clear_values(uint32_t seen, int lane) {
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -479,19 +488,50 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cac
 #pragma unroll
   for (int i = 0; i < Tile::ND; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
-  for (int k0 = start + w * kTile; k0 < end; k0 += NW * kTile) {
-    const int k1 = k0 + 16;
-    const int p0 = pages[k0 >> shift], p1 = k1 < end ? pages[k1 >> shift] : -1;
+  // Pages of the tile at entry k0 (at the part's last tile where k0 lies past its end) and
+  // its rows.  A page that holds nothing is read as page 0 and not used.
+  struct Pages {
+    int k0, p0, p1;
+  };
+  struct Where {
+    int64_t at0, at1;   // element offsets of the two halves
+    uint32_t seen;      // entries that count
+  };
+  const int step = NW * kTile, first = start + w * kTile;
+  const int last = first + (max_i(end - 1 - first, 0) / step) * step;
+  const auto pages_of = [&](int k) {
+    const int k0 = min_i(k, last);
+    return Pages{k0, pages[k0 >> shift], pages[min_i(k0 + 16, end - 1) >> shift]};
+  };
+  const auto where = [&](Pages p) {
+    const int p0 = __builtin_amdgcn_readfirstlane(p.p0), p1 = __builtin_amdgcn_readfirstlane(p.p1);
     const bool ok0 = p0 >= 0 && p0 < cache.n_pages, ok1 = p1 >= 0 && p1 < cache.n_pages;
-    // rows of a page that holds nothing are read from page 0 and not used
-    const int64_t at0 = ((ok0 ? p0 : 0) * page_rows + head_at + (k0 & in_mask)) * DH;
-    const int64_t at1 = ((ok1 ? p1 : 0) * page_rows + head_at + (k1 & in_mask)) * DH;
-    tile.load((const T*)cache.k + at0, (const T*)cache.k + at1, (const T*)cache.v + at0, (const T*)cache.v + at1,
-              lane);
-    uint32_t seen = (ok0 ? 0xffffu : 0u) | (ok1 ? 0xffff0000u : 0u);
-    if (end - k0 < 32) seen &= (1u << (end - k0)) - 1u;
+    Where wh;
+    wh.at0 = ((ok0 ? p0 : 0) * page_rows + head_at + (p.k0 & in_mask)) * DH;
+    wh.at1 = ((ok1 ? p1 : 0) * page_rows + head_at + ((p.k0 + 16) & in_mask)) * DH;
+    wh.seen = (ok0 ? 0xffffu : 0u) | (ok1 ? 0xffff0000u : 0u);
+    if (end - p.k0 < 32) wh.seen &= (1u << (end - p.k0)) - 1u;
+    return wh;
+  };
+  const T* kc = (const T*)cache.k;
+  const T* vc = (const T*)cache.v;
+  // The next tile's rows are asked for as soon as this one's leave their registers: its
+  // keys after the scores, its values once they are in LDS; their pages a tile earlier.
+  // After the last tile these loads repeat it, so that no wait depends on a branch.
+  Where cur{}, nxt{};
+  Pages ahead{};
+  if (first < end) {
+    cur = where(pages_of(first));
+    tile.load_k(kc + cur.at0, kc + cur.at1, lane);
+    tile.load_v(vc + cur.at0, vc + cur.at1, lane);
+    nxt = where(pages_of(first + step));
+    ahead = pages_of(first + 2 * step);
+  }
+  for (int k0 = first; k0 < end; k0 += step) {
+    const uint32_t seen = cur.seen;
     f32x4_t s[2];
     tile.scores(s);
+    tile.load_k(kc + nxt.at0, kc + nxt.at1, lane);
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -504,6 +544,13 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cac
         for (int i = 0; i < 4; ++i)
           if (!(seen >> (t * 16 + 4 * g + i) & 1)) s[t][i] = -INFINITY;
     }
+    cur = nxt;
+    if constexpr (Tile::kStaged) {
+      tile.stage_v(area + w * Tile::LDS, lane);
+      tile.load_v(vc + cur.at0, vc + cur.at1, lane);
+    }
+    nxt = where(ahead);
+    ahead = pages_of(k0 + 3 * step);
     float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
                      fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
@@ -522,6 +569,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cac
         l += s[t][i];
       }
     tile.values(s, o, area + w * Tile::LDS, lane);
+    if constexpr (!Tile::kStaged) tile.load_v(vc + cur.at0, vc + cur.at1, lane);
   }
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
@@ -561,22 +609,50 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cac
 }
 
 // Joins the parts of one (sequence, query head): o = sum_s e^(lse_s - M) o_s / sum_s e^(lse_s - M).
+// A workgroup of 256 threads: every wave forms the weights (the same sums in the same
+// order), 256 / DH thread groups take the parts in turn, eight loads in flight each.
+// Bound: latency; 64 parts of 128 channels, 64 rows: 19.5 us with one group and a load
+// at a time.
+constexpr int kMaxDecodeParts = 256;
+
 template <typename T, int DH>
-__global__ __launch_bounds__(DH) void decode_join_kernel(PagedTable tab, DecodeArgs a, int n_kv, int page_shift) {
-  const int x = threadIdx.x, seq = blockIdx.x / a.n_heads, h = blockIdx.x % a.n_heads;
+__global__ __launch_bounds__(256) void decode_join_kernel(PagedTable tab, DecodeArgs a, int n_kv, int page_shift) {
+  constexpr int NG = 256 / DH;
+  __shared__ float wt[kMaxDecodeParts], red[NG][DH];
+  const int tid = threadIdx.x, lane = tid & 63, x = tid % DH, g = tid / DH;
+  const int seq = blockIdx.x / a.n_heads, h = blockIdx.x % a.n_heads;
   const int row = tab.per_head ? seq * n_kv + h / (a.n_heads / n_kv) : seq;
   const int len = table_length(tab, row, page_shift);
   const int per = part_entries(len, a.n_parts), n = max_i(1, (len + per - 1) / per);
   const int64_t at = (int64_t)blockIdx.x * a.n_parts;
-  float M = -INFINITY;
-  for (int p = 0; p < n; ++p) M = fmaxf(M, a.part_lse[at + p]);
-  const float ref = M == -INFINITY ? 0.f : M;
-  float L = 0.f, v = 0.f;
-  for (int p = 0; p < n; ++p) {
-    const float c = exp_diff(a.part_lse[at + p] - ref);
-    L += c;
-    v += c * a.part_o[(at + p) * DH + x];
+  float M = -INFINITY, lse[kMaxDecodeParts / 64];
+#pragma unroll
+  for (int i = 0; i < kMaxDecodeParts / 64; ++i) {
+    lse[i] = i * 64 + lane < n ? a.part_lse[at + i * 64 + lane] : -INFINITY;
+    M = fmaxf(M, lse[i]);
   }
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor(M, d, 64));
+  const float ref = M == -INFINITY ? 0.f : M;
+  float L = 0.f;
+#pragma unroll
+  for (int i = 0; i < kMaxDecodeParts / 64; ++i) {
+    lse[i] = exp_diff(lse[i] - ref);
+    L += lse[i];
+    if (tid < 64 && i * 64 < n) wt[i * 64 + lane] = lse[i];
+  }
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) L += __shfl_xor(L, d, 64);
+  __syncthreads();
+  const float* po = a.part_o + at * DH + x;
+  float v = 0.f;
+#pragma unroll 8
+  for (int p = g; p < n; p += NG) v = fmaf(wt[p], po[(int64_t)p * DH], v);
+  red[g][x] = v;
+  __syncthreads();
+  if (g != 0) return;
+#pragma unroll
+  for (int i = 1; i < NG; ++i) v += red[i][x];
   Act<T>::store((T*)a.out + (int64_t)seq * a.out_rs + (int64_t)h * DH + x, L == 0.f ? 0.f : v / L);
   if (a.lse && x == 0) a.lse[blockIdx.x] = L == 0.f ? -INFINITY : ref + logf(L);
 }
@@ -586,7 +662,7 @@ __global__ __launch_bounds__(DH) void decode_join_kernel(PagedTable tab, DecodeA
 int decode_parts(int n_seqs, int n_heads, int n_kv, int64_t max_entries) {
   const int64_t rows = (int64_t)n_seqs * n_kv * ((n_heads / n_kv + 15) / 16);
   const int64_t want = (1024 + rows - 1) / rows, most = std::max<int64_t>(1, max_entries / 256);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), 256));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), kMaxDecodeParts));
 }
 
 hipError_t launch_decode(const PagedView& cache, const PagedTable& tab, const DecodeArgs& a, hipStream_t s) {
@@ -596,7 +672,7 @@ hipError_t launch_decode(const PagedView& cache, const PagedTable& tab, const De
   do {                                                                                                          \
     decode_kernel<T, DH><<<(uint32_t)blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, a);                         \
     if (a.n_parts > 1)                                                                                          \
-      decode_join_kernel<T, DH><<<tab.n_seqs * a.n_heads, DH, 0, s>>>(tab, a, cache.n_kv, cache.page_shift);    \
+      decode_join_kernel<T, DH><<<tab.n_seqs * a.n_heads, 256, 0, s>>>(tab, a, cache.n_kv, cache.page_shift);    \
   } while (0)
   RK_PAGED_DISPATCH(cache.bf16, cache.head_dim, RK_DECODE);
 #undef RK_DECODE
