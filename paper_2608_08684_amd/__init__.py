@@ -397,55 +397,77 @@ class Model:
 
 
 # ----------------------------------------------------------------------------- paged cache, token log probabilities
+# A decode step makes several of these calls on a few microseconds of work each, so their checks are one
+# comparison chain per tensor and the message is put together only where one fails.
 def _dtype_id(t, what: str) -> int:
     import torch
-    if t.dtype == torch.bfloat16:
+    if t.dtype is torch.bfloat16:
         return RK_BF16
-    if t.dtype == torch.float32:
+    if t.dtype is torch.float32:
         return RK_F32
     raise ValueError(f"{what}: bfloat16 or float32, not {t.dtype}")
 
 
-def _need(t, what: str, like, dtype, shape=None, contiguous: bool = True):
-    """Checks a tensor of a call (``like``: a tensor that names the device): None passes through."""
-    if t is None:
-        return None
-    if t.device != like.device:
-        raise ValueError(f"{what}: on {t.device}, not on {like.device}")
+def _refuse(t, what: str, dev: int, dtype, shape, contiguous: bool):
+    if t.get_device() != dev:
+        raise ValueError(f"{what}: on {t.device}, not on cuda:{dev}")
     if t.dtype != dtype:
         raise ValueError(f"{what}: {t.dtype}, not {dtype}")
     if shape is not None and tuple(t.shape) != tuple(shape):
         raise ValueError(f"{what}: shape {tuple(t.shape)}, not {tuple(shape)}")
     if contiguous and not t.is_contiguous():
         raise ValueError(f"{what}: must be contiguous")
-    return t
 
 
-def _need_rows(t, what: str, like, n_rows: int, n_heads: int, head_dim: int):
-    """[n_rows, n_heads, head_dim] with heads one after the other in a row: its row stride."""
-    _need(t, what, like, like.dtype, (n_rows, n_heads, head_dim), contiguous=False)
-    _, sh, sd = t.stride()
-    if sd != 1 or (n_heads > 1 and sh != head_dim):
+def _need(t, what: str, dev: int, dtype, shape) -> Optional[int]:
+    """The address of a contiguous tensor of a call on device ``dev``; None stays None."""
+    if t is None:
+        return None
+    if t.get_device() != dev or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        _refuse(t, what, dev, dtype, shape, True)
+    return t.data_ptr()
+
+
+def _need_rows(t, what: str, dev: int, dtype, shape):
+    """(address, row stride) of [rows, heads, head_dim] with a row's heads one after the other."""
+    if t.get_device() != dev or t.dtype is not dtype or t.shape != shape:
+        _refuse(t, what, dev, dtype, shape, False)
+    n, heads, d = shape
+    row, head, one = t.stride()
+    if one != 1 or (head != d and heads > 1):
         raise ValueError(f"{what}: the heads of a row must be contiguous")
-    return t.stride(0) if n_rows > 1 else max(t.stride(0), n_heads * head_dim)
+    return t.data_ptr(), row if n > 1 else max(row, heads * d)
 
 
-def _on_device(tensor, stream, call):
-    """``call(stream)`` with the tensors' device current: on ``stream``, or on that device's current stream."""
-    import torch
-    if tensor.device.index == torch.cuda.current_device():
-        return _check(call(_stream(stream)))
-    with torch.cuda.device(tensor.device):
-        return _check(call(_stream(stream)))
+def _need_workspace(t, dev: int):
+    """(address, bytes) of a contiguous tensor of any type."""
+    if t.get_device() != dev or not t.is_contiguous():
+        _refuse(t, "workspace", dev, t.dtype, None, True)
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
-def _need_cuda(t, what: str):
-    if t.device.type != "cuda":
+def _need_cuda(t, what: str) -> int:
+    dev = t.get_device()
+    if dev < 0:
         raise ValueError(f"{what}: must be on the GPU")
+    return dev
 
 
-def _bytes(t) -> int:
-    return t.numel() * t.element_size()
+def _launch(dev: int, stream, fn, *args):
+    """``fn(*args, stream)`` with device ``dev`` current: on ``stream``, or on that device's current stream."""
+    import torch
+    if dev != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            return _launch(dev, stream, fn, *args)
+    if stream is None:
+        # torch.cuda.current_stream() builds a Stream object around this number: 2.7 us of a 10 us call
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        stream = raw(dev) if raw is not None else torch.cuda.current_stream(dev).cuda_stream
+    else:
+        stream = getattr(stream, "cuda_stream", stream)
+    status = fn(*args, stream)
+    if status != RK_OK:
+        _check(status)
 
 
 class PagedSeqs:
@@ -455,17 +477,19 @@ class PagedSeqs:
 
     def __init__(self, pages, lengths):
         import torch
-        _need_cuda(pages, "pages")
+        self.device = dev = _need_cuda(pages, "pages")
         if pages.dim() != 2 or pages.shape[0] < 1 or pages.shape[1] < 1:
             raise ValueError("pages: [n_seqs, max_pages], neither 0")
-        _need(pages, "pages", pages, torch.int32, contiguous=False)
+        if pages.dtype != torch.int32:
+            raise ValueError(f"pages: {pages.dtype}, not torch.int32")
         n, width = pages.shape
-        if (width > 1 and pages.stride(1) != 1) or pages.stride(0) < 0:
+        if width > 1 and pages.stride(1) != 1:
             raise ValueError("pages: a row must be contiguous")
-        _need(lengths, "lengths", pages, torch.int32, (n,))
+        _need(lengths, "lengths", dev, torch.int32, (n,))
         self.pages, self.lengths, self.n_seqs, self.max_pages = pages, lengths, n, width
         stride = pages.stride(0) if n > 1 else max(pages.stride(0), width)
         self._c = _PagedSeqs(pages.data_ptr(), lengths.data_ptr(), stride, n, width)
+        self._ref = ctypes.byref(self._c)
 
 
 class PagedCache:
@@ -473,30 +497,33 @@ class PagedCache:
     float32, ``key_bounds`` [n_pages, n_kv_heads, 2, head_dim] or None."""
 
     def __init__(self, k, v, key_bounds=None):
-        _need_cuda(k, "k")
+        self.device = dev = _need_cuda(k, "k")
         if k.dim() != 4:
             raise ValueError("k: [n_pages, n_kv_heads, page_size, head_dim]")
         dtype = _dtype_id(k, "k")
-        _need(k, "k", k, k.dtype)
-        _need(v, "v", k, k.dtype, k.shape)
         n_pages, n_kv, page, d = k.shape
-        _need(key_bounds, "key_bounds", k, k.dtype, (n_pages, n_kv, 2, d))
-        self.k, self.v, self.key_bounds = k, v, key_bounds
+        at = [_need(t, what, dev, k.dtype, shape) for t, what, shape in
+              ((k, "k", k.shape), (v, "v", k.shape), (key_bounds, "key_bounds", (n_pages, n_kv, 2, d)))]
+        self.k, self.v, self.key_bounds, self.dtype = k, v, key_bounds, k.dtype
         self.n_kv_heads, self.page_size, self.head_dim = n_kv, page, d
-        self._c = _PagedCache(k.data_ptr(), v.data_ptr(), _ptr(key_bounds), n_pages, page, n_kv, d, dtype)
+        self._c = _PagedCache(*at, n_pages, page, n_kv, d, dtype)
+        self._ref = ctypes.byref(self._c)
 
     def workspace_size(self, n_seqs: int, max_pages: int, n_heads: int, n_select: int = 0) -> int:
-        return int(load().rk_paged_workspace_size(ctypes.byref(self._c), int(n_seqs), int(max_pages), int(n_heads),
+        return int(load().rk_paged_workspace_size(self._ref, int(n_seqs), int(max_pages), int(n_heads),
                                                   int(n_select)))
+
+    def _own(self, seqs: PagedSeqs) -> int:
+        if seqs.device != self.device:
+            raise ValueError(f"seqs: on cuda:{seqs.device}, not on cuda:{self.device}")
+        return self.device
 
     def append(self, seqs: PagedSeqs, k, v, row_offsets: Optional[Sequence[int]] = None, q=None, q_out=None,
                positions=None, rope_theta: float = 0.0, stream=None):
         """rk_paged_append.  k, v: [rows, n_kv_heads, head_dim], any strides of whole 16-byte pieces; row_offsets:
         host offsets of the sequences' rows, or None for one row each; q, q_out: [rows, n_heads, head_dim]."""
         import torch
-        _need(seqs.pages, "seqs", self.k, torch.int32, contiguous=False)
-        offsets = None
-        n_rows = seqs.n_seqs
+        dev, dtype, n_rows, offsets = self._own(seqs), self.dtype, seqs.n_seqs, None
         if row_offsets is not None:
             offsets = np.ascontiguousarray(np.asarray(row_offsets, dtype=np.int64))
             if offsets.shape != (seqs.n_seqs + 1,):
@@ -504,54 +531,51 @@ class PagedCache:
             n_rows = int(offsets[-1])
         shape = (n_rows, self.n_kv_heads, self.head_dim)
         for t, what in ((k, "k"), (v, "v")):
-            _need(t, what, self.k, self.k.dtype, shape, contiguous=False)
-            if n_rows and t.stride(2) != 1:
-                raise ValueError(f"{what}: a head's values must be contiguous")
-        n_heads = q_stride = qo_stride = 0
+            if t.get_device() != dev or t.dtype is not dtype or t.shape != shape:
+                _refuse(t, what, dev, dtype, shape, False)
+        (k_row, k_head, k_one), (v_row, v_head, v_one) = k.stride(), v.stride()
+        if n_rows and (k_one != 1 or v_one != 1):
+            raise ValueError("k, v: a head's values must be contiguous")
+        n_heads = q_at = q_row = qo_at = qo_row = 0
         if (q is None) != (q_out is None):
             raise ValueError("q and q_out go together")
         if q is not None:
-            n_heads = q.shape[1]
-            q_stride = _need_rows(q, "q", self.k, n_rows, n_heads, self.head_dim)
-            qo_stride = _need_rows(q_out, "q_out", self.k, n_rows, n_heads, self.head_dim)
-        _need(positions, "positions", self.k, torch.int32, (n_rows,))
-        if n_rows == 0 and (offsets is None or not offsets.any()):
+            n_heads = q.shape[1] if q.dim() == 3 else 0
+            q_at, q_row = _need_rows(q, "q", dev, dtype, (n_rows, n_heads, self.head_dim))
+            qo_at, qo_row = _need_rows(q_out, "q_out", dev, dtype, (n_rows, n_heads, self.head_dim))
+        pos_at = _need(positions, "positions", dev, torch.int32, (n_rows,))
+        if n_rows == 0 and not offsets.any():
             return
-        rows = _PagedRows(None if offsets is None else offsets.ctypes.data, k.data_ptr(), v.data_ptr(), k.stride(0),
-                          k.stride(1), v.stride(0), v.stride(1), _ptr(q), _ptr(q_out), q_stride, qo_stride, n_heads,
-                          rope_theta, _ptr(positions))
-        _on_device(self.k, stream, lambda s: load().rk_paged_append(ctypes.byref(self._c), ctypes.byref(seqs._c),
-                                                                    ctypes.byref(rows), s))
+        rows = _PagedRows(None if offsets is None else offsets.ctypes.data, k.data_ptr(), v.data_ptr(), k_row, k_head,
+                          v_row, v_head, q_at, qo_at, q_row, qo_row, n_heads, rope_theta, pos_at)
+        _launch(dev, stream, load().rk_paged_append, self._ref, seqs._ref, ctypes.byref(rows))
 
-    def _attention_args(self, seqs, q, out, lse, workspace):
+    def _attend(self, fn, head, seqs, q, out, workspace, scale, lse, stream):
         import torch
-        _need(seqs.pages, "seqs", self.k, torch.int32, contiguous=False)
+        dev, dtype, n = self._own(seqs), self.dtype, seqs.n_seqs
         if q.dim() != 3:
             raise ValueError("q: [n_seqs, n_heads, head_dim]")
         n_heads = q.shape[1]
-        q_stride = _need_rows(q, "q", self.k, seqs.n_seqs, n_heads, self.head_dim)
-        out_stride = _need_rows(out, "out", self.k, seqs.n_seqs, n_heads, self.head_dim)
-        _need(lse, "lse", self.k, torch.float32, (seqs.n_seqs, n_heads))
-        _need(workspace, "workspace", self.k, workspace.dtype)
-        return n_heads, q_stride, out_stride
+        shape = (n, n_heads, self.head_dim)
+        q_at, q_row = _need_rows(q, "q", dev, dtype, shape)
+        out_at, out_row = _need_rows(out, "out", dev, dtype, shape)
+        lse_at = _need(lse, "lse", dev, torch.float32, (n, n_heads))
+        ws_at, ws_bytes = _need_workspace(workspace, dev)
+        _launch(dev, stream, fn, self._ref, seqs._ref, *head, q_at, q_row, n_heads, scale, out_at, out_row, lse_at,
+                ws_at, ws_bytes)
 
     def attention(self, seqs: PagedSeqs, q, out, workspace, scale: float = 0.0, lse=None, stream=None):
         """rk_paged_attention: q, out [n_seqs, n_heads, head_dim], lse float32 [n_seqs, n_heads]."""
-        n_heads, qs, os_ = self._attention_args(seqs, q, out, lse, workspace)
-        _on_device(self.k, stream, lambda s: load().rk_paged_attention(
-            ctypes.byref(self._c), ctypes.byref(seqs._c), q.data_ptr(), qs, n_heads, scale, out.data_ptr(), os_,
-            _ptr(lse), workspace.data_ptr(), _bytes(workspace), s))
+        self._attend(load().rk_paged_attention, (), seqs, q, out, workspace, scale, lse, stream)
 
     def attention_selected(self, seqs: PagedSeqs, q, out, workspace, n_select: int, keep_first: int = 1,
                            keep_last: int = 1, scale: float = 0.0, lse=None, selected=None, stream=None):
         """rk_paged_attention_selected: selected int32 [n_seqs, n_kv_heads, n_select] or None."""
         import torch
-        n_heads, qs, os_ = self._attention_args(seqs, q, out, lse, workspace)
-        _need(selected, "selected", self.k, torch.int32, (seqs.n_seqs, self.n_kv_heads, n_select))
-        sel = _PageSelection(n_select, keep_first, keep_last, _ptr(selected))
-        _on_device(self.k, stream, lambda s: load().rk_paged_attention_selected(
-            ctypes.byref(self._c), ctypes.byref(seqs._c), ctypes.byref(sel), q.data_ptr(), qs, n_heads, scale,
-            out.data_ptr(), os_, _ptr(lse), workspace.data_ptr(), _bytes(workspace), s))
+        sel = _PageSelection(n_select, keep_first, keep_last, _need(selected, "selected", self.device, torch.int32,
+                                                                    (seqs.n_seqs, self.n_kv_heads, n_select)))
+        self._attend(load().rk_paged_attention_selected, (ctypes.byref(sel),), seqs, q, out, workspace, scale, lse,
+                     stream)
 
 
 def token_logprobs_workspace_size(n_rows: int, vocab: int, n_top: int = 0, dtype: str = "f32") -> int:
@@ -565,25 +589,22 @@ def token_logprobs(logits, tokens, workspace, logprob=None, rank=None, entropy=N
     """rk_token_logprobs.  logits: [rows, vocab] float32 or bfloat16, rows may be strided; tokens: int32 [rows] or
     None; logprob, entropy: float32 [rows]; rank: int32 [rows]; top_ids int32 and top_logprobs float32 [rows, n_top]."""
     import torch
-    _need_cuda(logits, "logits")
+    dev = _need_cuda(logits, "logits")
     if logits.dim() != 2:
         raise ValueError("logits: [rows, vocab]")
     dtype = _dtype_id(logits, "logits")
     n, vocab = logits.shape
-    if n and vocab > 1 and logits.stride(1) != 1:
+    row, one = logits.stride()
+    if n and vocab > 1 and one != 1:
         raise ValueError("logits: a row must be contiguous")
-    top = next((t.shape[-1] for t in (top_ids, top_logprobs) if t is not None), 0)
-    _need(tokens, "tokens", logits, torch.int32, (n,))
-    _need(logprob, "logprob", logits, torch.float32, (n,))
-    _need(entropy, "entropy", logits, torch.float32, (n,))
-    _need(rank, "rank", logits, torch.int32, (n,))
-    _need(top_ids, "top_ids", logits, torch.int32, (n, top))
-    _need(top_logprobs, "top_logprobs", logits, torch.float32, (n, top))
-    _need(workspace, "workspace", logits, workspace.dtype)
-    stride = logits.stride(0) if n > 1 else max(logits.stride(0), vocab)
-    _on_device(logits, stream, lambda s: load().rk_token_logprobs(
-        logits.data_ptr(), dtype, n, vocab, stride, _ptr(tokens), top, _ptr(logprob), _ptr(rank), _ptr(entropy),
-        _ptr(top_ids), _ptr(top_logprobs), workspace.data_ptr(), _bytes(workspace), s))
+    top = top_ids.shape[-1] if top_ids is not None else top_logprobs.shape[-1] if top_logprobs is not None else 0
+    f32, i32 = torch.float32, torch.int32
+    at = (_need(tokens, "tokens", dev, i32, (n,)), top, _need(logprob, "logprob", dev, f32, (n,)),
+          _need(rank, "rank", dev, i32, (n,)), _need(entropy, "entropy", dev, f32, (n,)),
+          _need(top_ids, "top_ids", dev, i32, (n, top)), _need(top_logprobs, "top_logprobs", dev, f32, (n, top)))
+    ws_at, ws_bytes = _need_workspace(workspace, dev)
+    _launch(dev, stream, load().rk_token_logprobs, logits.data_ptr(), dtype, n, vocab,
+            row if n > 1 else max(row, vocab), *at, ws_at, ws_bytes)
 
 
 def spearman(x: Sequence[float], y: Sequence[float]) -> float:
