@@ -696,160 +696,354 @@ __device__ __forceinline__ uint64_t score_key(double x) {
   return u >> 63 ? ~u : u | 0x8000000000000000ull;
 }
 
+constexpr int kSelectThreads = 256;
+constexpr int kWavePages = 1024;    // pages whose keys one wave holds in registers
+
+// Q-, Q+ of a KV head, by the first DH threads
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void page_scores_kernel(PagedView cache, PagedTable tab, SelectArgs a, int chunks) {
-  constexpr int VE = Pack<T>::N, LPP = 2 * DH / VE;   // lanes per page: its lower bounds, then its upper
-  __shared__ double qs[2][DH];                        // Q-, Q+
-  const int G = cache.n_kv, grp = a.n_heads / G;
-  const int chunk = blockIdx.x % chunks, sh = blockIdx.x / chunks, seq = sh / G, hk = sh % G;
-  const int len = table_length(tab, seq, cache.page_shift);
-  const int count = (len + (1 << cache.page_shift) - 1) >> cache.page_shift;
-  const int per = (tab.max_pages + chunks - 1) / chunks, first = chunk * per, last = min_i(count, first + per);
-  if (first >= last) return;
-  for (int x = threadIdx.x; x < DH; x += 256) {
-    double lo = 0.0, hi = 0.0;
-    const T* qp = (const T*)a.q + (int64_t)seq * a.q_rs + (int64_t)hk * grp * DH + x;
-    for (int h = 0; h < grp; ++h) {
-      const double v = (double)Act<T>::load(qp + (int64_t)h * DH);
-      lo += v < 0.0 ? v : 0.0;
-      hi += v < 0.0 ? 0.0 : v;
-    }
-    qs[0][x] = lo;
-    qs[1][x] = hi;
+__device__ __forceinline__ void sum_queries(const SelectArgs& a, int seq, int hk, int grp, double (*qs)[DH]) {
+  const int x = threadIdx.x;
+  if (x >= DH) return;
+  double lo = 0.0, hi = 0.0;
+  const T* qp = (const T*)a.q + (int64_t)seq * a.q_rs + (int64_t)hk * grp * DH + x;
+  for (int h = 0; h < grp; ++h) {
+    const double v = (double)Act<T>::load(qp + (int64_t)h * DH);
+    lo += v < 0.0 ? v : 0.0;
+    hi += v < 0.0 ? 0.0 : v;
   }
-  __syncthreads();
+  qs[0][x] = lo;
+  qs[1][x] = hi;
+}
+
+// Keys of pages first .. last - 1 of a sequence: a group of LPP lanes per page (its lower
+// bounds, then its upper ones), four pages in flight.  put(p, key).
+template <typename T, int DH, int NT, typename Put>
+__device__ __forceinline__ void score_pages(const PagedView& cache, const PagedTable& tab, const SelectArgs& a, int seq,
+                                            int hk, int count, int first, int last, const double (*qs)[DH], Put put) {
+  constexpr int VE = Pack<T>::N, LPP = 2 * DH / VE, PER = NT / LPP, U = 4;
   const int sub = threadIdx.x % LPP, x0 = (sub * VE) % DH, side = sub * VE / DH;
   double q[VE];
 #pragma unroll
   for (int e = 0; e < VE; ++e) q[e] = qs[side][x0 + e];
-  for (int p = first + threadIdx.x / LPP; p < last; p += 256 / LPP) {
-    const int page = tab.pages[(int64_t)seq * tab.stride + p];
-    const bool ok = page >= 0 && page < cache.n_pages;
-    float f[VE];
-    Pack<T>::get(*(const v4u*)((const T*)cache.bounds + ((int64_t)(ok ? page : 0) * G + hk) * 2 * DH + sub * VE), f);
-    double s = 0.0;
+  const int32_t* pages = tab.pages + (int64_t)seq * tab.stride;
+  for (int p0 = first + threadIdx.x / LPP; p0 - (int)threadIdx.x / LPP < last; p0 += PER * U) {
+    v4u raw[U];
+    bool ok[U];
 #pragma unroll
-    for (int e = 0; e < VE; ++e) s += q[e] * (q[e] != 0.0 ? (double)f[e] : 0.0);   // an infinite bound of 0 counts 0
+    for (int u = 0; u < U; ++u) {
+      const int page = pages[min_i(p0 + u * PER, last - 1)];
+      ok[u] = page >= 0 && page < cache.n_pages;
+      raw[u] = *(const v4u*)((const T*)cache.bounds + ((int64_t)(ok[u] ? page : 0) * cache.n_kv + hk) * 2 * DH + sub * VE);
+    }
 #pragma unroll
-    for (int d = LPP / 2; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
-    if (sub == 0) {
-      uint64_t key = score_key(s);
-      if (p < a.keep_first || p >= count - a.keep_last) key = ~0ull;
-      a.keys[(int64_t)sh * tab.max_pages + p] = ok ? key : 0ull;
+    for (int u = 0; u < U; ++u) {
+      const int p = p0 + u * PER;
+      float f[VE];
+      Pack<T>::get(raw[u], f);
+      double s = 0.0;
+#pragma unroll
+      for (int e = 0; e < VE; ++e) s += q[e] * (q[e] != 0.0 ? (double)f[e] : 0.0);   // an infinite bound of 0 counts 0
+#pragma unroll
+      for (int d = LPP / 2; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
+      if (sub == 0 && p < last)
+        put(p, !ok[u] ? 0ull : p < a.keep_first || p >= count - a.keep_last ? ~0ull : score_key(s));
     }
   }
 }
 
-constexpr int kSelectThreads = 256;
+struct SelectShared {
+  uint64_t range[kSelectThreads / 64][2];
+  int hist[256], scan[kSelectThreads / 64], found[3], has_last;
+};
 
-// One workgroup per (sequence, KV head): the n_select largest keys, ties to the lower
-// page, by the digits of the key from the top, 8 bits a step; the search ends as soon
-// as the pages at or above the digits found are exactly those wanted.
-__global__ __launch_bounds__(kSelectThreads) void page_select_kernel(PagedView cache, PagedTable tab, SelectArgs a) {
-  constexpr int NT = kSelectThreads;
+// Where the chosen pages of a row go.
+struct Taken {
+  int32_t *list, *selected;
+  const int32_t* pages;
+  __device__ __forceinline__ Taken(const PagedTable& tab, const SelectArgs& a, int seq, int row) {
+    list = a.list + (int64_t)row * a.n_select;
+    selected = a.selected ? a.selected + (int64_t)row * a.n_select : nullptr;
+    pages = tab.pages + (int64_t)seq * tab.stride;
+  }
+  __device__ __forceinline__ void put(int i, int p, int page) const {   // page p of the sequence
+    list[i] = page;
+    if (selected) selected[i] = p;
+  }
+};
+
+// One wave: the n_select largest keys of `count` <= kWavePages pages, ties to the lower
+// page, by halving an interval of keys until exactly that many reach its lower end (a
+// dozen steps on scores that differ; 64 and a tie at most).  Every step is counting in
+// registers, no barrier: 512 pages, SELECT_WAVE us; by digits in a workgroup 5.8.
+// key(p): 0 for a page that holds nothing, never taken.
+template <typename Key>
+__device__ __forceinline__ void take_pages_wave(const PagedTable& tab, const SelectArgs& a, int seq, int row, int len,
+                                                int count, int page_shift, Key key) {
+  constexpr int HELD = kWavePages / 64;
+  const int lane = threadIdx.x & 63, n = a.n_select;
+  const uint64_t lower = (1ull << lane) - 1;
+  const Taken out(tab, a, seq, row);
+  uint64_t k[HELD];
+  int page[HELD];
+  int real = 0, forced = 0;
+  uint32_t top = 0, bottom = 0;   // of the upper halves of the keys in between: the largest, the complement of the least
+  // whole runs of loads, no branch between them
+#pragma unroll
+  for (int i0 = 0; i0 < HELD; i0 += 4) {
+    if (i0 * 64 < count) {
+#pragma unroll
+      for (int i = i0; i < i0 + 4; ++i) {
+        k[i] = key(min_i(i * 64 + lane, count - 1));
+        page[i] = out.pages[min_i(i * 64 + lane, count - 1)];
+      }
+#pragma unroll
+      for (int i = i0; i < i0 + 4; ++i) k[i] = i * 64 + lane < count ? k[i] : 0ull;
+    } else {
+#pragma unroll
+      for (int i = i0; i < i0 + 4; ++i) k[i] = 0;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) {
+    if (i * 64 >= count) break;
+    real += __popcll(__ballot(k[i] != 0));
+    forced += __popcll(__ballot(k[i] == ~0ull));
+    if (k[i] != 0 && k[i] != ~0ull) {
+      top = max(top, (uint32_t)(k[i] >> 32));
+      bottom = max(bottom, ~(uint32_t)(k[i] >> 32));
+    }
+  }
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) {
+    top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
+    bottom = max(bottom, (uint32_t)__shfl_xor((int)bottom, d, 64));
+  }
+  // first by the upper halves, in which scores that differ by a millionth differ
+  uint32_t lo32 = ~(uint32_t)__builtin_amdgcn_readfirstlane((int)bottom);
+  uint32_t hi32 = (uint32_t)__builtin_amdgcn_readfirstlane((int)top);
+  bool exact = real <= n || forced == n;
+  const bool given = exact;
+  while (!exact && lo32 < hi32) {
+    const uint32_t mid = lo32 + (hi32 - lo32) / 2 + 1;
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+      if (i * 64 < count) c += __popcll(__ballot((uint32_t)(k[i] >> 32) >= mid));
+    if (c >= n) lo32 = mid; else hi32 = mid - 1;
+    exact = c == n;
+  }
+  uint64_t lo = given ? (real <= n ? 1ull : ~0ull) : (uint64_t)lo32 << 32;
+  uint64_t hi = (uint64_t)lo32 << 32 | 0xffffffffu;
+  while (!exact && lo < hi) {
+    const uint64_t mid = lo + (hi - lo) / 2 + 1;
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+      if (i * 64 < count) c += __popcll(__ballot(k[i] >= mid));
+    if (c >= n) lo = mid; else hi = mid - 1;
+    exact = c == n;
+  }
+  int want = n;   // of the keys equal to lo
+  if (!exact) {
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+      if (i * 64 < count) want -= __popcll(__ballot(k[i] > lo));
+  }
+  int taken = 0;
+  bool last = false;
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) {
+    if (i * 64 >= count) break;
+    bool take = k[i] > lo || (exact && k[i] == lo);
+    if (!exact) {
+      const uint64_t e = __ballot(k[i] == lo);
+      if (k[i] == lo && __popcll(e & lower) < want) take = true;
+      want -= __popcll(e);
+    }
+    const uint64_t b = __ballot(take);
+    if (take) out.put(taken + __popcll(b & lower), i * 64 + lane, page[i]);
+    taken += __popcll(b);
+    if ((count - 1) / 64 == i) last = b >> ((count - 1) & 63) & 1;
+  }
+  for (int i = taken + lane; i < n; i += 64) out.put(i, -1, -1);
+  // entries of the chosen pages: whole pages, but for the sequence's last one, which comes last
+  if (lane == 0) a.list_len[row] = (taken << page_shift) - (last ? (count << page_shift) - len : 0);
+}
+
+// The workgroup: the same for any number of pages, by the digits of the key, 8 bits a step
+// from the highest bit in which any two differ; the search ends as soon as the pages at
+// or above the digits found are exactly those wanted.
+template <typename Key>
+__device__ __forceinline__ void take_pages(const PagedView& cache, const PagedTable& tab, const SelectArgs& a, int seq,
+                                           int sh_row, int len, int count, SelectShared& sh, Key key) {
+  constexpr int NT = kSelectThreads, NW = NT / 64;
   static_assert(NT == 256, "a thread per digit");
-  __shared__ int hist[256], scan[NT / 64], found[3], has_last;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, sh = blockIdx.x, seq = sh / cache.n_kv;
-  const int len = table_length(tab, seq, cache.page_shift), ps = 1 << cache.page_shift;
-  const int count = (len + ps - 1) >> cache.page_shift;
-  const uint64_t* keys = a.keys + (int64_t)sh * tab.max_pages;
-  const int32_t* pages = tab.pages + (int64_t)seq * tab.stride;
-  // keys with the digits of `prefix` above `shift` bits: want of them are still to be chosen
-  uint64_t prefix = 0;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, ps = 1 << cache.page_shift;
+  const Taken out(tab, a, seq, sh_row);
+  // keys that agree with prefix above `shift` bits: `want` of them are still to be chosen
+  uint64_t prefix = 1;
   int want = a.n_select, shift = 64;
-  bool exact = false;   // every key at or above prefix is taken
-  if (count <= a.n_select) {
-    prefix = 1;         // all pages that hold something
-    shift = 0;
-    exact = true;
+  bool exact = count <= a.n_select;   // every key from prefix up is taken
+  if (tid == 0) sh.has_last = 0;
+  if (!exact) {
+    uint64_t lo = ~0ull, hi = 0;
+    for (int p = tid; p < count; p += NT) {
+      const uint64_t k = key(p);
+      lo = k < lo ? k : lo;
+      hi = k > hi ? k : hi;
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) {
+      const uint64_t l = __shfl_xor((unsigned long long)lo, d, 64), h = __shfl_xor((unsigned long long)hi, d, 64);
+      lo = l < lo ? l : lo;
+      hi = h > hi ? h : hi;
+    }
+    if (lane == 0) { sh.range[w][0] = lo; sh.range[w][1] = hi; }
+    __syncthreads();
+    for (int i = 0; i < NW; ++i) {
+      lo = sh.range[i][0] < lo ? sh.range[i][0] : lo;
+      hi = sh.range[i][1] > hi ? sh.range[i][1] : hi;
+    }
+    shift = lo == hi ? 0 : 64 - __builtin_clzll(lo ^ hi);   // bits that are not the same in all keys
+    prefix = shift == 64 ? 0 : hi >> shift << shift;
   }
   while (!exact && shift > 0) {
-    shift -= 8;
-    for (int i = tid; i < 256; i += NT) hist[i] = 0;
+    const int width = min_i(shift, 8), above = shift;
+    shift -= width;
+    sh.hist[tid] = 0;
     __syncthreads();
     for (int p = tid; p < count; p += NT) {
-      const uint64_t k = keys[p];
-      if (shift == 56 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1);
+      const uint64_t k = key(p);
+      if (above == 64 || (k >> above) == (prefix >> above)) atomicAdd(&sh.hist[(k >> shift) & ((1 << width) - 1)], 1);
     }
     __syncthreads();
     // thread t holds digit 255 - t: the digit at which the counts from the top reach `want`
-    const int c = hist[255 - tid];
+    const int c = sh.hist[255 - tid];
     int sum = c;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
       const int o = __shfl_up(sum, d, 64);
       if (lane >= d) sum += o;
     }
-    if (lane == 63) scan[w] = sum;
+    if (lane == 63) sh.scan[w] = sum;
     __syncthreads();
-    for (int i = 0; i < w; ++i) sum += scan[i];
+    for (int i = 0; i < w; ++i) sum += sh.scan[i];
     if (sum >= want && sum - c < want) {
-      found[0] = 255 - tid;
-      found[1] = sum - c;
-      found[2] = c;
+      sh.found[0] = 255 - tid;
+      sh.found[1] = sum - c;
+      sh.found[2] = c;
     }
     __syncthreads();
-    prefix |= (uint64_t)found[0] << shift;
-    want -= found[1];
-    exact = found[2] == want;
-    __syncthreads();
+    prefix |= (uint64_t)sh.found[0] << shift;
+    want -= sh.found[1];
+    exact = sh.found[2] == want;
   }
-  // keys above the prefix, and of those equal to it (all digits used) the first `want`;
-  // keys of 0 hold nothing and are never taken
+  // keys above the prefix, and of those equal to it (all digits used) the first `want`
   int taken = 0, equal = 0;
-  if (tid == 0) has_last = 0;
   for (int p0 = 0; p0 < count; p0 += NT) {
     const int p = p0 + tid;
-    const uint64_t k = p < count ? (count <= a.n_select ? (uint64_t)(pages[p] >= 0 && pages[p] < cache.n_pages) : keys[p])
-                                 : 0ull;
-    bool eq = false, take = false;
-    if (k != 0) {
-      if (exact) take = k >= prefix;
-      else if (k > prefix) take = true;
-      else eq = k == prefix;
+    const uint64_t k = p < count ? key(p) : 0ull;
+    bool take = k != 0 && (exact ? k >= prefix : k > prefix);
+    const bool eq = !exact && k != 0 && k == prefix;
+    if (!exact) {   // rank among the equal keys, in page order
+      const uint64_t b = __ballot(eq);
+      __syncthreads();
+      if (lane == 0) sh.scan[w] = __popcll(b);
+      __syncthreads();
+      int before = equal;
+      for (int i = 0; i < NW; ++i) {
+        before += i < w ? sh.scan[i] : 0;
+        equal += sh.scan[i];
+      }
+      if (eq && before + __popcll(b & ((1ull << lane) - 1)) < want) take = true;
     }
-    // ranks among the equal keys, then among the taken ones, in page order
-    const uint64_t be = __ballot(eq);
-    if (lane == 0) scan[w] = __popcll(be);
+    const uint64_t b = __ballot(take);
     __syncthreads();
-    int before = equal, all = 0;
-    for (int i = 0; i < NT / 64; ++i) { before += i < w ? scan[i] : 0; all += scan[i]; }
+    if (lane == 0) sh.scan[w] = __popcll(b);
     __syncthreads();
-    if (eq && before + __popcll(be & ((1ull << lane) - 1)) < want) take = true;
-    equal += all;
-    const uint64_t bt = __ballot(take);
-    if (lane == 0) scan[w] = __popcll(bt);
-    __syncthreads();
-    before = taken;
-    all = 0;
-    for (int i = 0; i < NT / 64; ++i) { before += i < w ? scan[i] : 0; all += scan[i]; }
-    __syncthreads();
+    int at = taken + __popcll(b & ((1ull << lane) - 1));
+    for (int i = 0; i < NW; ++i) {
+      at += i < w ? sh.scan[i] : 0;
+      taken += sh.scan[i];
+    }
     if (take) {
-      const int at = before + __popcll(bt & ((1ull << lane) - 1));
-      a.list[(int64_t)sh * a.n_select + at] = pages[p];
-      if (a.selected) a.selected[(int64_t)sh * a.n_select + at] = p;
-      if (p == count - 1) has_last = 1;
+      out.put(at, p, out.pages[p]);
+      if (p == count - 1) sh.has_last = 1;
     }
-    taken += all;
   }
-  for (int i = taken + tid; i < a.n_select; i += NT) {
-    a.list[(int64_t)sh * a.n_select + i] = -1;
-    if (a.selected) a.selected[(int64_t)sh * a.n_select + i] = -1;
-  }
+  for (int i = taken + tid; i < a.n_select; i += NT) out.put(i, -1, -1);
   __syncthreads();
-  // entries of the chosen pages: whole pages, but for the sequence's last one, which comes last
-  if (tid == 0) a.list_len[sh] = taken * ps - (has_last ? count * ps - len : 0);
+  if (tid == 0) a.list_len[sh_row] = taken * ps - (sh.has_last ? count * ps - len : 0);
 }
 
+// One workgroup per (sequence, KV head): scores in LDS, then the choice.
+template <typename T, int DH>
+__global__ __launch_bounds__(kSelectThreads) void page_choose_kernel(PagedView cache, PagedTable tab, SelectArgs a) {
+  __shared__ double qs[2][DH];
+  __shared__ uint64_t keys[kWavePages];
+  const int G = cache.n_kv, seq = blockIdx.x / G, hk = blockIdx.x % G;
+  const int len = table_length(tab, seq, cache.page_shift);
+  const int count = (len + (1 << cache.page_shift) - 1) >> cache.page_shift;
+  sum_queries<T, DH>(a, seq, hk, a.n_heads / G, qs);
+  __syncthreads();
+  score_pages<T, DH, kSelectThreads>(cache, tab, a, seq, hk, count, 0, count, qs,
+                                     [&](int p, uint64_t k) { keys[p] = k; });
+  __syncthreads();
+  if (threadIdx.x < 64)
+    take_pages_wave(tab, a, seq, blockIdx.x, len, count, cache.page_shift, [&](int p) { return keys[p]; });
+}
+
+// The two halves for more pages: keys of a run of pages per workgroup, then the choice.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void page_scores_kernel(PagedView cache, PagedTable tab, SelectArgs a, int chunks) {
+  __shared__ double qs[2][DH];
+  const int G = cache.n_kv, chunk = blockIdx.x % chunks, row = blockIdx.x / chunks, seq = row / G, hk = row % G;
+  const int len = table_length(tab, seq, cache.page_shift);
+  const int count = (len + (1 << cache.page_shift) - 1) >> cache.page_shift;
+  const int per = (tab.max_pages + chunks - 1) / chunks, first = chunk * per, last = min_i(count, first + per);
+  if (first >= last) return;
+  sum_queries<T, DH>(a, seq, hk, a.n_heads / G, qs);
+  __syncthreads();
+  score_pages<T, DH, 256>(cache, tab, a, seq, hk, count, first, last, qs,
+                          [&](int p, uint64_t k) { a.keys[(int64_t)row * tab.max_pages + p] = k; });
+}
+
+// WAVE: at most kWavePages pages, one wave per row.
+template <bool WAVE>
+__global__ __launch_bounds__(WAVE ? 64 : kSelectThreads) void page_select_kernel(PagedView cache, PagedTable tab,
+                                                                                 SelectArgs a) {
+  const int row = blockIdx.x, seq = row / cache.n_kv;
+  const int len = table_length(tab, seq, cache.page_shift);
+  const int count = (len + (1 << cache.page_shift) - 1) >> cache.page_shift;
+  const uint64_t* keys = a.keys + (int64_t)row * tab.max_pages;
+  if constexpr (WAVE) {
+    take_pages_wave(tab, a, seq, row, len, count, cache.page_shift, [&](int p) { return keys[p]; });
+  } else {
+    __shared__ SelectShared sh;
+    take_pages(cache, tab, a, seq, row, len, count, sh, [&](int p) { return keys[p]; });
+  }
+}
+
+// One launch where one CU reads a row's bounds in less than the time of another, or where
+// the rows alone fill the card.
+constexpr int64_t kChooseBytes = 1 << 16;
+
 hipError_t launch_page_select(const PagedView& cache, const PagedTable& tab, const SelectArgs& a, hipStream_t s) {
-  const int rows = tab.n_seqs * cache.n_kv;
-  // a workgroup's fill of 256 threads four times over, split further while CUs are idle
-  const int per_pass = 256 * 16 / (2 * cache.head_dim * (cache.bf16 ? 2 : 4));
+  const int rows = tab.n_seqs * cache.n_kv, page_bytes = 2 * cache.head_dim * (cache.bf16 ? 2 : 4);
+  if (tab.max_pages <= kWavePages && ((int64_t)tab.max_pages * page_bytes <= kChooseBytes || rows >= 1024)) {
+#define RK_CHOOSE(T, DH) page_choose_kernel<T, DH><<<rows, kSelectThreads, 0, s>>>(cache, tab, a)
+    RK_PAGED_DISPATCH(cache.bf16, cache.head_dim, RK_CHOOSE);
+#undef RK_CHOOSE
+    return hipGetLastError();
+  }
+  // a workgroup's threads four times over, split further while CUs are idle
+  const int per_pass = 256 * 16 * 4 / page_bytes;
   const int chunks = std::max(1, std::min((tab.max_pages + per_pass - 1) / per_pass, std::max(1, 2048 / rows)));
 #define RK_SCORES(T, DH) page_scores_kernel<T, DH><<<(uint32_t)rows * chunks, 256, 0, s>>>(cache, tab, a, chunks)
   RK_PAGED_DISPATCH(cache.bf16, cache.head_dim, RK_SCORES);
 #undef RK_SCORES
-  page_select_kernel<<<rows, kSelectThreads, 0, s>>>(cache, tab, a);
+  if (tab.max_pages <= kWavePages) page_select_kernel<true><<<rows, 64, 0, s>>>(cache, tab, a);
+  else page_select_kernel<false><<<rows, kSelectThreads, 0, s>>>(cache, tab, a);
   return hipGetLastError();
 }
 
