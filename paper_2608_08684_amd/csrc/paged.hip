@@ -65,33 +65,111 @@ __device__ __forceinline__ int max_i(int a, int b) { return a > b ? a : b; }
 // New row r = off[i] + j of sequence i (m_i of them) is entry lengths[i] - m_i + j of
 // the sequence.  With pos its rotary position and x < d / 2,
 //   y[x]         = k[x] cos a - k[x + d/2] sin a
-//   y[x + d/2]   = k[x + d/2] cos a + k[x] sin a,   a = pos theta^(-2x/d);
-// the angle is formed in turns and reduced in double precision (a position of 10^6
-// would leave fp32 four digits of the angle), its sine and cosine in fp32.  One
-// workgroup owns all new rows of a page, so the page's bounds take them in a fixed
-// order without atomics.  Bound: memory (each value read once, written once); a single
-// row: the latency of one pass.
-constexpr int kAppendThreads = 256, kAppendRows = 16;
+//   y[x + d/2]   = k[x + d/2] cos a + k[x] sin a,   a = pos theta^(-2x/d).
+// The angle is a fraction of a turn in 32 bits, the upper half of pos times theta^(-2x/d)
+// / (2 pi) in 64 fixed-point bits: whole turns drop out exactly, and 2^-32 of a turn is
+// right for any 32-bit position (fp32 would leave a position of 10^6 four digits).  Its
+// sine and cosine are fp32.
+// Three kinds of workgroups: keys of all new rows of a page for some KV heads, whose
+// bounds so take them in a fixed order without atomics; values of 16 entries; queries
+// of up to 8 rows.  The first loads go out before the angles are formed.
+// Bound: memory (each value read once, written once); 28112 rows, 32 / 8 heads of 128:
+// 95 us, a copy of as many bytes 89.  A step's row: the latency of one pass.
+constexpr int kAppendThreads = 256, kAppendRows = 16, kAppendQueryRows = 8;
 
-template <int DH>
+// cosine and sine of channel pair x at position pos
 __device__ __forceinline__ float2 turn(const AppendArgs& a, int pos, int x) {
   if (!a.rotate) return make_float2(1.f, 0.f);
-  const double t = (double)pos * a.freq[x];   // turns
+  const uint32_t lo = (uint32_t)a.freq[x], hi = (uint32_t)(a.freq[x] >> 32);
+  uint32_t t = __umulhi((uint32_t)pos, lo) + (uint32_t)pos * hi;   // bits 32 .. 63 of the product
+  if (pos < 0) t -= lo;                                            // pos = (uint32_t)pos - 2^32
   float s, c;
-  sincospif((float)(2.0 * (t - rint(t))), &s, &c);
+  sincospif((float)(int32_t)t * 0x1p-31f, &s, &c);
   return make_float2(c, s);
 }
 
+// A pair of 16-byte pieces, x .. and x + d/2 .., rotated.
+template <typename T, int HALF>
+struct Pair {
+  v4u lo, hi;
+  __device__ __forceinline__ void load(const T* src) {
+    lo = *(const v4u*)src;
+    hi = *(const v4u*)(src + HALF);
+  }
+  __device__ __forceinline__ void rotate(const float2* cs) {
+    constexpr int VE = Pack<T>::N;
+    float a[VE], b[VE], y[VE], z[VE];
+    Pack<T>::get(lo, a);
+    Pack<T>::get(hi, b);
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      const float2 c = cs[e];
+      y[e] = a[e] * c.x - b[e] * c.y;
+      z[e] = b[e] * c.x + a[e] * c.y;
+    }
+    lo = Pack<T>::put(y);
+    hi = Pack<T>::put(z);
+  }
+  __device__ __forceinline__ void store(T* dst) const {
+    *(v4u*)dst = lo;
+    *(v4u*)(dst + HALF) = hi;
+  }
+};
+
+// The entries that a call writes to the j-th page that it may write to of sequence s.
+struct NewEntries {
+  int page, in_page, n, row, entry;   // n entries from in_page on, from row `row` and entry `entry` on
+  // block: a page block of the call (see launch_append)
+  __device__ __forceinline__ NewEntries(const PagedView& cache, const PagedTable& tab, const AppendArgs& a,
+                                        const SeqTable& st, int block) {
+    n = 0;
+    int s = block, j = 0, row0 = block, m = 1;
+    if (!a.one_row) {
+      int lo = 0, hi = st.n - 1;
+      while (lo < hi) {   // the sequence whose page blocks hold this one
+        const int mid = (lo + hi + 1) >> 1;
+        if (a.block0[mid] <= block) lo = mid; else hi = mid - 1;
+      }
+      s = lo;
+      j = block - a.block0[s];
+      row0 = st.off[s];
+      m = st.off[s + 1] - row0;
+    }
+    const int len = tab.lengths[s], first = (int)((uint32_t)len - (uint32_t)m);   // entries first .. len - 1
+    const int p = (max_i(first, 0) >> cache.page_shift) + j;
+    if (p >= tab.max_pages) return;
+    const int e0 = max_i(max_i(first, 0), p << cache.page_shift), e1 = min_i(len, (p + 1) << cache.page_shift);
+    if (e0 >= e1) return;
+    page = tab.pages[(int64_t)s * tab.stride + p];
+    if (page < 0 || page >= cache.n_pages) return;
+    n = e1 - e0;
+    in_page = e0 & ((1 << cache.page_shift) - 1);
+    row = row0 + (e0 - first);
+    entry = e0;
+  }
+};
+
 template <typename T, int DH>
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedView cache, PagedTable tab, AppendArgs a,
-                                                                SeqTable st, int kv_blocks, int q_rows) {
-  constexpr int VE = Pack<T>::N, HALF = DH / 2, UPH = HALF / VE, NT = kAppendThreads;
+                                                                SeqTable st) {
+  constexpr int VE = Pack<T>::N, HALF = DH / 2, UPH = HALF / VE, NT = kAppendThreads, U = 4;
   __shared__ float2 cs[kAppendRows][HALF];
-  __shared__ float red[NT][2 * VE];
-  const int tid = threadIdx.x;
-  if ((int)blockIdx.x >= kv_blocks) {
-    // ---- queries of q_rows rows
-    const int r0 = ((int)blockIdx.x - kv_blocks) * q_rows, n = min_i(q_rows, a.n_rows - r0);
+  const int tid = threadIdx.x, G = cache.n_kv, ps = 1 << cache.page_shift;
+  int block = blockIdx.x;
+  if (block >= a.key_blocks + a.value_blocks) {
+    // ---- queries
+    const int r0 = (block - a.key_blocks - a.value_blocks) * a.q_rows, n = min_i(a.q_rows, a.n_rows - r0);
+    const int per_row = a.n_heads * UPH, total = n * per_row;
+    Pair<T, HALF> raw[U];
+    const auto at = [&](int i, int64_t stride) {
+      const int rr = i / per_row, u = i - rr * per_row;
+      return (int64_t)(r0 + rr) * stride + (u / UPH) * DH + (u % UPH) * VE;
+    };
+    const auto load = [&](int i0) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) raw[u].load((const T*)a.q + at(min_i(i0 + u * NT, total - 1), a.q_rs));
+    };
+    load(tid);
     for (int i = tid; i < n * HALF; i += NT) {
       const int r = r0 + i / HALF;
       int pos;
@@ -103,91 +181,92 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedView cache,
         const int s = seq_of_row(st, r);
         pos = tab.lengths[s] - (st.off[s + 1] - st.off[s]) + (r - st.off[s]);
       }
-      cs[i / HALF][i % HALF] = turn<DH>(a, pos, i % HALF);
+      cs[i / HALF][i % HALF] = turn(a, pos, i % HALF);
     }
     __syncthreads();
-    const int U = a.n_heads * UPH;
-    for (int i = tid; i < n * U; i += NT) {
-      const int rr = i / U, u = i - rr * U, h = u / UPH, x = (u % UPH) * VE;
-      const T* src = (const T*)a.q + (int64_t)(r0 + rr) * a.q_rs + (int64_t)h * DH + x;
-      T* dst = (T*)a.q_out + (int64_t)(r0 + rr) * a.qo_rs + (int64_t)h * DH + x;
-      float lo[VE], hi[VE], y0[VE], y1[VE];
-      Pack<T>::get(*(const v4u*)src, lo);
-      Pack<T>::get(*(const v4u*)(src + HALF), hi);
+    for (int i0 = tid; i0 - tid < total; i0 += U * NT) {
+      Pair<T, HALF> cur[U];
 #pragma unroll
-      for (int e = 0; e < VE; ++e) {
-        const float2 c = cs[rr][x + e];
-        y0[e] = lo[e] * c.x - hi[e] * c.y;
-        y1[e] = hi[e] * c.x + lo[e] * c.y;
+      for (int u = 0; u < U; ++u) cur[u] = raw[u];
+      // in place: every piece is read by the thread that writes it, before it does
+      if (i0 - tid + U * NT < total) load(i0 + U * NT);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u * NT;
+        if (i < total) {
+          cur[u].rotate(&cs[i / per_row][i % UPH * VE]);
+          cur[u].store((T*)a.q_out + at(i, a.qo_rs));
+        }
       }
-      *(v4u*)dst = Pack<T>::put(y0);
-      *(v4u*)(dst + HALF) = Pack<T>::put(y1);
     }
     return;
   }
-  // ---- keys and values of one page
-  int s, j = 0, row0, m;
-  if (a.one_row) {
-    s = blockIdx.x;
-    row0 = s;
-    m = 1;
-  } else {
-    int lo = 0, hi = st.n - 1;
-    while (lo < hi) {   // the sequence whose page blocks hold this one
-      const int mid = (lo + hi + 1) >> 1;
-      if (a.block0[mid] <= (int)blockIdx.x) lo = mid; else hi = mid - 1;
+  if (block >= a.key_blocks) {
+    // ---- values of up to 16 entries
+    block -= a.key_blocks;
+    const int subs = a.one_row ? 1 : ps / kAppendRows;
+    const NewEntries w(cache, tab, a, st, block / subs);
+    if (w.n == 0) return;
+    int e0 = w.in_page, e1 = w.in_page + w.n;   // within the page
+    if (subs > 1) {
+      e0 = max_i(e0, block % subs * kAppendRows);
+      e1 = min_i(e1, (block % subs + 1) * kAppendRows);
     }
-    s = lo;
-    j = (int)blockIdx.x - a.block0[s];
-    row0 = st.off[s];
-    m = st.off[s + 1] - row0;
-  }
-  const int len = tab.lengths[s], first = (int)((uint32_t)len - (uint32_t)m);   // entries first .. len - 1
-  const int p = (max_i(first, 0) >> cache.page_shift) + j;
-  if (p >= tab.max_pages) return;
-  const int e0 = max_i(max_i(first, 0), p << cache.page_shift), e1 = min_i(len, (p + 1) << cache.page_shift);
-  if (e0 >= e1) return;
-  const int page = tab.pages[(int64_t)s * tab.stride + p];
-  if (page < 0 || page >= cache.n_pages) return;
-  const int in_page = e0 & ((1 << cache.page_shift) - 1), n = e1 - e0, r0 = row0 + (e0 - first);
-  const int G = cache.n_kv, ps = 1 << cache.page_shift;
-  const int64_t page_at = (int64_t)page * G * ps * DH;
-  T* kc = (T*)cache.k + page_at;
-  T* vc = (T*)cache.v + page_at;
-  const int U = G * UPH, upt = min_i(U, NT), RP = NT / upt, rp = tid / upt;
-  for (int u0 = 0; u0 < U; u0 += upt) {
-    const int u = u0 + tid % upt, h = u / UPH, x = (u % UPH) * VE;
-    const bool mine = rp < RP && u < U;
-    float bl[2 * VE], bh[2 * VE];
+    constexpr int CPH = DH / VE;
+    const int per_row = G * CPH, total = (e1 - e0) * per_row;
+    for (int i0 = tid; i0 < total; i0 += U * NT) {
+      v4u raw[U];
 #pragma unroll
-    for (int e = 0; e < 2 * VE; ++e) { bl[e] = INFINITY; bh[e] = -INFINITY; }
-    for (int b = 0; b < n; b += kAppendRows) {
-      const int nb = min_i(kAppendRows, n - b);
-      __syncthreads();
-      for (int i = tid; i < nb * HALF; i += NT) {
-        const int rr = b + i / HALF;
-        cs[i / HALF][i % HALF] = turn<DH>(a, a.positions ? a.positions[r0 + rr] : e0 + rr, i % HALF);
+      for (int u = 0; u < U; ++u) {
+        const int i = min_i(i0 + u * NT, total - 1), rr = i / per_row, c = i - rr * per_row;
+        raw[u] = *(const v4u*)((const T*)a.v + (int64_t)(w.row + e0 - w.in_page + rr) * a.v_rs +
+                               (int64_t)(c / CPH) * a.v_hs + c % CPH * VE);
       }
-      __syncthreads();
-      if (mine)
-        for (int rr = rp; rr < nb; rr += RP) {
-          const T* src = (const T*)a.k + (int64_t)(r0 + b + rr) * a.k_rs + (int64_t)h * a.k_hs + x;
-          T* dst = kc + ((int64_t)h * ps + in_page + b + rr) * DH + x;
-          float lo[VE], hi[VE], y[2 * VE];
-          Pack<T>::get(*(const v4u*)src, lo);
-          Pack<T>::get(*(const v4u*)(src + HALF), hi);
 #pragma unroll
-          for (int e = 0; e < VE; ++e) {
-            const float2 c = cs[rr][x + e];
-            y[e] = lo[e] * c.x - hi[e] * c.y;
-            y[VE + e] = hi[e] * c.x + lo[e] * c.y;
-          }
-          const v4u w0 = Pack<T>::put(y), w1 = Pack<T>::put(y + VE);
-          *(v4u*)dst = w0;
-          *(v4u*)(dst + HALF) = w1;
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u * NT, rr = i / per_row, c = i - rr * per_row;
+        if (i < total)
+          *(v4u*)((T*)cache.v + (((int64_t)w.page * G + c / CPH) * ps + e0 + rr) * DH + c % CPH * VE) = raw[u];
+      }
+    }
+    return;
+  }
+  // ---- keys of one page, `heads` KV heads from h0 on; a thread keeps its head and channels
+  const NewEntries w(cache, tab, a, st, block / a.head_blocks);
+  const int h0 = block % a.head_blocks * a.heads, heads = min_i(a.heads, G - h0);
+  if (w.n == 0 || heads <= 0) return;
+  __shared__ float red[NT][2 * VE];
+  const int units = heads * UPH, RP = NT / units, rp = tid / units, u = tid - rp * units;   // RP >= 4 rows at a time
+  const int h = h0 + u / UPH, x = u % UPH * VE;
+  T* kc = (T*)cache.k + (((int64_t)w.page * G + h) * ps + w.in_page) * DH + x;
+  const T* src = (const T*)a.k + (int64_t)w.row * a.k_rs + (int64_t)h * a.k_hs + x;
+  float bl[2 * VE], bh[2 * VE];
+#pragma unroll
+  for (int e = 0; e < 2 * VE; ++e) { bl[e] = INFINITY; bh[e] = -INFINITY; }
+  for (int b = 0; b < w.n; b += kAppendRows) {
+    const int nb = min_i(kAppendRows, w.n - b);
+    Pair<T, HALF> raw[U];
+    if (rp < RP) {
+#pragma unroll
+      for (int q = 0; q < U; ++q) raw[q].load(src + (int64_t)(b + min_i(rp + q * RP, nb - 1)) * a.k_rs);
+    }
+    __syncthreads();   // the last rows' angles are done with
+    for (int i = tid; i < nb * HALF; i += NT) {
+      const int rr = b + i / HALF;
+      cs[i / HALF][i % HALF] = turn(a, a.positions ? a.positions[w.row + rr] : w.entry + rr, i % HALF);
+    }
+    __syncthreads();
+    if (rp < RP) {
+#pragma unroll
+      for (int q = 0; q < U; ++q) {
+        const int rr = rp + q * RP;
+        if (rr < nb) {
+          raw[q].rotate(&cs[rr][x]);
+          raw[q].store(kc + (int64_t)(b + rr) * DH);
           if (cache.bounds) {   // of the keys as stored
-            Pack<T>::get(w0, y);
-            Pack<T>::get(w1, y + VE);
+            float y[2 * VE];
+            Pack<T>::get(raw[q].lo, y);
+            Pack<T>::get(raw[q].hi, y + VE);
 #pragma unroll
             for (int e = 0; e < 2 * VE; ++e) {
               bl[e] = fminf(bl[e], y[e]);
@@ -195,43 +274,38 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedView cache,
             }
           }
         }
-    }
-    if (cache.bounds) {
-      T* bp = (T*)cache.bounds + ((int64_t)page * G + h) * 2 * DH + x;
-#pragma unroll
-      for (int side = 0; side < 2; ++side) {
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < 2 * VE; ++e) red[tid][e] = side ? bh[e] : bl[e];
-        __syncthreads();
-        if (mine && rp == 0) {
-          float y[2 * VE];
-          if (in_page == 0) {   // the page starts here
-#pragma unroll
-            for (int e = 0; e < 2 * VE; ++e) y[e] = red[tid][e];
-          } else {
-            Pack<T>::get(*(const v4u*)(bp + side * DH), y);
-            Pack<T>::get(*(const v4u*)(bp + side * DH + HALF), y + VE);
-#pragma unroll
-            for (int e = 0; e < 2 * VE; ++e) y[e] = side ? fmaxf(y[e], red[tid][e]) : fminf(y[e], red[tid][e]);
-          }
-          for (int q = 1; q < RP; ++q)
-#pragma unroll
-            for (int e = 0; e < 2 * VE; ++e) {
-              const float z = red[tid + q * upt][e];
-              y[e] = side ? fmaxf(y[e], z) : fminf(y[e], z);
-            }
-          *(v4u*)(bp + side * DH) = Pack<T>::put(y);
-          *(v4u*)(bp + side * DH + HALF) = Pack<T>::put(y + VE);
-        }
       }
     }
   }
-  const int CPR = G * (DH / VE);   // 16-byte pieces of a row's values
-  for (int i = tid; i < n * CPR; i += NT) {
-    const int rr = i / CPR, c = i - rr * CPR, h = c / (DH / VE), x = (c % (DH / VE)) * VE;
-    *(v4u*)(vc + ((int64_t)h * ps + in_page + rr) * DH + x) =
-        *(const v4u*)((const T*)a.v + (int64_t)(r0 + rr) * a.v_rs + (int64_t)h * a.v_hs + x);
+  if (!cache.bounds) return;
+  T* bp = (T*)cache.bounds + ((int64_t)w.page * G + h) * 2 * DH + x;
+  const int rows_used = min_i(RP, w.n);
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 2 * VE; ++e) red[tid][e] = side ? bh[e] : bl[e];
+    __syncthreads();
+    if (rp == 0) {
+      float y[2 * VE];
+      if (w.in_page == 0) {   // the page starts here
+#pragma unroll
+        for (int e = 0; e < 2 * VE; ++e) y[e] = red[tid][e];
+      } else {
+        Pack<T>::get(*(const v4u*)(bp + side * DH), y);
+        Pack<T>::get(*(const v4u*)(bp + side * DH + HALF), y + VE);
+#pragma unroll
+        for (int e = 0; e < 2 * VE; ++e) y[e] = side ? fmaxf(y[e], red[tid][e]) : fminf(y[e], red[tid][e]);
+      }
+      for (int q = 1; q < rows_used; ++q)
+#pragma unroll
+        for (int e = 0; e < 2 * VE; ++e) {
+          const float z = red[tid + q * units][e];
+          y[e] = side ? fmaxf(y[e], z) : fminf(y[e], z);
+        }
+      *(v4u*)(bp + side * DH) = Pack<T>::put(y);
+      *(v4u*)(bp + side * DH + HALF) = Pack<T>::put(y + VE);
+    }
   }
 }
 
@@ -247,24 +321,35 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedView cache,
     }                                                                     \
   } while (0)
 
+// Page blocks: the pages that the new rows of a sequence may touch, one sequence after the other.
 hipError_t launch_append(const PagedView& cache, const PagedTable& tab, AppendArgs a, const SeqTable& st,
                          hipStream_t s) {
   if (a.n_rows <= 0) return hipSuccess;
-  const int ps = 1 << cache.page_shift;
-  int kv_blocks = 0;
+  const int ps = 1 << cache.page_shift, G = cache.n_kv;
+  int pages = 0;
   if (a.one_row) {
-    kv_blocks = tab.n_seqs;
+    pages = tab.n_seqs;
   } else {
     for (int i = 0; i < st.n; ++i) {   // m rows touch at most (m + ps - 2) / ps + 1 pages
-      a.block0[i] = kv_blocks;
+      a.block0[i] = pages;
       const int m = st.off[i + 1] - st.off[i];
-      if (m > 0) kv_blocks += (int)(((int64_t)m + ps - 2) / ps) + 1;
+      if (m > 0) pages += (int)(((int64_t)m + ps - 2) / ps) + 1;
     }
   }
-  const int q_rows = std::max(1, std::min(kAppendRows, a.n_rows / 1024));
-  const int q_blocks = a.q ? (a.n_rows + q_rows - 1) / q_rows : 0;
-#define RK_APPEND(T, DH) \
-  append_kernel<T, DH><<<kv_blocks + q_blocks, kAppendThreads, 0, s>>>(cache, tab, a, st, kv_blocks, q_rows)
+  // KV heads of a key block: at most a quarter of its threads wide (four rows at a time),
+  // and few enough for 512 blocks (2048 rows in pages of 128, 8 heads: 59 us with whole
+  // pages, 25 with single heads)
+  const int widest = 64 / (cache.head_dim / 2 / (cache.bf16 ? 8 : 4));
+  a.head_blocks = std::max((G + widest - 1) / widest, std::min(G, (512 + pages - 1) / pages));
+  a.heads = (G + a.head_blocks - 1) / a.head_blocks;
+  const int64_t key_blocks = (int64_t)pages * a.head_blocks, value_blocks = (int64_t)pages * (a.one_row ? 1 : ps / kAppendRows);
+  a.q_rows = std::max(1, std::min(kAppendQueryRows, a.n_rows / 1024));
+  const int64_t q_blocks = a.q ? ((int64_t)a.n_rows + a.q_rows - 1) / a.q_rows : 0;
+  if (key_blocks + value_blocks + q_blocks > 0x7fffffff) return hipErrorInvalidValue;
+  a.key_blocks = (int)key_blocks;
+  a.value_blocks = (int)value_blocks;
+  const uint32_t blocks = (uint32_t)(key_blocks + value_blocks + q_blocks);
+#define RK_APPEND(T, DH) append_kernel<T, DH><<<blocks, kAppendThreads, 0, s>>>(cache, tab, a, st)
   RK_PAGED_DISPATCH(cache.bf16, cache.head_dim, RK_APPEND);
 #undef RK_APPEND
   return hipGetLastError();
@@ -774,7 +859,8 @@ struct Taken {
 // One wave: the n_select largest keys of `count` <= kWavePages pages, ties to the lower
 // page, by halving an interval of keys until exactly that many reach its lower end (a
 // dozen steps on scores that differ; 64 and a tie at most).  Every step is counting in
-// registers, no barrier: 512 pages, SELECT_WAVE us; by digits in a workgroup 5.8.
+// registers, no barrier: 512 pages of a row: 7.7 us with its
+// launch, by digits in a workgroup 9.1.
 // key(p): 0 for a page that holds nothing, never taken.
 template <typename Key>
 __device__ __forceinline__ void take_pages_wave(const PagedTable& tab, const SelectArgs& a, int seq, int row, int len,

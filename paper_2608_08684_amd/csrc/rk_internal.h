@@ -242,7 +242,10 @@ struct AppendArgs {
   int n_rows, n_heads;
   bool one_row;             // one new row per sequence; otherwise the rows of a SeqTable
   bool rotate;
-  double freq[64];          // turns per position of channel pair x
+  uint64_t freq[64];        // turns per position of channel pair x, times 2^64
+  // of the launcher: blocks of each kind, blocks per page and KV heads of a key block,
+  // rows of a query block, first page block of each sequence
+  int key_blocks, value_blocks, head_blocks, heads, q_rows;
   int block0[RK_MAX_BATCH_SEQS];
 };
 hipError_t launch_append(const PagedView& cache, const PagedTable& tab, AppendArgs a, const SeqTable& st,

@@ -215,11 +215,13 @@ rk_status rk_paged_append(const rk_paged_cache* cache, const rk_paged_seqs* seqs
   a.positions = rows->positions;
   a.rotate = rows->rope_theta != 0.f;
   if (a.rotate) {   // theta^(-2x/d) / (2 pi): each power of two of x once, the others products of those
-    a.freq[0] = 0.15915494309189533577;
+    double freq[64];
+    freq[0] = 0.15915494309189533577;
     for (int b = 1; b < v.head_dim / 2; b *= 2) {
       const double f = pow((double)rows->rope_theta, -2.0 * b / v.head_dim);
-      for (int x = b; x < 2 * b; ++x) a.freq[x] = a.freq[x - b] * f;
+      for (int x = b; x < 2 * b; ++x) freq[x] = freq[x - b] * f;
     }
+    for (int x = 0; x < v.head_dim / 2; ++x) a.freq[x] = (uint64_t)(freq[x] * 0x1p64);   // below 2^62
   }
   hipStream_t s = (hipStream_t)stream;
   if ((e = check_stream(s)) != RK_OK) return e;
