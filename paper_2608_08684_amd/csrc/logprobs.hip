@@ -405,6 +405,9 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
     const int b = b0 + w * 64;                     // .. of this wave's
     if (b0 + NT * U < x.n_vec) load(next, b + NT * U);
     float best = -INFINITY;
+    // these passes' own sums: chains of 16 or 32 terms, then one of the passes (a chain of a
+    // thread's 500 terms left the entropy 2e-6 off)
+    float s = 0.f, t = 0.f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int vb = b + u * NT;
@@ -416,14 +419,17 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
       for (int e = 1; e < N; ++e) vm = fmaxf(vm, f[e]);
       best = fmaxf(best, vm);
       if (vm > q.c + kLazy) {
+        q.s += s;
+        q.t += t;
+        s = t = 0.f;
         q.raise(vm);
         c = q.ref();
       }
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         const float d = f[e] - c, p = __builtin_amdgcn_exp2f(d * kLog2e);
-        q.s += p;
-        q.t = fmaf(p, fmaxf(d, -1.0e4f), q.t);
+        s += p;
+        t = fmaf(p, fmaxf(d, -1.0e4f), t);
       }
       if (has) {
         const int id0 = vb * N - x.shift;   // of the wave: 64 N consecutive logits
@@ -440,6 +446,8 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
         }
       }
     }
+    q.s += s;
+    q.t += t;
     largest = fmaxf(largest, best);
     if constexpr (TOP) {
       // a group holds logits if its first vector does
