@@ -57,6 +57,13 @@ template <> struct Pack<float> {
 // log2(e): scaling the scores themselves would put that factor's rounding, times a
 // score of 50, into the weights.
 __device__ __forceinline__ float exp_diff(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+// The same with the product's rounding and log2(e)'s made good, for fp32 caches, whose
+// outputs show them: e^-10 is off by 5e-7 without.
+__device__ __forceinline__ float exp_diff_exact(float x) {
+  x = x < -200.f ? -200.f : x;   // 0 either way; a NaN stays
+  const float t = x * kLog2e, r = fmaf(x, kLog2e, -t) + x * 1.925963033500e-8f;
+  return __builtin_amdgcn_exp2f(t) * fmaf(r, 0.6931471806f, 1.0f);
+}
 
 __device__ __forceinline__ int min_i(int a, int b) { return a < b ? a : b; }
 __device__ __forceinline__ int max_i(int a, int b) { return a > b ? a : b; }
@@ -508,11 +515,15 @@ template <int DH> struct DecodeTile<float, DH> {
   __device__ __forceinline__ void scores(f32x4_t s[2]) const {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      // four sums over a quarter of the channels each: shorter chains, and none waits for another
+      f32x4_t a[4];
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
+      for (int e = 0; e < 4; ++e) {
+        a[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[t][c][e], q[c][e], s[t], 0, 0, 0);
+        for (int c = 0; c < NC; ++c) a[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[t][c][e], q[c][e], a[e], 0, 0, 0);
+      }
+      s[t] = (a[0] + a[1]) + (a[2] + a[3]);
     }
   }
   __device__ __forceinline__ void values(const f32x4_t p[2], f32x4_t* o, char*, int) const {
@@ -650,7 +661,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cac
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        s[t][i] = exp_diff(s[t][i] - ref);
+        s[t][i] = sizeof(T) == 4 ? exp_diff_exact(s[t][i] - ref) : exp_diff(s[t][i] - ref);
         l += s[t][i];
       }
     tile.values(s, o, area + w * Tile::LDS, lane);
