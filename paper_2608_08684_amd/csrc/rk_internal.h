@@ -256,13 +256,14 @@ struct DecodeArgs {
   float* lse;
   int64_t q_rs, out_rs;     // elements
   int n_heads, n_parts;
+  bool longest_first;       // of the launcher
   float scale;              // of the scores
   float* part_o;            // [n_seqs * n_heads, n_parts, head_dim], n_parts > 1 only
   float* part_lse;          // [n_seqs * n_heads, n_parts]
 };
 // Parts that the length is split into (the workspace is sized by it).
 int decode_parts(int n_seqs, int n_heads, int n_kv, int64_t max_entries);
-hipError_t launch_decode(const PagedView& cache, const PagedTable& tab, const DecodeArgs& a, hipStream_t s);
+hipError_t launch_decode(const PagedView& cache, const PagedTable& tab, DecodeArgs a, hipStream_t s);
 struct SelectArgs {
   const void* q;
   int64_t q_rs;
