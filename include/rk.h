@@ -553,8 +553,8 @@ typedef struct {
 /* Writes the new Keys, rotated (rotate-half, as the model's projections), and Values
  * to the entries lengths[i] - m_i .. lengths[i] - 1 of each sequence, m_i its number
  * of rows, and updates the bounds of their pages.  Rows whose entry is negative or
- * lies on no page are not written (their queries are still rotated).  No two
- * sequences of a call may write to the same page.                               */
+ * lies on no page are not written (their queries are still rotated).  A page that a
+ * call writes to must be named by one sequence, once.                           */
 rk_status rk_paged_append(const rk_paged_cache *cache, const rk_paged_seqs *seqs, const rk_paged_rows *rows,
                           void *stream);
 

@@ -186,7 +186,7 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedView cache,
         pos = (int)((uint32_t)tab.lengths[r] - 1u);
       } else {
         const int s = seq_of_row(st, r);
-        pos = tab.lengths[s] - (st.off[s + 1] - st.off[s]) + (r - st.off[s]);
+        pos = (int)((uint32_t)tab.lengths[s] - (uint32_t)(st.off[s + 1] - r));
       }
       cs[i / HALF][i % HALF] = turn(a, pos, i % HALF);
     }
