@@ -626,7 +626,7 @@ rk_status rk_token_logprobs(const void *logits, rk_dtype dtype, int64_t n_rows, 
  * (families: "rmsnorm", "gemm_qkv", "noise", "attention", "gemm_o",
  * "gemm_gate_up", "gemm_down", "lm_lse", "lm_kl", "kl_logits", "lm_logits",
  * "local", "snap_scores", "snap_select", "paged_append", "paged_attention",
- * "page_select", "token_logprobs").
+ * "token_logprobs").
  * rk_timing_end waits for the recorded events, returns the number of launches
  * and their summed duration in milliseconds, and stops recording.  Host-side
  * state is process-wide; not for concurrent use from several threads.          */

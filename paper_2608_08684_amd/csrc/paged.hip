@@ -362,6 +362,326 @@ hipError_t launch_append(const PagedView& cache, const PagedTable& tab, AppendAr
   return hipGetLastError();
 }
 
+// --------------------------------------------------------------------------- page selection
+// Score of a page for one KV head: sum over the query heads h that share it of
+// sum_x max(q_hx lo_x, q_hx hi_x), an upper bound of the summed products with any key
+// of the page.  The heads can be summed first: sum_x hi_x Q+_x + lo_x Q-_x with
+// Q+ = sum_h max(q_h, 0), Q- = sum_h min(q_h, 0).  In double precision throughout, so
+// the choice does not hang on the order of a sum.  Bound: memory, the bounds of every
+// page read once.
+//
+// A score becomes a whole number that orders the same way: larger for a larger score;
+// the largest of all for pages that are always kept, 0 for pages that hold nothing (a
+// NaN score counts as -inf).
+__device__ __forceinline__ uint64_t score_key(double x) {
+  if (x != x) x = -INFINITY;
+  const uint64_t u = (uint64_t)__double_as_longlong(x + 0.0);   // -0 and 0 are one score
+  return u >> 63 ? ~u : u | 0x8000000000000000ull;
+}
+
+__device__ __forceinline__ int table_length(const PagedTable& tab, int row, int page_shift) {
+  return max_i(0, (int)min((int64_t)tab.lengths[row], (int64_t)tab.max_pages << page_shift));
+}
+
+constexpr int kSelectThreads = 256;
+constexpr int kWavePages = 1024;    // pages whose keys one wave holds in registers
+
+// Q-, Q+ of a KV head, by the first DH threads
+template <typename T, int DH>
+__device__ __forceinline__ void sum_queries(const SelectArgs& a, int seq, int hk, int grp, double (*qs)[DH]) {
+  const int x = threadIdx.x;
+  if (x >= DH) return;
+  double lo = 0.0, hi = 0.0;
+  const T* qp = (const T*)a.q + (int64_t)seq * a.q_rs + (int64_t)hk * grp * DH + x;
+  for (int h = 0; h < grp; ++h) {
+    const double v = (double)Act<T>::load(qp + (int64_t)h * DH);
+    lo += v < 0.0 ? v : 0.0;
+    hi += v < 0.0 ? 0.0 : v;
+  }
+  qs[0][x] = lo;
+  qs[1][x] = hi;
+}
+
+// The workgroup: keys of pages first .. last - 1 of a sequence's `count`.  A group of LPP
+// lanes takes a page (its lower bounds, then its upper ones), four pages in flight, the
+// first of them before the queries are summed.  put(p, key).
+template <typename T, int DH, typename Put>
+__device__ __forceinline__ void score_pages(const PagedView& cache, const PagedTable& tab, const SelectArgs& a, int seq,
+                                            int hk, int count, int first, int last, double (*qs)[DH], Put put) {
+  constexpr int VE = Pack<T>::N, LPP = 2 * DH / VE, PER = kSelectThreads / LPP, U = 4;
+  const int group = threadIdx.x / LPP, sub = threadIdx.x % LPP, x0 = (sub * VE) % DH, side = sub * VE / DH;
+  const int32_t* pages = tab.pages + (int64_t)seq * tab.stride;
+  v4u raw[U];
+  bool ok[U];
+  const auto load = [&](int p0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int page = pages[min_i(p0 + group + u * PER, last - 1)];
+      ok[u] = page >= 0 && page < cache.n_pages;
+      raw[u] = *(const v4u*)((const T*)cache.bounds + ((int64_t)(ok[u] ? page : 0) * cache.n_kv + hk) * 2 * DH + sub * VE);
+    }
+  };
+  if (first < last) load(first);
+  sum_queries<T, DH>(a, seq, hk, a.n_heads / cache.n_kv, qs);
+  __syncthreads();
+  double q[VE];
+#pragma unroll
+  for (int e = 0; e < VE; ++e) q[e] = qs[side][x0 + e];
+  for (int p0 = first; p0 < last; p0 += PER * U) {
+    if (p0 > first) load(p0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int p = p0 + group + u * PER;
+      float f[VE];
+      Pack<T>::get(raw[u], f);
+      double s = 0.0;
+#pragma unroll
+      for (int e = 0; e < VE; ++e) s += q[e] * (q[e] != 0.0 ? (double)f[e] : 0.0);   // an infinite bound of 0 counts 0
+#pragma unroll
+      for (int d = LPP / 2; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
+      if (sub == 0 && p < last)
+        put(p, !ok[u] ? 0ull : p < a.keep_first || p >= count - a.keep_last ? ~0ull : score_key(s));
+    }
+  }
+}
+
+struct SelectShared {
+  uint64_t range[kSelectThreads / 64][2];
+  int hist[256], scan[kSelectThreads / 64], found[3], has_last;
+};
+
+// One wave: the n_select largest keys of `count` <= kWavePages pages, ties to the lower
+// page, by halving an interval of keys until exactly that many reach its lower end (a
+// dozen steps on scores that differ; 64 and a tie at most).  Every step is counting in
+// registers, no barrier.  key(p): 0 for a page that holds nothing, never taken.
+// put(i, p, page): the i-th is page p of the sequence.  Returns the entries of the chosen
+// pages: whole pages, but for the sequence's last one, which comes last.
+template <typename Key, typename Put>
+__device__ __forceinline__ int take_pages_wave(const int32_t* pages, int n, int len, int count, int page_shift, Key key,
+                                               Put put) {
+  constexpr int HELD = kWavePages / 64;
+  const int lane = threadIdx.x & 63;
+  const uint64_t lower = (1ull << lane) - 1;
+  uint64_t k[HELD];
+  int page[HELD];
+  int real = 0, forced = 0;
+  uint32_t top = 0, bottom = 0;   // of the upper halves of the keys in between: the largest, the complement of the least
+  // whole runs of loads, no branch between them
+#pragma unroll
+  for (int i0 = 0; i0 < HELD; i0 += 4) {
+    if (i0 * 64 < count) {
+#pragma unroll
+      for (int i = i0; i < i0 + 4; ++i) {
+        k[i] = key(min_i(i * 64 + lane, count - 1));
+        page[i] = pages[min_i(i * 64 + lane, count - 1)];
+      }
+#pragma unroll
+      for (int i = i0; i < i0 + 4; ++i) k[i] = i * 64 + lane < count ? k[i] : 0ull;
+    } else {
+#pragma unroll
+      for (int i = i0; i < i0 + 4; ++i) k[i] = 0;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) {
+    if (i * 64 >= count) break;
+    real += __popcll(__ballot(k[i] != 0));
+    forced += __popcll(__ballot(k[i] == ~0ull));
+    if (k[i] != 0 && k[i] != ~0ull) {
+      top = max(top, (uint32_t)(k[i] >> 32));
+      bottom = max(bottom, ~(uint32_t)(k[i] >> 32));
+    }
+  }
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) {
+    top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
+    bottom = max(bottom, (uint32_t)__shfl_xor((int)bottom, d, 64));
+  }
+  // first by the upper halves, in which scores that differ by a millionth differ
+  uint32_t lo32 = ~(uint32_t)__builtin_amdgcn_readfirstlane((int)bottom);
+  uint32_t hi32 = (uint32_t)__builtin_amdgcn_readfirstlane((int)top);
+  bool exact = real <= n || forced == n;
+  const bool given = exact;
+  while (!exact && lo32 < hi32) {
+    const uint32_t mid = lo32 + (hi32 - lo32) / 2 + 1;
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+      if (i * 64 < count) c += __popcll(__ballot((uint32_t)(k[i] >> 32) >= mid));
+    if (c >= n) lo32 = mid; else hi32 = mid - 1;
+    exact = c == n;
+  }
+  uint64_t lo = given ? (real <= n ? 1ull : ~0ull) : (uint64_t)lo32 << 32;
+  uint64_t hi = (uint64_t)lo32 << 32 | 0xffffffffu;
+  while (!exact && lo < hi) {
+    const uint64_t mid = lo + (hi - lo) / 2 + 1;
+    int c = 0;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+      if (i * 64 < count) c += __popcll(__ballot(k[i] >= mid));
+    if (c >= n) lo = mid; else hi = mid - 1;
+    exact = c == n;
+  }
+  int want = n;   // of the keys equal to lo
+  if (!exact) {
+#pragma unroll
+    for (int i = 0; i < HELD; ++i)
+      if (i * 64 < count) want -= __popcll(__ballot(k[i] > lo));
+  }
+  int taken = 0;
+  bool last = false;
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) {
+    if (i * 64 >= count) break;
+    bool take = k[i] > lo || (exact && k[i] == lo);
+    if (!exact) {
+      const uint64_t e = __ballot(k[i] == lo);
+      if (k[i] == lo && __popcll(e & lower) < want) take = true;
+      want -= __popcll(e);
+    }
+    const uint64_t b = __ballot(take);
+    if (take) put(taken + __popcll(b & lower), i * 64 + lane, page[i]);
+    taken += __popcll(b);
+    if ((count - 1) / 64 == i) last = b >> ((count - 1) & 63) & 1;
+  }
+  for (int i = taken + lane; i < n; i += 64) put(i, -1, -1);
+  return (taken << page_shift) - (last ? (count << page_shift) - len : 0);
+}
+
+// The workgroup: the same for any number of pages, by the digits of the key, 8 bits a step
+// from the highest bit in which any two differ; the search ends as soon as the pages at
+// or above the digits found are exactly those wanted.  The list goes to the workspace.
+template <typename Key>
+__device__ __forceinline__ void take_pages(const PagedView& cache, const PagedTable& tab, const SelectArgs& a, int seq,
+                                           int sh_row, int len, int count, SelectShared& sh, Key key) {
+  constexpr int NT = kSelectThreads, NW = NT / 64;
+  static_assert(NT == 256, "a thread per digit");
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, ps = 1 << cache.page_shift;
+  const int32_t* pages = tab.pages + (int64_t)seq * tab.stride;
+  const auto put = [&](int i, int p, int page) {
+    a.list[(int64_t)sh_row * a.n_select + i] = page;
+    if (a.selected) a.selected[(int64_t)sh_row * a.n_select + i] = p;
+  };
+  // keys that agree with prefix above `shift` bits: `want` of them are still to be chosen
+  uint64_t prefix = 1;
+  int want = a.n_select, shift = 64;
+  bool exact = count <= a.n_select;   // every key from prefix up is taken
+  if (tid == 0) sh.has_last = 0;
+  if (!exact) {
+    uint64_t lo = ~0ull, hi = 0;
+    for (int p = tid; p < count; p += NT) {
+      const uint64_t k = key(p);
+      lo = k < lo ? k : lo;
+      hi = k > hi ? k : hi;
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) {
+      const uint64_t l = __shfl_xor((unsigned long long)lo, d, 64), h = __shfl_xor((unsigned long long)hi, d, 64);
+      lo = l < lo ? l : lo;
+      hi = h > hi ? h : hi;
+    }
+    if (lane == 0) { sh.range[w][0] = lo; sh.range[w][1] = hi; }
+    __syncthreads();
+    for (int i = 0; i < NW; ++i) {
+      lo = sh.range[i][0] < lo ? sh.range[i][0] : lo;
+      hi = sh.range[i][1] > hi ? sh.range[i][1] : hi;
+    }
+    shift = lo == hi ? 0 : 64 - __builtin_clzll(lo ^ hi);   // bits that are not the same in all keys
+    prefix = shift == 64 ? 0 : hi >> shift << shift;
+  }
+  while (!exact && shift > 0) {
+    const int width = min_i(shift, 8), above = shift;
+    shift -= width;
+    sh.hist[tid] = 0;
+    __syncthreads();
+    for (int p = tid; p < count; p += NT) {
+      const uint64_t k = key(p);
+      if (above == 64 || (k >> above) == (prefix >> above)) atomicAdd(&sh.hist[(k >> shift) & ((1 << width) - 1)], 1);
+    }
+    __syncthreads();
+    // thread t holds digit 255 - t: the digit at which the counts from the top reach `want`
+    const int c = sh.hist[255 - tid];
+    int sum = c;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(sum, d, 64);
+      if (lane >= d) sum += o;
+    }
+    if (lane == 63) sh.scan[w] = sum;
+    __syncthreads();
+    for (int i = 0; i < w; ++i) sum += sh.scan[i];
+    if (sum >= want && sum - c < want) {
+      sh.found[0] = 255 - tid;
+      sh.found[1] = sum - c;
+      sh.found[2] = c;
+    }
+    __syncthreads();
+    prefix |= (uint64_t)sh.found[0] << shift;
+    want -= sh.found[1];
+    exact = sh.found[2] == want;
+  }
+  // keys above the prefix, and of those equal to it (all digits used) the first `want`
+  int taken = 0, equal = 0;
+  for (int p0 = 0; p0 < count; p0 += NT) {
+    const int p = p0 + tid;
+    const uint64_t k = p < count ? key(p) : 0ull;
+    bool take = k != 0 && (exact ? k >= prefix : k > prefix);
+    const bool eq = !exact && k != 0 && k == prefix;
+    if (!exact) {   // rank among the equal keys, in page order
+      const uint64_t b = __ballot(eq);
+      __syncthreads();
+      if (lane == 0) sh.scan[w] = __popcll(b);
+      __syncthreads();
+      int before = equal;
+      for (int i = 0; i < NW; ++i) {
+        before += i < w ? sh.scan[i] : 0;
+        equal += sh.scan[i];
+      }
+      if (eq && before + __popcll(b & ((1ull << lane) - 1)) < want) take = true;
+    }
+    const uint64_t b = __ballot(take);
+    __syncthreads();
+    if (lane == 0) sh.scan[w] = __popcll(b);
+    __syncthreads();
+    int at = taken + __popcll(b & ((1ull << lane) - 1));
+    for (int i = 0; i < NW; ++i) {
+      at += i < w ? sh.scan[i] : 0;
+      taken += sh.scan[i];
+    }
+    if (take) {
+      put(at, p, pages[p]);
+      if (p == count - 1) sh.has_last = 1;
+    }
+  }
+  for (int i = taken + tid; i < a.n_select; i += NT) put(i, -1, -1);
+  __syncthreads();
+  if (tid == 0) a.list_len[sh_row] = taken * ps - (sh.has_last ? count * ps - len : 0);
+}
+
+// Keys of a run of pages per workgroup.
+template <typename T, int DH>
+__global__ __launch_bounds__(kSelectThreads) void page_scores_kernel(PagedView cache, PagedTable tab, SelectArgs a,
+                                                                     int chunks) {
+  __shared__ double qs[2][DH];
+  const int G = cache.n_kv, chunk = blockIdx.x % chunks, row = blockIdx.x / chunks, seq = row / G, hk = row % G;
+  const int len = table_length(tab, seq, cache.page_shift);
+  const int count = (len + (1 << cache.page_shift) - 1) >> cache.page_shift;
+  const int per = (tab.max_pages + chunks - 1) / chunks, first = chunk * per, last = min_i(count, first + per);
+  if (first >= last) return;
+  score_pages<T, DH>(cache, tab, a, seq, hk, count, first, last, qs,
+                     [&](int p, uint64_t k) { a.keys[(int64_t)row * tab.max_pages + p] = k; });
+}
+
+// More pages than a wave holds: the choice by itself, for the attention to read.
+__global__ __launch_bounds__(kSelectThreads) void page_select_kernel(PagedView cache, PagedTable tab, SelectArgs a) {
+  __shared__ SelectShared sh;
+  const int row = blockIdx.x, seq = row / cache.n_kv;
+  const int len = table_length(tab, seq, cache.page_shift);
+  const int count = (len + (1 << cache.page_shift) - 1) >> cache.page_shift;
+  const uint64_t* keys = a.keys + (int64_t)row * tab.max_pages;
+  take_pages(cache, tab, a, seq, row, len, count, sh, [&](int p) { return keys[p]; });
+}
+
 // --------------------------------------------------------------------------- attention of one new token
 // o_h = sum_u softmax_u(scale q_h . k_u) v_u over the entries u < length of the
 // sequence; query head h reads KV head h / (H / H_kv).  One pass over the cache with a
@@ -549,15 +869,19 @@ __device__ __forceinline__ int part_entries(int len, int n_parts) {
   return max_i((per + unit - 1) / unit, 1) * unit;
 }
 
-__device__ __forceinline__ int table_length(const PagedTable& tab, int row, int page_shift) {
-  return max_i(0, (int)min((int64_t)tab.lengths[row], (int64_t)tab.max_pages << page_shift));
-}
+// SEL: attention over selected pages.  kKeys: their keys are in the workspace; kScores:
+// the workgroup forms them; either way its first wave then makes the choice, the same
+// one in every part of a row (what that costs, a few microseconds, is less than a launch
+// and the way through memory).
+enum class Sel { kNone, kKeys, kScores };
 
-template <typename T, int DH>
-__global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cache, PagedTable tab, DecodeArgs a) {
+template <typename T, int DH, Sel SEL>
+__global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cache, PagedTable tab, DecodeArgs a,
+                                                                   SelectArgs sel) {
   using Tile = DecodeTile<T, DH>;
   constexpr int NW = kDecodeWaves, SP = DH + 4;
-  constexpr int AREA = Tile::LDS * NW > NW * 16 * SP * 4 ? Tile::LDS * NW : NW * 16 * SP * 4;
+  constexpr int AREA0 = Tile::LDS * NW > NW * 16 * SP * 4 ? Tile::LDS * NW : NW * 16 * SP * 4;
+  constexpr int AREA = AREA0 > 2 * DH * 8 + kWavePages * 8 ? AREA0 : 2 * DH * 8 + kWavePages * 8;
   __shared__ __attribute__((aligned(16))) char area[AREA];
   __shared__ float sm[NW][16], sl[NW][16];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -579,11 +903,40 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cac
     row = tab.per_head ? seq * G + hk : seq;
     len = table_length(tab, row, cache.page_shift);
   }
+  const int32_t* pages = tab.pages + (int64_t)row * tab.stride;
+  __shared__ int chosen[SEL == Sel::kNone ? 1 : kWavePages], chosen_len;
+  if constexpr (SEL != Sel::kNone) {
+    const int count = (len + (1 << cache.page_shift) - 1) >> cache.page_shift, list = seq * G + hk;
+    const uint64_t* keys = sel.keys + (int64_t)list * tab.max_pages;
+    if constexpr (SEL == Sel::kScores) {
+      static_assert(kSelectThreads == 64 * NW && AREA >= 2 * DH * 8 + kWavePages * 8, "the scores' place");
+      double (*qs)[DH] = reinterpret_cast<double (*)[DH]>(area);
+      uint64_t* scored = reinterpret_cast<uint64_t*>(area + 2 * DH * 8);
+      score_pages<T, DH>(cache, tab, sel, seq, hk, count, 0, count, qs, [&](int p, uint64_t k) { scored[p] = k; });
+      keys = scored;
+      __syncthreads();
+    }
+    if (w == 0) {
+      const bool tell = part == 0 && ht == 0;
+      const int n = take_pages_wave(pages, sel.n_select, len, count, cache.page_shift,
+                                    [&](int p) { return keys[p]; },
+                                    [&](int i, int p, int page) {
+                                      chosen[i] = page;
+                                      if (tell && sel.selected) sel.selected[(int64_t)list * sel.n_select + i] = p;
+                                    });
+      if (lane == 0) {
+        chosen_len = n;
+        if (tell) sel.list_len[list] = n;   // for the joining kernel
+      }
+    }
+    __syncthreads();
+    len = chosen_len;
+  }
+  const auto page_at = [&](int i) { return SEL == Sel::kNone ? pages[i] : chosen[i]; };
   const int per = part_entries(len, a.n_parts);
   const int start = part * per, end = min_i(len, start + per);
   if (part > 0 && start >= len) return;   // the joining kernel knows; part 0 of an empty sequence stays
   const int nh = min_i(16, grp - ht * 16), h0 = hk * grp + ht * 16;
-  const int32_t* pages = tab.pages + (int64_t)row * tab.stride;
   const int shift = cache.page_shift, in_mask = (1 << shift) - 1;
   const int64_t head_at = (int64_t)hk << shift, page_rows = (int64_t)G << shift;
 
@@ -607,7 +960,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cac
   const int last = first + (max_i(end - 1 - first, 0) / step) * step;
   const auto pages_of = [&](int k) {
     const int k0 = min_i(k, last);
-    return Pages{k0, pages[k0 >> shift], pages[min_i(k0 + 16, end - 1) >> shift]};
+    return Pages{k0, page_at(k0 >> shift), page_at(min_i(k0 + 16, end - 1) >> shift)};
   };
   const auto where = [&](Pages p) {
     const int p0 = __builtin_amdgcn_readfirstlane(p.p0), p1 = __builtin_amdgcn_readfirstlane(p.p1);
@@ -778,383 +1131,59 @@ hipError_t launch_decode(const PagedView& cache, const PagedTable& tab, DecodeAr
   // start are short (32 sequences of 100 .. 8192 entries, 8 KV heads: 128 -> 117 us; equal
   // lengths pay 1 %, 16 short fp32 sequences 43 -> 46 us; 64 lanes know 64 sequences)
   a.longest_first = blocks > 512 && tab.n_seqs <= 64 && !tab.per_head;
-#define RK_DECODE(T, DH)                                                                                        \
-  do {                                                                                                          \
-    decode_kernel<T, DH><<<(uint32_t)blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, a);                         \
-    if (a.n_parts > 1)                                                                                          \
-      decode_join_kernel<T, DH><<<tab.n_seqs * a.n_heads, 256, 0, s>>>(tab, a, cache.n_kv, cache.page_shift);    \
+#define RK_DECODE(T, DH)                                                                                           \
+  do {                                                                                                             \
+    decode_kernel<T, DH, Sel::kNone><<<(uint32_t)blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, a, SelectArgs{});  \
+    if (a.n_parts > 1)                                                                                             \
+      decode_join_kernel<T, DH><<<tab.n_seqs * a.n_heads, 256, 0, s>>>(tab, a, cache.n_kv, cache.page_shift);      \
   } while (0)
   RK_PAGED_DISPATCH(cache.bf16, cache.head_dim, RK_DECODE);
 #undef RK_DECODE
   return hipGetLastError();
 }
 
-// --------------------------------------------------------------------------- page selection
-// Score of a page for one KV head: sum over the query heads h that share it of
-// sum_x max(q_hx lo_x, q_hx hi_x), an upper bound of the summed products with any key
-// of the page.  The heads can be summed first: sum_x hi_x Q+_x + lo_x Q-_x with
-// Q+ = sum_h max(q_h, 0), Q- = sum_h min(q_h, 0).  In double precision throughout, so
-// the choice does not hang on the order of a sum.  Bound: memory, the bounds of every
-// page read once.
-//
-// A score becomes a whole number that orders the same way: larger for a larger score;
-// the largest of all for pages that are always kept, 0 for pages that hold nothing (a
-// NaN score counts as -inf).
-__device__ __forceinline__ uint64_t score_key(double x) {
-  if (x != x) x = -INFINITY;
-  const uint64_t u = (uint64_t)__double_as_longlong(x + 0.0);   // -0 and 0 are one score
-  return u >> 63 ? ~u : u | 0x8000000000000000ull;
-}
+// Bounds of a row up to which the attention's workgroups score the pages themselves: a CU
+// reads them in less time than another launch takes.  8 sequences of 2048 in pages of 16,
+// 12 heads of 64, 32 KB of bounds a row: 13.9 us, with the scores in a launch of their own
+// 14.5; half as many pages 9.2 and 11.0; twice as many, 64 KB, 20.0 and 17.3.  Not where more
+// than two parts of a row outnumber the places that 256 CUs have for them: 32 sequences of
+// 4096 in pages of 64, 8 KV heads of 128, 4 parts: 51.7 and 47.
+constexpr int64_t kScoreBytes = 1 << 15;
 
-constexpr int kSelectThreads = 256;
-constexpr int kWavePages = 1024;    // pages whose keys one wave holds in registers
-
-// Q-, Q+ of a KV head, by the first DH threads
-template <typename T, int DH>
-__device__ __forceinline__ void sum_queries(const SelectArgs& a, int seq, int hk, int grp, double (*qs)[DH]) {
-  const int x = threadIdx.x;
-  if (x >= DH) return;
-  double lo = 0.0, hi = 0.0;
-  const T* qp = (const T*)a.q + (int64_t)seq * a.q_rs + (int64_t)hk * grp * DH + x;
-  for (int h = 0; h < grp; ++h) {
-    const double v = (double)Act<T>::load(qp + (int64_t)h * DH);
-    lo += v < 0.0 ? v : 0.0;
-    hi += v < 0.0 ? 0.0 : v;
-  }
-  qs[0][x] = lo;
-  qs[1][x] = hi;
-}
-
-// Keys of pages first .. last - 1 of a sequence: a group of LPP lanes per page (its lower
-// bounds, then its upper ones), four pages in flight.  put(p, key).
-template <typename T, int DH, int NT, typename Put>
-__device__ __forceinline__ void score_pages(const PagedView& cache, const PagedTable& tab, const SelectArgs& a, int seq,
-                                            int hk, int count, int first, int last, const double (*qs)[DH], Put put) {
-  constexpr int VE = Pack<T>::N, LPP = 2 * DH / VE, PER = NT / LPP, U = 4;
-  const int sub = threadIdx.x % LPP, x0 = (sub * VE) % DH, side = sub * VE / DH;
-  double q[VE];
-#pragma unroll
-  for (int e = 0; e < VE; ++e) q[e] = qs[side][x0 + e];
-  const int32_t* pages = tab.pages + (int64_t)seq * tab.stride;
-  for (int p0 = first + threadIdx.x / LPP; p0 - (int)threadIdx.x / LPP < last; p0 += PER * U) {
-    v4u raw[U];
-    bool ok[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int page = pages[min_i(p0 + u * PER, last - 1)];
-      ok[u] = page >= 0 && page < cache.n_pages;
-      raw[u] = *(const v4u*)((const T*)cache.bounds + ((int64_t)(ok[u] ? page : 0) * cache.n_kv + hk) * 2 * DH + sub * VE);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int p = p0 + u * PER;
-      float f[VE];
-      Pack<T>::get(raw[u], f);
-      double s = 0.0;
-#pragma unroll
-      for (int e = 0; e < VE; ++e) s += q[e] * (q[e] != 0.0 ? (double)f[e] : 0.0);   // an infinite bound of 0 counts 0
-#pragma unroll
-      for (int d = LPP / 2; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
-      if (sub == 0 && p < last)
-        put(p, !ok[u] ? 0ull : p < a.keep_first || p >= count - a.keep_last ? ~0ull : score_key(s));
-    }
-  }
-}
-
-struct SelectShared {
-  uint64_t range[kSelectThreads / 64][2];
-  int hist[256], scan[kSelectThreads / 64], found[3], has_last;
-};
-
-// Where the chosen pages of a row go.
-struct Taken {
-  int32_t *list, *selected;
-  const int32_t* pages;
-  __device__ __forceinline__ Taken(const PagedTable& tab, const SelectArgs& a, int seq, int row) {
-    list = a.list + (int64_t)row * a.n_select;
-    selected = a.selected ? a.selected + (int64_t)row * a.n_select : nullptr;
-    pages = tab.pages + (int64_t)seq * tab.stride;
-  }
-  __device__ __forceinline__ void put(int i, int p, int page) const {   // page p of the sequence
-    list[i] = page;
-    if (selected) selected[i] = p;
-  }
-};
-
-// One wave: the n_select largest keys of `count` <= kWavePages pages, ties to the lower
-// page, by halving an interval of keys until exactly that many reach its lower end (a
-// dozen steps on scores that differ; 64 and a tie at most).  Every step is counting in
-// registers, no barrier: 512 pages of a row: 7.7 us with its
-// launch, by digits in a workgroup 9.1.
-// key(p): 0 for a page that holds nothing, never taken.
-template <typename Key>
-__device__ __forceinline__ void take_pages_wave(const PagedTable& tab, const SelectArgs& a, int seq, int row, int len,
-                                                int count, int page_shift, Key key) {
-  constexpr int HELD = kWavePages / 64;
-  const int lane = threadIdx.x & 63, n = a.n_select;
-  const uint64_t lower = (1ull << lane) - 1;
-  const Taken out(tab, a, seq, row);
-  uint64_t k[HELD];
-  int page[HELD];
-  int real = 0, forced = 0;
-  uint32_t top = 0, bottom = 0;   // of the upper halves of the keys in between: the largest, the complement of the least
-  // whole runs of loads, no branch between them
-#pragma unroll
-  for (int i0 = 0; i0 < HELD; i0 += 4) {
-    if (i0 * 64 < count) {
-#pragma unroll
-      for (int i = i0; i < i0 + 4; ++i) {
-        k[i] = key(min_i(i * 64 + lane, count - 1));
-        page[i] = out.pages[min_i(i * 64 + lane, count - 1)];
-      }
-#pragma unroll
-      for (int i = i0; i < i0 + 4; ++i) k[i] = i * 64 + lane < count ? k[i] : 0ull;
-    } else {
-#pragma unroll
-      for (int i = i0; i < i0 + 4; ++i) k[i] = 0;
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < HELD; ++i) {
-    if (i * 64 >= count) break;
-    real += __popcll(__ballot(k[i] != 0));
-    forced += __popcll(__ballot(k[i] == ~0ull));
-    if (k[i] != 0 && k[i] != ~0ull) {
-      top = max(top, (uint32_t)(k[i] >> 32));
-      bottom = max(bottom, ~(uint32_t)(k[i] >> 32));
-    }
-  }
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) {
-    top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
-    bottom = max(bottom, (uint32_t)__shfl_xor((int)bottom, d, 64));
-  }
-  // first by the upper halves, in which scores that differ by a millionth differ
-  uint32_t lo32 = ~(uint32_t)__builtin_amdgcn_readfirstlane((int)bottom);
-  uint32_t hi32 = (uint32_t)__builtin_amdgcn_readfirstlane((int)top);
-  bool exact = real <= n || forced == n;
-  const bool given = exact;
-  while (!exact && lo32 < hi32) {
-    const uint32_t mid = lo32 + (hi32 - lo32) / 2 + 1;
-    int c = 0;
-#pragma unroll
-    for (int i = 0; i < HELD; ++i)
-      if (i * 64 < count) c += __popcll(__ballot((uint32_t)(k[i] >> 32) >= mid));
-    if (c >= n) lo32 = mid; else hi32 = mid - 1;
-    exact = c == n;
-  }
-  uint64_t lo = given ? (real <= n ? 1ull : ~0ull) : (uint64_t)lo32 << 32;
-  uint64_t hi = (uint64_t)lo32 << 32 | 0xffffffffu;
-  while (!exact && lo < hi) {
-    const uint64_t mid = lo + (hi - lo) / 2 + 1;
-    int c = 0;
-#pragma unroll
-    for (int i = 0; i < HELD; ++i)
-      if (i * 64 < count) c += __popcll(__ballot(k[i] >= mid));
-    if (c >= n) lo = mid; else hi = mid - 1;
-    exact = c == n;
-  }
-  int want = n;   // of the keys equal to lo
-  if (!exact) {
-#pragma unroll
-    for (int i = 0; i < HELD; ++i)
-      if (i * 64 < count) want -= __popcll(__ballot(k[i] > lo));
-  }
-  int taken = 0;
-  bool last = false;
-#pragma unroll
-  for (int i = 0; i < HELD; ++i) {
-    if (i * 64 >= count) break;
-    bool take = k[i] > lo || (exact && k[i] == lo);
-    if (!exact) {
-      const uint64_t e = __ballot(k[i] == lo);
-      if (k[i] == lo && __popcll(e & lower) < want) take = true;
-      want -= __popcll(e);
-    }
-    const uint64_t b = __ballot(take);
-    if (take) out.put(taken + __popcll(b & lower), i * 64 + lane, page[i]);
-    taken += __popcll(b);
-    if ((count - 1) / 64 == i) last = b >> ((count - 1) & 63) & 1;
-  }
-  for (int i = taken + lane; i < n; i += 64) out.put(i, -1, -1);
-  // entries of the chosen pages: whole pages, but for the sequence's last one, which comes last
-  if (lane == 0) a.list_len[row] = (taken << page_shift) - (last ? (count << page_shift) - len : 0);
-}
-
-// The workgroup: the same for any number of pages, by the digits of the key, 8 bits a step
-// from the highest bit in which any two differ; the search ends as soon as the pages at
-// or above the digits found are exactly those wanted.
-template <typename Key>
-__device__ __forceinline__ void take_pages(const PagedView& cache, const PagedTable& tab, const SelectArgs& a, int seq,
-                                           int sh_row, int len, int count, SelectShared& sh, Key key) {
-  constexpr int NT = kSelectThreads, NW = NT / 64;
-  static_assert(NT == 256, "a thread per digit");
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, ps = 1 << cache.page_shift;
-  const Taken out(tab, a, seq, sh_row);
-  // keys that agree with prefix above `shift` bits: `want` of them are still to be chosen
-  uint64_t prefix = 1;
-  int want = a.n_select, shift = 64;
-  bool exact = count <= a.n_select;   // every key from prefix up is taken
-  if (tid == 0) sh.has_last = 0;
-  if (!exact) {
-    uint64_t lo = ~0ull, hi = 0;
-    for (int p = tid; p < count; p += NT) {
-      const uint64_t k = key(p);
-      lo = k < lo ? k : lo;
-      hi = k > hi ? k : hi;
-    }
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) {
-      const uint64_t l = __shfl_xor((unsigned long long)lo, d, 64), h = __shfl_xor((unsigned long long)hi, d, 64);
-      lo = l < lo ? l : lo;
-      hi = h > hi ? h : hi;
-    }
-    if (lane == 0) { sh.range[w][0] = lo; sh.range[w][1] = hi; }
-    __syncthreads();
-    for (int i = 0; i < NW; ++i) {
-      lo = sh.range[i][0] < lo ? sh.range[i][0] : lo;
-      hi = sh.range[i][1] > hi ? sh.range[i][1] : hi;
-    }
-    shift = lo == hi ? 0 : 64 - __builtin_clzll(lo ^ hi);   // bits that are not the same in all keys
-    prefix = shift == 64 ? 0 : hi >> shift << shift;
-  }
-  while (!exact && shift > 0) {
-    const int width = min_i(shift, 8), above = shift;
-    shift -= width;
-    sh.hist[tid] = 0;
-    __syncthreads();
-    for (int p = tid; p < count; p += NT) {
-      const uint64_t k = key(p);
-      if (above == 64 || (k >> above) == (prefix >> above)) atomicAdd(&sh.hist[(k >> shift) & ((1 << width) - 1)], 1);
-    }
-    __syncthreads();
-    // thread t holds digit 255 - t: the digit at which the counts from the top reach `want`
-    const int c = sh.hist[255 - tid];
-    int sum = c;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(sum, d, 64);
-      if (lane >= d) sum += o;
-    }
-    if (lane == 63) sh.scan[w] = sum;
-    __syncthreads();
-    for (int i = 0; i < w; ++i) sum += sh.scan[i];
-    if (sum >= want && sum - c < want) {
-      sh.found[0] = 255 - tid;
-      sh.found[1] = sum - c;
-      sh.found[2] = c;
-    }
-    __syncthreads();
-    prefix |= (uint64_t)sh.found[0] << shift;
-    want -= sh.found[1];
-    exact = sh.found[2] == want;
-  }
-  // keys above the prefix, and of those equal to it (all digits used) the first `want`
-  int taken = 0, equal = 0;
-  for (int p0 = 0; p0 < count; p0 += NT) {
-    const int p = p0 + tid;
-    const uint64_t k = p < count ? key(p) : 0ull;
-    bool take = k != 0 && (exact ? k >= prefix : k > prefix);
-    const bool eq = !exact && k != 0 && k == prefix;
-    if (!exact) {   // rank among the equal keys, in page order
-      const uint64_t b = __ballot(eq);
-      __syncthreads();
-      if (lane == 0) sh.scan[w] = __popcll(b);
-      __syncthreads();
-      int before = equal;
-      for (int i = 0; i < NW; ++i) {
-        before += i < w ? sh.scan[i] : 0;
-        equal += sh.scan[i];
-      }
-      if (eq && before + __popcll(b & ((1ull << lane) - 1)) < want) take = true;
-    }
-    const uint64_t b = __ballot(take);
-    __syncthreads();
-    if (lane == 0) sh.scan[w] = __popcll(b);
-    __syncthreads();
-    int at = taken + __popcll(b & ((1ull << lane) - 1));
-    for (int i = 0; i < NW; ++i) {
-      at += i < w ? sh.scan[i] : 0;
-      taken += sh.scan[i];
-    }
-    if (take) {
-      out.put(at, p, out.pages[p]);
-      if (p == count - 1) sh.has_last = 1;
-    }
-  }
-  for (int i = taken + tid; i < a.n_select; i += NT) out.put(i, -1, -1);
-  __syncthreads();
-  if (tid == 0) a.list_len[sh_row] = taken * ps - (sh.has_last ? count * ps - len : 0);
-}
-
-// One workgroup per (sequence, KV head): scores in LDS, then the choice.
-template <typename T, int DH>
-__global__ __launch_bounds__(kSelectThreads) void page_choose_kernel(PagedView cache, PagedTable tab, SelectArgs a) {
-  __shared__ double qs[2][DH];
-  __shared__ uint64_t keys[kWavePages];
-  const int G = cache.n_kv, seq = blockIdx.x / G, hk = blockIdx.x % G;
-  const int len = table_length(tab, seq, cache.page_shift);
-  const int count = (len + (1 << cache.page_shift) - 1) >> cache.page_shift;
-  sum_queries<T, DH>(a, seq, hk, a.n_heads / G, qs);
-  __syncthreads();
-  score_pages<T, DH, kSelectThreads>(cache, tab, a, seq, hk, count, 0, count, qs,
-                                     [&](int p, uint64_t k) { keys[p] = k; });
-  __syncthreads();
-  if (threadIdx.x < 64)
-    take_pages_wave(tab, a, seq, blockIdx.x, len, count, cache.page_shift, [&](int p) { return keys[p]; });
-}
-
-// The two halves for more pages: keys of a run of pages per workgroup, then the choice.
-template <typename T, int DH>
-__global__ __launch_bounds__(256) void page_scores_kernel(PagedView cache, PagedTable tab, SelectArgs a, int chunks) {
-  __shared__ double qs[2][DH];
-  const int G = cache.n_kv, chunk = blockIdx.x % chunks, row = blockIdx.x / chunks, seq = row / G, hk = row % G;
-  const int len = table_length(tab, seq, cache.page_shift);
-  const int count = (len + (1 << cache.page_shift) - 1) >> cache.page_shift;
-  const int per = (tab.max_pages + chunks - 1) / chunks, first = chunk * per, last = min_i(count, first + per);
-  if (first >= last) return;
-  sum_queries<T, DH>(a, seq, hk, a.n_heads / G, qs);
-  __syncthreads();
-  score_pages<T, DH, 256>(cache, tab, a, seq, hk, count, first, last, qs,
-                          [&](int p, uint64_t k) { a.keys[(int64_t)row * tab.max_pages + p] = k; });
-}
-
-// WAVE: at most kWavePages pages, one wave per row.
-template <bool WAVE>
-__global__ __launch_bounds__(WAVE ? 64 : kSelectThreads) void page_select_kernel(PagedView cache, PagedTable tab,
-                                                                                 SelectArgs a) {
-  const int row = blockIdx.x, seq = row / cache.n_kv;
-  const int len = table_length(tab, seq, cache.page_shift);
-  const int count = (len + (1 << cache.page_shift) - 1) >> cache.page_shift;
-  const uint64_t* keys = a.keys + (int64_t)row * tab.max_pages;
-  if constexpr (WAVE) {
-    take_pages_wave(tab, a, seq, row, len, count, cache.page_shift, [&](int p) { return keys[p]; });
-  } else {
-    __shared__ SelectShared sh;
-    take_pages(cache, tab, a, seq, row, len, count, sh, [&](int p) { return keys[p]; });
-  }
-}
-
-// One launch where one CU reads a row's bounds in less than the time of another, or where
-// the rows alone fill the card.
-constexpr int64_t kChooseBytes = 1 << 16;
-
-hipError_t launch_page_select(const PagedView& cache, const PagedTable& tab, const SelectArgs& a, hipStream_t s) {
+hipError_t launch_decode_selected(const PagedView& cache, const PagedTable& tab, const DecodeArgs& a,
+                                  const SelectArgs& sel, hipStream_t s) {
   const int rows = tab.n_seqs * cache.n_kv, page_bytes = 2 * cache.head_dim * (cache.bf16 ? 2 : 4);
-  if (tab.max_pages <= kWavePages && ((int64_t)tab.max_pages * page_bytes <= kChooseBytes || rows >= 1024)) {
-#define RK_CHOOSE(T, DH) page_choose_kernel<T, DH><<<rows, kSelectThreads, 0, s>>>(cache, tab, a)
-    RK_PAGED_DISPATCH(cache.bf16, cache.head_dim, RK_CHOOSE);
-#undef RK_CHOOSE
-    return hipGetLastError();
-  }
-  // a workgroup's threads four times over, split further while CUs are idle
-  const int per_pass = 256 * 16 * 4 / page_bytes;
-  const int chunks = std::max(1, std::min((tab.max_pages + per_pass - 1) / per_pass, std::max(1, 2048 / rows)));
-#define RK_SCORES(T, DH) page_scores_kernel<T, DH><<<(uint32_t)rows * chunks, 256, 0, s>>>(cache, tab, a, chunks)
-  RK_PAGED_DISPATCH(cache.bf16, cache.head_dim, RK_SCORES);
+  PagedTable lists = tab;   // a row for each (sequence, KV head): its chosen pages
+  lists.pages = sel.list; lists.lengths = sel.list_len; lists.stride = lists.max_pages = sel.n_select;
+  lists.per_head = true;
+  const bool held = tab.max_pages <= kWavePages && sel.n_select <= kWavePages;
+  const bool alone = held && (int64_t)tab.max_pages * page_bytes <= kScoreBytes &&
+                     (a.n_parts <= 2 || (int64_t)rows * a.n_parts <= 512);
+  if (!alone) {
+    // a workgroup's threads four times over, split further while CUs are idle
+    const int per_pass = kSelectThreads * 16 * 4 / page_bytes;
+    const int chunks = std::max(1, std::min((tab.max_pages + per_pass - 1) / per_pass, std::max(1, 2048 / rows)));
+#define RK_SCORES(T, DH) \
+  page_scores_kernel<T, DH><<<(uint32_t)rows * chunks, kSelectThreads, 0, s>>>(cache, tab, sel, chunks)
+    RK_PAGED_DISPATCH(cache.bf16, cache.head_dim, RK_SCORES);
 #undef RK_SCORES
-  if (tab.max_pages <= kWavePages) page_select_kernel<true><<<rows, 64, 0, s>>>(cache, tab, a);
-  else page_select_kernel<false><<<rows, kSelectThreads, 0, s>>>(cache, tab, a);
+  }
+  if (!held) {
+    page_select_kernel<<<rows, kSelectThreads, 0, s>>>(cache, tab, sel);
+    return launch_decode(cache, lists, a, s);
+  }
+  DecodeArgs d = a;
+  d.longest_first = false;
+  const uint32_t blocks = (uint32_t)((int64_t)rows * ((a.n_heads / cache.n_kv + 15) / 16) * a.n_parts);
+#define RK_DECODE(T, DH)                                                                                              \
+  do {                                                                                                                \
+    if (alone) decode_kernel<T, DH, Sel::kScores><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, d, sel);           \
+    else decode_kernel<T, DH, Sel::kKeys><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, d, sel);                   \
+    if (a.n_parts > 1)                                                                                                \
+      decode_join_kernel<T, DH><<<tab.n_seqs * a.n_heads, 256, 0, s>>>(lists, d, cache.n_kv, cache.page_shift);       \
+  } while (0)
+  RK_PAGED_DISPATCH(cache.bf16, cache.head_dim, RK_DECODE);
+#undef RK_DECODE
   return hipGetLastError();
 }
 

@@ -273,7 +273,9 @@ struct SelectArgs {
   int32_t* list_len;        // [n_seqs * n_kv] entries
   int32_t* selected;        // [n_seqs * n_kv, n_select] pages of the sequence, then -1; or NULL
 };
-hipError_t launch_page_select(const PagedView& cache, const PagedTable& tab, const SelectArgs& a, hipStream_t s);
+// launch_decode over the pages that sel chooses from tab's.
+hipError_t launch_decode_selected(const PagedView& cache, const PagedTable& tab, const DecodeArgs& a,
+                                  const SelectArgs& sel, hipStream_t s);
 
 // --------------------------------------------------------------------------- token log probabilities
 struct LogprobArgs {

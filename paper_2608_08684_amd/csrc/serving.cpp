@@ -138,23 +138,19 @@ rk_status attention(const rk_paged_cache* cache, const rk_paged_seqs* seqs, cons
   hipStream_t s = (hipStream_t)stream;
   if ((e = check_stream(s)) != RK_OK) return e;
   char* ws = (char*)workspace;
-  if (sel) {
-    SelectArgs a;
-    a.q = q; a.q_rs = q_row_stride;
-    a.n_heads = n_heads; a.n_select = sel->n_select; a.keep_first = sel->keep_first; a.keep_last = sel->keep_last;
-    a.keys = (uint64_t*)(ws + p.keys); a.list = (int32_t*)(ws + p.list); a.list_len = (int32_t*)(ws + p.list_len);
-    a.selected = sel->selected;
-    Timed timed("page_select", s);
-    if ((e = hip_status("page selection", launch_page_select(v, t, a, s))) != RK_OK) return e;
-    t.pages = a.list; t.lengths = a.list_len; t.stride = sel->n_select; t.max_pages = sel->n_select; t.per_head = true;
-  }
-  DecodeArgs a;
+  DecodeArgs a{};
   a.q = q; a.out = out; a.lse = lse; a.q_rs = q_row_stride; a.out_rs = out_row_stride;
   a.n_heads = n_heads; a.n_parts = p.n_parts;
   a.scale = scale > 0.f ? scale : (float)(1.0 / sqrt((double)v.head_dim));
   a.part_o = (float*)(ws + p.part_o); a.part_lse = (float*)(ws + p.part_lse);
   Timed timed("paged_attention", s);
-  return hip_status("paged attention", launch_decode(v, t, a, s));
+  if (!sel) return hip_status("paged attention", launch_decode(v, t, a, s));
+  SelectArgs c{};
+  c.q = q; c.q_rs = q_row_stride;
+  c.n_heads = n_heads; c.n_select = sel->n_select; c.keep_first = sel->keep_first; c.keep_last = sel->keep_last;
+  c.keys = (uint64_t*)(ws + p.keys); c.list = (int32_t*)(ws + p.list); c.list_len = (int32_t*)(ws + p.list_len);
+  c.selected = sel->selected;
+  return hip_status("attention over selected pages", launch_decode_selected(v, t, a, c, s));
 }
 
 }  // namespace

@@ -195,6 +195,13 @@ def test_more_pages_than_the_sequences_have():
     check_selected(case, 64, 2, 2)
 
 
+@pytest.mark.parametrize("n_select", [3, 1023, 1024, 1025])
+@pytest.mark.parametrize("pages", [1, 1023, 1024, 1025])
+def test_around_a_thousand_pages(pages, n_select):
+    case = Case([16 * pages - 5, 16 * (pages // 2)], 2, 1, 64, 16, "bf16", seed=pages + n_select, bounds=True)
+    check_selected(case, n_select, 0, 2)
+
+
 def test_ties_go_to_the_lower_page():
     """Pages with the same bounds, and a query of zeros (every score 0)."""
     case = Case([640, 640], 4, 2, 64, 16, "bf16", seed=13, bounds=True)
