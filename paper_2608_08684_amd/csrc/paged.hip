@@ -1147,7 +1147,9 @@ hipError_t launch_decode(const PagedView& cache, const PagedTable& tab, DecodeAr
 // 12 heads of 64, 32 KB of bounds a row: 13.9 us, with the scores in a launch of their own
 // 14.5; half as many pages 9.2 and 11.0; twice as many, 64 KB, 20.0 and 17.3.  Not where more
 // than two parts of a row outnumber the places that 256 CUs have for them: 32 sequences of
-// 4096 in pages of 64, 8 KV heads of 128, 4 parts: 51.7 and 47.
+// 4096 in pages of 64, 8 KV heads of 128, 4 parts: 51.7 and 47.  Nor where more than 16 query
+// heads share a KV head, which would be scored by several workgroups, one of which may
+// have written its outputs over the queries that another still reads.
 constexpr int64_t kScoreBytes = 1 << 15;
 
 hipError_t launch_decode_selected(const PagedView& cache, const PagedTable& tab, const DecodeArgs& a,
@@ -1157,7 +1159,8 @@ hipError_t launch_decode_selected(const PagedView& cache, const PagedTable& tab,
   lists.pages = sel.list; lists.lengths = sel.list_len; lists.stride = lists.max_pages = sel.n_select;
   lists.per_head = true;
   const bool held = tab.max_pages <= kWavePages && sel.n_select <= kWavePages;
-  const bool alone = held && (int64_t)tab.max_pages * page_bytes <= kScoreBytes &&
+  const int head_tiles = (a.n_heads / cache.n_kv + 15) / 16;
+  const bool alone = held && head_tiles == 1 && (int64_t)tab.max_pages * page_bytes <= kScoreBytes &&
                      (a.n_parts <= 2 || (int64_t)rows * a.n_parts <= 512);
   if (!alone) {
     // a workgroup's threads four times over, split further while CUs are idle
@@ -1174,7 +1177,7 @@ hipError_t launch_decode_selected(const PagedView& cache, const PagedTable& tab,
   }
   DecodeArgs d = a;
   d.longest_first = false;
-  const uint32_t blocks = (uint32_t)((int64_t)rows * ((a.n_heads / cache.n_kv + 15) / 16) * a.n_parts);
+  const uint32_t blocks = (uint32_t)((int64_t)rows * head_tiles * a.n_parts);
 #define RK_DECODE(T, DH)                                                                                              \
   do {                                                                                                                \
     if (alone) decode_kernel<T, DH, Sel::kScores><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, d, sel);           \

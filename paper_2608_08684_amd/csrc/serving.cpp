@@ -11,6 +11,7 @@ namespace rk {
 namespace {
 
 const int64_t kMaxGrid = 0x7fffffff;
+const int32_t kMaxSeqs = 1 << 23;
 const int64_t kMaxEntries = 1 << 30;   // of one sequence: part bounds stay within 32 bits
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -65,6 +66,7 @@ rk_status check_buffers(const PagedView& v) {
 rk_status check_seqs(const rk_paged_seqs* q, const PagedView& v, PagedTable* t) {
   if (!q || !q->pages || !q->lengths) return bad(RK_ERR_ARG, "null sequences, pages or lengths");
   if (q->n_seqs < 1 || q->max_pages < 1) return bad(RK_ERR_ARG, "n_seqs and max_pages must be positive");
+  if (q->n_seqs > kMaxSeqs) return bad(RK_ERR_SHAPE, "n_seqs must be at most 2^23");
   if (q->page_stride < q->max_pages) return bad(RK_ERR_ARG, "page_stride below max_pages");
   if (((int64_t)q->max_pages << v.page_shift) > kMaxEntries) return bad(RK_ERR_SHAPE, "max_pages * page_size must be at most 2^30");
   t->pages = q->pages; t->lengths = q->lengths; t->stride = q->page_stride;

@@ -303,6 +303,21 @@ def test_captured_calls_follow_lengths_and_pages():
         assert torch.equal(eager[0], o2) and torch.equal(eager[2], sel)
 
 
+@pytest.mark.parametrize("heads, kv_heads, d, page, dtype", SHAPES)
+@pytest.mark.parametrize("longest", [100, 1800])
+def test_outputs_over_the_queries(heads, kv_heads, d, page, dtype, longest):
+    import torch
+    case = Case([longest, 1, 0, 77, longest // 2], heads, kv_heads, d, page, dtype, seed=heads + longest, bounds=True)
+    ws = case.workspace(3)
+    for call in (lambda q, out: case.cache.attention(case.seqs, q, out, ws),
+                 lambda q, out: case.cache.attention_selected(case.seqs, q, out, ws, n_select=3)):
+        out, _ = case.outputs()
+        call(case.q, out)
+        own = case.q.clone()
+        call(own, own)
+        assert torch.equal(own, out)
+
+
 def test_binding_refusals():
     import torch
     case = Case([20], 4, 2, 64, 16, "bf16", seed=19)

@@ -30,7 +30,8 @@ CACHE_BAD = [
     (U, dict(head_dim=256, dtype=rk.RK_F32)),
 ]
 SEQS_BAD = [(A, dict(pages=None)), (A, dict(lengths=None)), (A, dict(n_seqs=0)), (A, dict(max_pages=0)),
-            (A, dict(page_stride=3)), (S, dict(max_pages=(1 << 26) + 1, page_stride=1 << 27))]
+            (A, dict(page_stride=3)), (S, dict(n_seqs=(1 << 23) + 1)),
+            (S, dict(max_pages=(1 << 26) + 1, page_stride=1 << 27))]
 
 
 def append(cache={}, seqs={}, rows={}):
