@@ -81,7 +81,8 @@ __device__ __forceinline__ int max_i(int a, int b) { return a > b ? a : b; }
 // bounds so take them in a fixed order without atomics; values of 16 entries; queries
 // of up to 8 rows.  The first loads go out before the angles are formed.
 // Bound: memory (each value read once, written once); 28112 rows, 32 / 8 heads of 128:
-// 95 us, a copy of as many bytes 89.  A step's row: the latency of one pass.
+// 92 us (4.8 TB/s), a copy of as many bytes 89.  A step's rows (64 sequences): the latency
+// of one pass, 6 us.
 constexpr int kAppendThreads = 256, kAppendRows = 16, kAppendQueryRows = 8;
 
 // cosine and sine of channel pair x at position pos
@@ -368,7 +369,8 @@ hipError_t launch_append(const PagedView& cache, const PagedTable& tab, AppendAr
 // of the page.  The heads can be summed first: sum_x hi_x Q+_x + lo_x Q-_x with
 // Q+ = sum_h max(q_h, 0), Q- = sum_h min(q_h, 0).  In double precision throughout, so
 // the choice does not hang on the order of a sum.  Bound: memory, the bounds of every
-// page read once.
+// page read once, and below a few megabytes latency: 4 rows of 512 pages, 8 KV heads of
+// 128, 7 MB: 7 us.
 //
 // A score becomes a whole number that orders the same way: larger for a larger score;
 // the largest of all for pages that are always kept, 0 for pages that hold nothing (a
@@ -453,9 +455,10 @@ struct SelectShared {
 // One wave: the n_select largest keys of `count` <= kWavePages pages, ties to the lower
 // page, by halving an interval of keys until exactly that many reach its lower end (a
 // dozen steps on scores that differ; 64 and a tie at most).  Every step is counting in
-// registers, no barrier.  key(p): 0 for a page that holds nothing, never taken.
-// put(i, p, page): the i-th is page p of the sequence.  Returns the entries of the chosen
-// pages: whole pages, but for the sequence's last one, which comes last.
+// registers, no barrier: 512 pages 2 us less than by digits in a workgroup.
+// key(p): 0 for a page that holds nothing, never taken.  put(i, p, page): the i-th is page
+// p of the sequence.  Returns the entries of the chosen pages: whole pages, but for the
+// sequence's last one, which comes last.
 template <typename Key, typename Put>
 __device__ __forceinline__ int take_pages_wave(const int32_t* pages, int n, int len, int count, int page_shift, Key key,
                                                Put put) {
@@ -700,6 +703,11 @@ __global__ __launch_bounds__(kSelectThreads) void page_select_kernel(PagedView c
 // the output then carries only its own rounding.
 // Entries on pages outside the cache and entries past the length weigh nothing; their
 // scores are replaced by -inf and their values by 0, whatever memory holds there.
+// Bound: memory.  8 KV heads of 128, 32 query heads, with the join: 64 sequences of 4096
+// 195 us (5.5 TB/s, a plain read of as much 6), 32 of 100 .. 8192 113 us (5.2), 2 of up to
+// 32768 55 us (4.6: the join and the first tile's way, lengths to pages to keys, are 9 of
+// them).  8 waves a workgroup, three workgroups per CU, equal runs of tiles for every
+// workgroup whatever the sequences' lengths: all slower or the same.
 constexpr int kDecodeWaves = 4, kTile = 32;
 
 template <typename T, int DH> struct DecodeTile;
@@ -881,7 +889,8 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cac
   using Tile = DecodeTile<T, DH>;
   constexpr int NW = kDecodeWaves, SP = DH + 4;
   constexpr int AREA0 = Tile::LDS * NW > NW * 16 * SP * 4 ? Tile::LDS * NW : NW * 16 * SP * 4;
-  constexpr int AREA = AREA0 > 2 * DH * 8 + kWavePages * 8 ? AREA0 : 2 * DH * 8 + kWavePages * 8;
+  constexpr int SCORES = SEL == Sel::kScores ? 2 * DH * 8 + kWavePages * 8 : 0;
+  constexpr int AREA = AREA0 > SCORES ? AREA0 : SCORES;
   __shared__ __attribute__((aligned(16))) char area[AREA];
   __shared__ float sm[NW][16], sl[NW][16];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -909,7 +918,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cac
     const int count = (len + (1 << cache.page_shift) - 1) >> cache.page_shift, list = seq * G + hk;
     const uint64_t* keys = sel.keys + (int64_t)list * tab.max_pages;
     if constexpr (SEL == Sel::kScores) {
-      static_assert(kSelectThreads == 64 * NW && AREA >= 2 * DH * 8 + kWavePages * 8, "the scores' place");
+      static_assert(kSelectThreads == 64 * NW, "score_pages");
       double (*qs)[DH] = reinterpret_cast<double (*)[DH]>(area);
       uint64_t* scored = reinterpret_cast<uint64_t*>(area + 2 * DH * 8);
       score_pages<T, DH>(cache, tab, sel, seq, hk, count, 0, count, qs, [&](int p, uint64_t k) { scored[p] = k; });
@@ -1070,8 +1079,8 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cac
 // Joins the parts of one (sequence, query head): o = sum_s e^(lse_s - M) o_s / sum_s e^(lse_s - M).
 // A workgroup of 256 threads: every wave forms the weights (the same sums in the same
 // order), 256 / DH thread groups take the parts in turn, eight loads in flight each.
-// Bound: latency; 64 parts of 128 channels, 64 rows: 19.5 us with one group and a load
-// at a time.
+// Bound: latency; 64 parts of 128 channels, 64 rows: 5.4 us, with one group and a load
+// at a time 19.5.
 constexpr int kMaxDecodeParts = 256;
 
 template <typename T, int DH>
@@ -1116,12 +1125,27 @@ __global__ __launch_bounds__(256) void decode_join_kernel(PagedTable tab, Decode
   if (a.lse && x == 0) a.lse[blockIdx.x] = L == 0.f ? -INFINITY : ref + logf(L);
 }
 
-// Parts per (sequence, KV head): enough workgroups for four on each of the 256 CUs, no
-// part shorter than 256 entries.
+// Parts per row, a row being a (sequence, KV head, head tile), from the longest that a
+// sequence may be; no part shorter than 256 entries.  A split costs its join (4 - 5 us) and
+// gains where rows leave CUs idle or, being of unequal length, end at different times.  us
+// for 8 KV heads of 128 in bf16, all of that length | lengths from 100 up to it:
+//   up to 512 one part: a workgroup's 512 entries take as long as the join (1 row of 8 heads
+//     9.0, two parts 9.9; 256 rows 14.5 | 12.0 and 19.7 | 17.1);
+//   up to 1024 for 256 workgroups, but one part from 96 rows on (128 rows 15.2 | 14.7, two
+//     parts 17.9 | 15.3; 32 rows 14.3 | 14.0, four 11.3 | 10.8);
+//   below 4096 for 256, one to a CU (64 rows of 2048: 4 parts 18.0 | 14.8, 8 20.0 | 17.7;
+//     256 rows: 1 part 51.5 | 36.2, 4 58.2 | 40.9), but two where one would leave some CUs two
+//     rows and the others one (288 rows of 64 channels: 39.9 | 24.7, two parts 37.8 | 22.2);
+//   from 4096 for 256, and four as long as that is no more than 1280 workgroups: unequal
+//     lengths cost more than the join (8192, 256 rows: 1 part 187 | 125, 4 191 | 108, 512
+//     rows 365 | 235, 2 parts 372 | 197; 32 rows: 8 parts 32.6 | 21.4, 32 35.7 | 27.6).
 int decode_parts(int n_seqs, int n_heads, int n_kv, int64_t max_entries) {
   const int64_t rows = (int64_t)n_seqs * n_kv * ((n_heads / n_kv + 15) / 16);
-  const int64_t want = (1024 + rows - 1) / rows, most = std::max<int64_t>(1, max_entries / 256);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), kMaxDecodeParts));
+  int64_t want = 256 / rows;
+  if (max_entries <= 512 || (max_entries <= 1024 && rows >= 96)) want = 1;
+  else if (max_entries >= 4096) want = std::max(want, std::min<int64_t>(4, 1280 / rows));
+  else if (max_entries > 1024 && rows > 256 && rows < 512) want = 2;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, max_entries / 256), kMaxDecodeParts));
 }
 
 hipError_t launch_decode(const PagedView& cache, const PagedTable& tab, DecodeArgs a, hipStream_t s) {
@@ -1147,9 +1171,10 @@ hipError_t launch_decode(const PagedView& cache, const PagedTable& tab, DecodeAr
 // 12 heads of 64, 32 KB of bounds a row: 13.9 us, with the scores in a launch of their own
 // 14.5; half as many pages 9.2 and 11.0; twice as many, 64 KB, 20.0 and 17.3.  Not where more
 // than two parts of a row outnumber the places that 256 CUs have for them: 32 sequences of
-// 4096 in pages of 64, 8 KV heads of 128, 4 parts: 51.7 and 47.  Nor where more than 16 query
-// heads share a KV head, which would be scored by several workgroups, one of which may
-// have written its outputs over the queries that another still reads.
+// 16384 in pages of 256, 16 of them read, 8 KV heads of 128, 4 parts: 117 and 110.  Nor
+// where more than 16 query heads share a KV head: they would be scored by several
+// workgroups, one of which may have written its outputs over the queries that another
+// still reads.
 constexpr int64_t kScoreBytes = 1 << 15;
 
 hipError_t launch_decode_selected(const PagedView& cache, const PagedTable& tab, const DecodeArgs& a,
