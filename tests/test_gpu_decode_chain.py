@@ -149,6 +149,40 @@ def test_decoding_over_compressed_caches(heads, kv_heads, head_dim, P, budgets, 
             assert dec.seqs[l].lengths.tolist() == [budgets[l] + W] * n
 
 
+class Side:
+    """The buffers of a decode step and the step: append, attention over selected pages, log probabilities."""
+
+    def __init__(self, n, H, G, d, page):
+        import torch
+        self.n, self.H, self.G, self.d = n, H, G, d
+        self.qkv = torch.empty(n, (H + 2 * G) * d, dtype=torch.bfloat16, device="cuda")
+        k = torch.zeros(3 * n + 1, G, page, d, dtype=torch.bfloat16, device="cuda")
+        self.cache = rk.PagedCache(k, k.clone(), torch.zeros(3 * n + 1, G, 2, d, dtype=k.dtype, device="cuda"))
+        self.seqs = rk.PagedSeqs(torch.arange(3 * n, dtype=torch.int32, device="cuda").view(n, 3),
+                                 torch.tensor([0, 7, 30], dtype=torch.int32, device="cuda") % 28)
+        self.q = torch.empty(n, H, d, dtype=torch.bfloat16, device="cuda")
+        self.out, self.lse = torch.empty_like(self.q), torch.empty(n, H, device="cuda")
+        self.ws = torch.empty(self.cache.workspace_size(n, 3, H, 2), dtype=torch.uint8, device="cuda")
+        self.logits = torch.empty(n, H * d, device="cuda")
+        self.tok = torch.tensor([1, 2, 511], dtype=torch.int32, device="cuda")
+        self.lp, self.ent = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+        self.ids = torch.empty(n, 9, dtype=torch.int32, device="cuda")
+        self.lws = torch.empty(rk.token_logprobs_workspace_size(n, H * d, 9), dtype=torch.uint8, device="cuda")
+
+    def step(self):
+        x, n, H, G, d = self.qkv, self.n, self.H, self.G, self.d
+        self.seqs.lengths.add_(1)
+        self.cache.append(self.seqs, x[:, H * d:(H + G) * d].view(n, G, d), x[:, (H + G) * d:].view(n, G, d),
+                          q=x[:, :H * d].view(n, H, d), q_out=self.q, rope_theta=1e4)
+        self.cache.attention_selected(self.seqs, self.q, self.out, self.ws, n_select=2, lse=self.lse)
+        self.logits.copy_(self.out.view(n, -1))      # any numbers that follow from the step
+        rk.token_logprobs(self.logits, self.tok, self.lws, logprob=self.lp, entropy=self.ent, top_ids=self.ids)
+
+    def all(self):
+        return (self.cache.k, self.cache.v, self.cache.key_bounds, self.q, self.out, self.lse, self.lp, self.ent,
+                self.ids, self.seqs.lengths)
+
+
 def test_the_steps_of_a_loop_as_one_graph():
     """A captured decode step (append, attention, log probabilities) replayed: the same cache, outputs and scores as
     eager steps, to the last bit."""
@@ -157,36 +191,7 @@ def test_the_steps_of_a_loop_as_one_graph():
     gen = torch.Generator().manual_seed(5)
     rows = torch.randn(steps, n, (H + 2 * G) * d, generator=gen).bfloat16().cuda()
 
-    class Side:
-        def __init__(self):
-            self.qkv = torch.empty(n, (H + 2 * G) * d, dtype=torch.bfloat16, device="cuda")
-            k = torch.zeros(3 * n + 1, G, page, d, dtype=torch.bfloat16, device="cuda")
-            self.cache = rk.PagedCache(k, k.clone(), torch.zeros(3 * n + 1, G, 2, d, dtype=k.dtype, device="cuda"))
-            self.seqs = rk.PagedSeqs(torch.arange(3 * n, dtype=torch.int32, device="cuda").view(n, 3),
-                                     torch.tensor([0, 7, 30], dtype=torch.int32, device="cuda") % 28)
-            self.q = torch.empty(n, H, d, dtype=torch.bfloat16, device="cuda")
-            self.out, self.lse = torch.empty_like(self.q), torch.empty(n, H, device="cuda")
-            self.ws = torch.empty(self.cache.workspace_size(n, 3, H, 2), dtype=torch.uint8, device="cuda")
-            self.logits = torch.empty(n, H * d, device="cuda")
-            self.tok = torch.tensor([1, 2, 511], dtype=torch.int32, device="cuda")
-            self.lp, self.ent = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
-            self.ids = torch.empty(n, 9, dtype=torch.int32, device="cuda")
-            self.lws = torch.empty(rk.token_logprobs_workspace_size(n, H * d, 9), dtype=torch.uint8, device="cuda")
-
-        def step(self):
-            x = self.qkv
-            self.seqs.lengths.add_(1)
-            self.cache.append(self.seqs, x[:, H * d:(H + G) * d].view(n, G, d), x[:, (H + G) * d:].view(n, G, d),
-                              q=x[:, :H * d].view(n, H, d), q_out=self.q, rope_theta=1e4)
-            self.cache.attention_selected(self.seqs, self.q, self.out, self.ws, n_select=2, lse=self.lse)
-            self.logits.copy_(self.out.view(n, -1))      # any numbers that follow from the step
-            rk.token_logprobs(self.logits, self.tok, self.lws, logprob=self.lp, entropy=self.ent, top_ids=self.ids)
-
-        def all(self):
-            return (self.cache.k, self.cache.v, self.cache.key_bounds, self.q, self.out, self.lse, self.lp, self.ent,
-                    self.ids, self.seqs.lengths)
-
-    eager, graphed = Side(), Side()
+    eager, graphed = Side(n, H, G, d, page), Side(n, H, G, d, page)
     graphed.qkv.copy_(rows[0])
     warm = torch.cuda.Stream()
     warm.wait_stream(torch.cuda.current_stream())
@@ -206,3 +211,26 @@ def test_the_steps_of_a_loop_as_one_graph():
         g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(eager.all(), graphed.all()))
+
+
+def test_two_loops_at_once():
+    """Two decode loops on streams of their own, each with its buffers, against the same loops one after the other."""
+    import torch
+    n, H, G, d, page, steps = 3, 8, 2, 64, 16, 18
+    gen = torch.Generator().manual_seed(6)
+    rows = torch.randn(2, steps, n, (H + 2 * G) * d, generator=gen).bfloat16().cuda()
+    alone, both = [[Side(n, H, G, d, page) for _ in range(2)] for _ in range(2)]
+    for side, own in zip(alone, rows):
+        for x in own:
+            side.qkv.copy_(x)
+            side.step()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for t in range(steps):
+        for side, own, stream in zip(both, rows, streams):
+            with torch.cuda.stream(stream):
+                side.qkv.copy_(own[t])
+                side.step()
+    torch.cuda.synchronize()
+    for one, other in zip(alone, both):
+        assert all(torch.equal(a, b) for a, b in zip(one.all(), other.all()))
