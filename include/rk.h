@@ -559,7 +559,8 @@ rk_status rk_paged_append(const rk_paged_cache *cache, const rk_paged_seqs *seqs
                           void *stream);
 
 /* Workspace bytes of rk_paged_attention (n_select = 0) or of both it and
- * rk_paged_attention_selected with that many pages; 0 for invalid arguments.     */
+ * rk_paged_attention_selected with that many pages, for up to n_seqs sequences and
+ * max_pages pages; 0 for invalid arguments.                                      */
 size_t rk_paged_workspace_size(const rk_paged_cache *cache, int32_t n_seqs, int32_t max_pages, int32_t n_heads,
                                int32_t n_select);
 

@@ -232,7 +232,10 @@ size_t rk_paged_workspace_size(const rk_paged_cache* cache, int32_t n_seqs, int3
   PagedView v;
   if (check_cache(cache, &v) != RK_OK || n_seqs < 1 || max_pages < 1 || n_select < 0) return 0;
   if (((int64_t)std::max(max_pages, n_select) << v.page_shift) > kMaxEntries || check_heads(v, n_seqs, n_heads) != RK_OK) return 0;
-  return paged_plan(v, n_seqs, max_pages, n_heads, n_select).total;
+  // fewer rows may be split into more parts; from 2048 rows on none is (decode_parts)
+  size_t most = paged_plan(v, n_seqs, max_pages, n_heads, n_select).total;
+  for (int n = std::min(n_seqs, 2048); n >= 1; --n) most = std::max(most, paged_plan(v, n, max_pages, n_heads, n_select).total);
+  return most;
 }
 
 rk_status rk_paged_attention(const rk_paged_cache* cache, const rk_paged_seqs* seqs, const void* q,

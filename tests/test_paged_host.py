@@ -105,8 +105,13 @@ def test_workspace_sizes():
         c = make(_PagedCache, CACHE, **{**dict(k=None, v=None, key_bounds=None), **kw})
         return rk.load().rk_paged_workspace_size(ctypes.byref(c), n, pages, heads, select)
     assert size() > 0 and size(select=4) > size() and size(pages=4096) > size()
-    # one part per sequence and KV head: nothing to join
-    assert size(n=4096, pages=4096) == size(n=4096, pages=8) < size(n=1, pages=4096)
+    # enough for fewer sequences and shorter tables, which may be split into more parts
+    sizes = [[size(n=n, pages=p, heads=64, select=s) for n in (1, 2, 5, 31, 32, 64, 100, 127, 300, 640, 641, 1279, 4096)
+              for p in (4, 8, 32, 64, 65, 100, 255, 256, 4096)] for s in (0, 1, 70, 300)]
+    grids = [np.array(x, dtype=np.int64).reshape(13, 9) for x in sizes]
+    for grid in grids:
+        assert (np.diff(grid, axis=0) >= 0).all() and (np.diff(grid, axis=1) >= 0).all()
+    assert all((b >= a).all() for a, b in zip(grids, grids[1:]))
     for bad in (dict(n=0), dict(pages=0), dict(heads=3), dict(select=-1), dict(page_size=20), dict(pages=1 << 27)):
         assert size(**bad) == 0
     sz = rk.token_logprobs_workspace_size
