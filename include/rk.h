@@ -602,7 +602,7 @@ rk_status rk_paged_attention_selected(const rk_paged_cache *cache, const rk_page
 /* Most alternatives of rk_token_logprobs. */
 #define RK_MAX_TOP 32
 
-/* Workspace bytes of rk_token_logprobs; 0 for invalid arguments. */
+/* Workspace bytes of rk_token_logprobs for up to n_rows rows; 0 for invalid arguments. */
 size_t rk_token_logprobs_workspace_size(int64_t n_rows, int32_t vocab, rk_dtype dtype, int32_t n_top);
 
 /* Of each row of logits x (those of rk_profile_layer and rk_policy_damage, or any):

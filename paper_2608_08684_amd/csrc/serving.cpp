@@ -272,7 +272,10 @@ static LogprobPlan logprob_plan(int64_t n_rows, int32_t vocab, rk_dtype dtype, i
 }
 
 size_t rk_token_logprobs_workspace_size(int64_t n_rows, int32_t vocab, rk_dtype dtype, int32_t n_top) {
-  return logprob_plan(n_rows, vocab, dtype, n_top).total;
+  // fewer rows may be split into more parts; beyond 256 the number of rows changes nothing there
+  size_t most = logprob_plan(n_rows, vocab, dtype, n_top).total;
+  for (int64_t n = std::min<int64_t>(n_rows, 256); n >= 1 && most; --n) most = std::max(most, logprob_plan(n, vocab, dtype, n_top).total);
+  return most;
 }
 
 rk_status rk_token_logprobs(const void *logits, rk_dtype dtype, int64_t n_rows, int32_t vocab, int64_t row_stride,

@@ -116,6 +116,10 @@ def test_workspace_sizes():
         assert size(**bad) == 0
     sz = rk.token_logprobs_workspace_size
     assert sz(16, 10 ** 6, 5) > sz(16, 10 ** 6, 0) > sz(16, 32000, 5) > 0 and sz(1, 1 << 22, 32) > 0
+    for vocab in (1000, 32000, 128256, 10 ** 6, 1 << 22):
+        for dtype in ("f32", "bf16"):
+            assert (np.diff([sz(n, vocab, 20, dtype) for n in (0, 1, 2, 3, 7, 16, 50, 64, 127, 128, 129, 256, 257, 2000)])
+                    >= 0).all()
     assert sz(-1, 10, 0) == sz(1, 0, 0) == sz(1, 10, 11) == sz(1, 100, rk.RK_MAX_TOP + 1) == sz(1, 10, -1) == 0
 
 
