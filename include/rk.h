@@ -573,7 +573,9 @@ size_t rk_paged_workspace_size(const rk_paged_cache *cache, int32_t n_seqs, int3
  *   scale:  0 for 1 / sqrt(head_dim).
  *   lse:    DEVICE fp32 [n_seqs, n_heads] or NULL: log sum_u e^(scale q . k_u).
  * A sequence with nothing to see gets zeros and a log-sum-exp of -inf.  fp32
- * softmax, sums and outputs, rounded once.                                       */
+ * softmax, sums and outputs, rounded once.  An infinite Value among the entries makes its
+ * channel that infinity (NaN with the other one beside it, or where its weight is below
+ * e^-60 of the largest, which may count as 0); a NaN Value or score makes it NaN.  */
 rk_status rk_paged_attention(const rk_paged_cache *cache, const rk_paged_seqs *seqs, const void *q,
                              int64_t q_row_stride, int32_t n_heads, float scale, void *out, int64_t out_row_stride,
                              float *lse, void *workspace, size_t ws_bytes, void *stream);

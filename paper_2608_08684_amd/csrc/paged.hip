@@ -65,6 +65,12 @@ __device__ __forceinline__ float exp_diff_exact(float x) {
   return __builtin_amdgcn_exp2f(t) * fmaf(r, 0.6931471806f, 1.0f);
 }
 
+// The largest bf16 below a positive x, as the bits of a float; 0 of 0.  What is left, x minus
+// it, is positive again, never 0 (at the least one step of x).
+__device__ __forceinline__ uint32_t bf16_below(float x) {
+  return __builtin_elementwise_sub_sat(__float_as_uint(x), 1u) & 0xffff0000u;
+}
+
 __device__ __forceinline__ int min_i(int a, int b) { return a < b ? a : b; }
 __device__ __forceinline__ int max_i(int a, int b) { return a > b ? a : b; }
 
@@ -698,9 +704,10 @@ __global__ __launch_bounds__(kSelectThreads) void page_select_kernel(PagedView c
 //           product (entries 4 g + i of its 16-lane group g), and V^T comes out of a
 //           row-major LDS tile with transposing reads (bf16) or from memory with d
 //           spread over the product's rows (fp32).
-// bf16: a weight p is split into bf16(p) + bf16(p - bf16(p)), 16 bits in all: the
-// matrix unit has the time (a tile's 16 KB take longer to arrive than 20 MFMAs), and
-// the output then carries only its own rounding.
+// bf16: a weight p is the sum of three bf16 numbers, all of its 24 bits: the matrix unit has
+// the time (a tile's 16 KB take longer to arrive than 32 MFMAs), and the output then carries
+// only its own rounding.  All three are positive, so that an infinite value stays one (a part
+// of the other sign, or of 0, would make it NaN).
 // Entries on pages outside the cache and entries past the length weigh nothing; their
 // scores are replaced by -inf and their values by 0, whatever memory holds there.
 // Bound: memory.  8 KV heads of 128, 32 query heads, with the join: 64 sequences of 4096
@@ -770,12 +777,16 @@ template <int DH> struct DecodeTile<bf16_t, DH> {
   }
   static constexpr bool kStaged = true;
   __device__ __forceinline__ void values(const f32x4_t p[2], f32x4_t* o, char* lds, int lane) const {
-    bf16x8_t hi, lo;
+    v4u part[3];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float x = p[e >> 2][e & 3];
-      hi[e] = (__bf16)x;
-      lo[e] = (__bf16)(x - (float)hi[e]);
+    for (int e = 0; e < 8; e += 2) {
+      const float x = p[e >> 2][e & 3], y = p[e >> 2][(e & 3) + 1];
+      const uint32_t x0 = bf16_below(x), y0 = bf16_below(y);
+      const float x1 = x - __uint_as_float(x0), y1 = y - __uint_as_float(y0);
+      const uint32_t x2 = bf16_below(x1), y2 = bf16_below(y1);
+      part[0][e / 2] = __builtin_amdgcn_perm(y0, x0, 0x07060302u);   // the upper halves
+      part[1][e / 2] = __builtin_amdgcn_perm(y2, x2, 0x07060302u);
+      part[2][e / 2] = (uint32_t)f2bf(x1 - __uint_as_float(x2)) | ((uint32_t)f2bf(y1 - __uint_as_float(y2)) << 16);
     }
     const int g = lane >> 4, jj = lane & 15, r = 4 * g + (jj >> 2);
 #pragma unroll
@@ -786,8 +797,10 @@ template <int DH> struct DecodeTile<bf16_t, DH> {
       const s16x4_t a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * CH * 16));
       const v4u a = {__builtin_bit_cast(v2u, a0)[0], __builtin_bit_cast(v2u, a0)[1], __builtin_bit_cast(v2u, a1)[0],
                      __builtin_bit_cast(v2u, a1)[1]};
-      o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), hi, o[b], 0, 0, 0);
-      o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), lo, o[b], 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a),
+                                                       __builtin_bit_cast(bf16x8_t, part[i]), o[b], 0, 0, 0);
     }
     wave_sync();
   }
