@@ -57,12 +57,13 @@ template <> struct Pack<float> {
 // log2(e): scaling the scores themselves would put that factor's rounding, times a
 // score of 50, into the weights.
 __device__ __forceinline__ float exp_diff(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
-// The same with the product's rounding and log2(e)'s made good, for fp32 caches, whose
-// outputs show them: e^-10 is off by 5e-7 without.
-__device__ __forceinline__ float exp_diff_exact(float x) {
+// unit e^x with the product's rounding and log2(e)'s made good, for the weights of fp32
+// caches, whose outputs show them: e^-10 is off by 5e-7 without.  (Rescales and joins do
+// without: what they are off by is no more than the rounding of a score as large.)
+__device__ __forceinline__ float exp_diff_exact(float x, float unit) {
   x = x < -200.f ? -200.f : x;   // 0 either way; a NaN stays
   const float t = x * kLog2e, r = fmaf(x, kLog2e, -t) + x * 1.925963033500e-8f;
-  return __builtin_amdgcn_exp2f(t) * fmaf(r, 0.6931471806f, 1.0f);
+  return __builtin_amdgcn_exp2f(t) * fmaf(r, 0.6931471806f * unit, unit);
 }
 
 // The largest bf16 below a positive x, as the bits of a float; 0 of 0.  What is left, x minus
@@ -969,6 +970,9 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cac
 #pragma unroll
   for (int i = 0; i < Tile::ND; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
+  // Weights count in units of a power of two above the part's entries: their sum stays below
+  // 1, and that of weighted values below the largest, however large they are.
+  const float unit = __uint_as_float((127u - (32u - __builtin_clz(max_i(end - start, 1)))) << 23);
   // Pages of the tile at entry k0 (at the part's last tile where k0 lies past its end) and
   // its rows.  A page that holds nothing is read as page 0 and not used.
   struct Pages {
@@ -1046,7 +1050,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cac
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        s[t][i] = sizeof(T) == 4 ? exp_diff_exact(s[t][i] - ref) : exp_diff(s[t][i] - ref);
+        s[t][i] = sizeof(T) == 4 ? exp_diff_exact(s[t][i] - ref, unit) : exp_diff(s[t][i] - ref) * unit;
         l += s[t][i];
       }
     tile.values(s, o, area + w * Tile::LDS, lane);
@@ -1077,7 +1081,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cac
     }
     // nothing seen: 0, with a log-sum-exp of -inf (a NaN sum stays NaN)
     v = L == 0.f ? 0.f : v / L;
-    const float lse = L == 0.f ? -INFINITY : ref + logf(L);
+    const float lse = L == 0.f ? -INFINITY : ref + logf(L / unit);
     const int64_t at = (int64_t)seq * a.n_heads + h0 + h;
     if (a.n_parts == 1) {
       Act<T>::store((T*)a.out + (int64_t)seq * a.out_rs + (int64_t)(h0 + h) * DH + x, v);
@@ -1118,7 +1122,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(PagedTable tab, Decode
   float L = 0.f;
 #pragma unroll
   for (int i = 0; i < kMaxDecodeParts / 64; ++i) {
-    lse[i] = exp_diff(lse[i] - ref);
+    lse[i] = exp_diff(lse[i] - ref) * (1.0f / kMaxDecodeParts);   // so that no sum of outputs overflows
     L += lse[i];
     if (tid < 64 && i * 64 < n) wt[i * 64 + lane] = lse[i];
   }
@@ -1135,7 +1139,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(PagedTable tab, Decode
 #pragma unroll
   for (int i = 1; i < NG; ++i) v += red[i][x];
   Act<T>::store((T*)a.out + (int64_t)seq * a.out_rs + (int64_t)h * DH + x, L == 0.f ? 0.f : v / L);
-  if (a.lse && x == 0) a.lse[blockIdx.x] = L == 0.f ? -INFINITY : ref + logf(L);
+  if (a.lse && x == 0) a.lse[blockIdx.x] = L == 0.f ? -INFINITY : ref + logf(L * kMaxDecodeParts);
 }
 
 // Parts per row, a row being a (sequence, KV head, head tile), from the longest that a

@@ -1,12 +1,13 @@
-"""Attention over a paged cache with infinite Values.
+"""Attention over a paged cache whose Values are infinite, or so large that the sum of a row's Values overflows.
 
-A weight is positive however small, so an infinite Value that a row sees makes its channel that infinity."""
+A weight is positive however small, so an infinite Value that a row sees makes its channel that infinity; a weighted mean
+is never larger than the largest Value."""
 import numpy as np
 import pytest
 
 from oracle import paged as OP
 
-from paged_helpers import Case, attention_tolerance, f64
+from paged_helpers import Case, attention_tolerance, check_attention, f64
 
 pytestmark = pytest.mark.gpu
 
@@ -106,3 +107,25 @@ def test_an_infinite_value_of_a_small_weight(dtype, d, n):
     case.cache.attention(case.seqs, case.q, out, case.workspace(), scale=1.0, lse=lse)
     assert (out[0, :, 7] == -float("inf")).all() and out[0, :, 8:].isfinite().all()
     assert (lse == 50.0).all()
+
+
+@pytest.mark.parametrize("heads, kv_heads, d, page, dtype", SHAPES)
+@pytest.mark.parametrize("lengths", [LENGTHS + [0], SPLIT], ids=["whole", "split"])
+@pytest.mark.parametrize("selected", [False, True], ids=["every page", "chosen pages"])
+def test_values_near_the_largest(heads, kv_heads, d, page, dtype, lengths, selected):
+    """Values of one sign and up to 3e38: their sum overflows, their mean does not."""
+    import torch
+    case = Case(lengths, heads, kv_heads, d, page, dtype, seed=3, bounds=selected)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = 3.0e38 * (0.5 + 0.5 * torch.rand(case.v.shape, generator=g, device="cuda"))
+    x[..., 1::2].neg_()
+    case.v.copy_(torch.where(case.v.isnan(), case.v, x.to(case.v.dtype)))
+    check_attention(case, *attend(case, case.table.shape[1] if selected else 0))
+
+
+@pytest.mark.parametrize("dtype, d", [("bf16", 64), ("f32", 64)])
+def test_small_values(dtype, d):
+    """Values down to 1e-30 keep their relative precision."""
+    case = Case(LENGTHS + SPLIT, 4, 2, d, 16, dtype, seed=5)
+    case.v.mul_(1.0e-30)
+    check_attention(case, *attend(case, 0))
