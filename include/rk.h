@@ -496,7 +496,8 @@ rk_status rk_spearman(const double *x, const double *y, int32_t n, double *rho);
  *               rotated Keys and the Values;
  *   key_bounds: DEVICE [n_pages, n_kv_heads, 2, head_dim] in dtype, or NULL: for
  *               each page, KV head and channel the least and the largest value over
- *               the Keys written to the page since its entry 0 was last written.
+ *               the Keys written to the page since its entry 0 was last written (both
+ *               NaN where one of those is).
  *               rk_paged_append keeps them, rk_paged_attention_selected reads them.
  * page_size: a power of two, 16 .. 256.  head_dim: as in rk_model_config.  All
  * buffers 16-byte aligned.                                                        */

@@ -72,6 +72,10 @@ __device__ __forceinline__ uint32_t bf16_below(float x) {
   return __builtin_elementwise_sub_sat(__float_as_uint(x), 1u) & 0xffff0000u;
 }
 
+// Bounds keep a NaN.
+__device__ __forceinline__ float least(float a, float b) { return __builtin_elementwise_minimum(a, b); }
+__device__ __forceinline__ float largest(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
 __device__ __forceinline__ int min_i(int a, int b) { return a < b ? a : b; }
 __device__ __forceinline__ int max_i(int a, int b) { return a > b ? a : b; }
 
@@ -284,8 +288,8 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedView cache,
             Pack<T>::get(raw[q].hi, y + VE);
 #pragma unroll
             for (int e = 0; e < 2 * VE; ++e) {
-              bl[e] = fminf(bl[e], y[e]);
-              bh[e] = fmaxf(bh[e], y[e]);
+              bl[e] = least(bl[e], y[e]);
+              bh[e] = largest(bh[e], y[e]);
             }
           }
         }
@@ -310,13 +314,13 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedView cache,
         Pack<T>::get(*(const v4u*)(bp + side * DH), y);
         Pack<T>::get(*(const v4u*)(bp + side * DH + HALF), y + VE);
 #pragma unroll
-        for (int e = 0; e < 2 * VE; ++e) y[e] = side ? fmaxf(y[e], red[tid][e]) : fminf(y[e], red[tid][e]);
+        for (int e = 0; e < 2 * VE; ++e) y[e] = side ? largest(y[e], red[tid][e]) : least(y[e], red[tid][e]);
       }
       for (int q = 1; q < rows_used; ++q)
 #pragma unroll
         for (int e = 0; e < 2 * VE; ++e) {
           const float z = red[tid + q * units][e];
-          y[e] = side ? fmaxf(y[e], z) : fminf(y[e], z);
+          y[e] = side ? largest(y[e], z) : least(y[e], z);
         }
       *(v4u*)(bp + side * DH) = Pack<T>::put(y);
       *(v4u*)(bp + side * DH + HALF) = Pack<T>::put(y + VE);
