@@ -569,8 +569,8 @@ size_t rk_paged_workspace_size(const rk_paged_cache *cache, int32_t n_seqs, int3
  *   out_i,h = sum_u softmax_u(scale q_i,h . k_u) v_u,  u < lengths[i],
  * query head h reading KV head h / (n_heads / n_kv_heads).
  *   q, out: DEVICE, dtype of the cache, sequence i at q + i * q_row_stride elements,
- *           n_heads contiguous heads; 16-byte aligned rows.  out may be q itself, and
- *           overlaps nothing else that the call reads.
+ *           n_heads contiguous heads; 16-byte aligned rows.  out may be q itself with
+ *           its stride, and overlaps nothing else that the call reads.
  *   scale:  0 for 1 / sqrt(head_dim).
  *   lse:    DEVICE fp32 [n_seqs, n_heads] or NULL: log sum_u e^(scale q . k_u).
  * A sequence with nothing to see gets zeros and a log-sum-exp of -inf.  fp32

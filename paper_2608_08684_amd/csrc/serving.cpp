@@ -127,6 +127,8 @@ rk_status attention(const rk_paged_cache* cache, const rk_paged_seqs* seqs, cons
   const int64_t width = (int64_t)n_heads * v.head_dim;
   if ((e = check_rows(q, q_row_stride, width, v.bf16, "q")) != RK_OK) return e;
   if ((e = check_rows(out, out_row_stride, width, v.bf16, "out")) != RK_OK) return e;
+  if (q == out && t.n_seqs > 1 && q_row_stride != out_row_stride)
+    return bad(RK_ERR_ARG, "outputs over the queries need one row stride");
   if (!isfinite(scale) || scale < 0.f) return bad(RK_ERR_ARG, "scale must be finite and >= 0 (0: 1 / sqrt(head_dim))");
   if (sel) {
     if (!v.bounds) return bad(RK_ERR_ARG, "the selection needs key_bounds");
