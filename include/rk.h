@@ -555,7 +555,10 @@ typedef struct {
  * to the entries lengths[i] - m_i .. lengths[i] - 1 of each sequence, m_i its number
  * of rows, and updates the bounds of their pages.  Rows whose entry is negative or
  * lies on no page are not written (their queries are still rotated).  A page that a
- * call writes to must be named by one sequence, once.                           */
+ * call writes to must be named by one sequence, once.  A call of more than 2^24 - 1
+ * workgroups is RK_ERR_SHAPE.  With many rows it takes, for each page written, one for
+ * every 2 KB of a Key row (n_kv_heads * head_dim values) and one for every 16 entries (or
+ * one, with a row per sequence), and one for 8 rows of queries.                 */
 rk_status rk_paged_append(const rk_paged_cache *cache, const rk_paged_seqs *seqs, const rk_paged_rows *rows,
                           void *stream);
 

@@ -341,33 +341,38 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedView cache,
   } while (0)
 
 // Page blocks: the pages that the new rows of a sequence may touch, one sequence after the other.
-hipError_t launch_append(const PagedView& cache, const PagedTable& tab, AppendArgs a, const SeqTable& st,
-                         hipStream_t s) {
-  if (a.n_rows <= 0) return hipSuccess;
+int64_t append_plan(const PagedView& cache, const PagedTable& tab, const SeqTable& st, AppendArgs* a) {
   const int ps = 1 << cache.page_shift, G = cache.n_kv;
   int pages = 0;
-  if (a.one_row) {
+  if (a->one_row) {
     pages = tab.n_seqs;
   } else {
     for (int i = 0; i < st.n; ++i) {   // m rows touch at most (m + ps - 2) / ps + 1 pages
-      a.block0[i] = pages;
+      a->block0[i] = pages;
       const int m = st.off[i + 1] - st.off[i];
       if (m > 0) pages += (int)(((int64_t)m + ps - 2) / ps) + 1;
     }
   }
+  if (pages == 0) return 0;
   // KV heads of a key block: at most a quarter of its threads wide (four rows at a time),
   // and few enough for 512 blocks (2048 rows in pages of 128, 8 heads: 59 us with whole
   // pages, 25 with single heads)
   const int widest = 64 / (cache.head_dim / 2 / (cache.bf16 ? 8 : 4));
-  a.head_blocks = std::max((G + widest - 1) / widest, std::min(G, (512 + pages - 1) / pages));
-  a.heads = (G + a.head_blocks - 1) / a.head_blocks;
-  const int64_t key_blocks = (int64_t)pages * a.head_blocks, value_blocks = (int64_t)pages * (a.one_row ? 1 : ps / kAppendRows);
-  a.q_rows = std::max(1, std::min(kAppendQueryRows, a.n_rows / 1024));
-  const int64_t q_blocks = a.q ? ((int64_t)a.n_rows + a.q_rows - 1) / a.q_rows : 0;
-  if (key_blocks + value_blocks + q_blocks > 0x7fffffff) return hipErrorInvalidValue;
-  a.key_blocks = (int)key_blocks;
-  a.value_blocks = (int)value_blocks;
-  const uint32_t blocks = (uint32_t)(key_blocks + value_blocks + q_blocks);
+  a->head_blocks = std::max((G + widest - 1) / widest, std::min(G, (512 + pages - 1) / pages));
+  a->heads = (G + a->head_blocks - 1) / a->head_blocks;
+  const int64_t key_blocks = (int64_t)pages * a->head_blocks;
+  const int64_t value_blocks = (int64_t)pages * (a->one_row ? 1 : ps / kAppendRows);
+  a->q_rows = std::max(1, std::min(kAppendQueryRows, a->n_rows / 1024));
+  const int64_t q_blocks = a->q ? ((int64_t)a->n_rows + a->q_rows - 1) / a->q_rows : 0;
+  a->key_blocks = (int)key_blocks;
+  a->value_blocks = (int)value_blocks;
+  return key_blocks + value_blocks + q_blocks;
+}
+
+hipError_t launch_append(const PagedView& cache, const PagedTable& tab, const AppendArgs& a, const SeqTable& st,
+                         int64_t workgroups, hipStream_t s) {
+  if (workgroups <= 0) return hipSuccess;
+  const uint32_t blocks = (uint32_t)workgroups;
 #define RK_APPEND(T, DH) append_kernel<T, DH><<<blocks, kAppendThreads, 0, s>>>(cache, tab, a, st)
   RK_PAGED_DISPATCH(cache.bf16, cache.head_dim, RK_APPEND);
 #undef RK_APPEND

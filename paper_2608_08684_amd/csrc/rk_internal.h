@@ -219,6 +219,9 @@ hipError_t launch_snap_select(const float* votes, int64_t prefix_rows, const voi
                               int pool_kernel, bool pool_avg, int n_items, const int16_t* seq, const int16_t* layer,
                               const int32_t* keep, const int64_t* entry0, int32_t* positions, void* k_out, void* v_out,
                               float* scores, hipStream_t s);
+// A launch has fewer than 2^32 threads; of workgroups of 256:
+constexpr int64_t kMaxWorkgroups = 0xffffffffll / 256;
+
 // --------------------------------------------------------------------------- paged cache
 struct PagedView {
   void *k, *v, *bounds;   // [n_pages, n_kv, 1 << page_shift, head_dim]; bounds [n_pages, n_kv, 2, head_dim] or NULL
@@ -243,13 +246,15 @@ struct AppendArgs {
   bool one_row;             // one new row per sequence; otherwise the rows of a SeqTable
   bool rotate;
   uint64_t freq[64];        // turns per position of channel pair x, times 2^64
-  // of the launcher: blocks of each kind, blocks per page and KV heads of a key block,
+  // of append_plan: blocks of each kind, blocks per page and KV heads of a key block,
   // rows of a query block, first page block of each sequence
   int key_blocks, value_blocks, head_blocks, heads, q_rows;
   int block0[RK_MAX_BATCH_SEQS];
 };
-hipError_t launch_append(const PagedView& cache, const PagedTable& tab, AppendArgs a, const SeqTable& st,
-                         hipStream_t s);
+// Workgroups of the launch (meaningful plans have at most kMaxWorkgroups).
+int64_t append_plan(const PagedView& cache, const PagedTable& tab, const SeqTable& st, AppendArgs* a);
+hipError_t launch_append(const PagedView& cache, const PagedTable& tab, const AppendArgs& a, const SeqTable& st,
+                         int64_t workgroups, hipStream_t s);
 struct DecodeArgs {
   const void* q;
   void* out;

@@ -223,10 +223,15 @@ rk_status rk_paged_append(const rk_paged_cache* cache, const rk_paged_seqs* seqs
     }
     for (int x = 0; x < v.head_dim / 2; ++x) a.freq[x] = (uint64_t)(freq[x] * 0x1p64);   // below 2^62
   }
+  const int64_t blocks = append_plan(v, t, st, &a);
+  if (blocks > kMaxWorkgroups) {
+    set_error("%lld workgroups: more than the %lld of a launch", (long long)blocks, (long long)kMaxWorkgroups);
+    return RK_ERR_SHAPE;
+  }
   hipStream_t s = (hipStream_t)stream;
   if ((e = check_stream(s)) != RK_OK) return e;
   Timed timed("paged_append", s);
-  return hip_status("paged append", launch_append(v, t, a, st, s));
+  return hip_status("paged append", launch_append(v, t, a, st, blocks, s));
 }
 
 size_t rk_paged_workspace_size(const rk_paged_cache* cache, int32_t n_seqs, int32_t max_pages, int32_t n_heads,

@@ -1,8 +1,10 @@
-"""Outputs laid over the queries with other strides are refused before any device work (no GPU needed)."""
+"""Outputs laid over the queries with other strides, and calls of more workgroups than a launch takes, are refused before any
+device work (no GPU needed)."""
+import numpy as np
 import pytest
 
 import paper_2608_08684_amd as rk
-from test_paged_host import A, attention
+from test_paged_host import A, S, append, attention
 
 
 @pytest.mark.parametrize("status, kw", [
@@ -17,3 +19,20 @@ def test_outputs_over_the_queries_have_their_stride(status, kw):
 def test_a_single_sequence_has_no_stride():
     """One row over another: only the workspace is wrong here."""
     assert attention(seqs=dict(n_seqs=1), os_=264, size=0) == rk.RK_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("cache, seqs, rows", [
+    (dict(n_kv_heads=32, head_dim=128, dtype=rk.RK_F32), dict(n_seqs=1 << 23),
+     dict(q=None, q_out=None, k_row_stride=4096, k_head_stride=128, v_row_stride=4096, v_head_stride=128)),
+    (dict(), dict(n_seqs=1 << 23), dict()),
+    (dict(n_kv_heads=65536), dict(n_seqs=1 << 14), dict(q=None, q_out=None)),
+])
+def test_appends_of_too_many_workgroups(cache, seqs, rows):
+    assert append(cache=cache, seqs=seqs, rows=rows) == S and b"workgroups" in rk.load().rk_last_error()
+
+
+def test_prompts_of_too_many_workgroups():
+    offs = np.asarray([0, 1 << 30], np.int64)
+    assert append(seqs=dict(n_seqs=1, max_pages=1 << 26, page_stride=1 << 26),
+                  rows=dict(offsets=offs.ctypes.data, q=None, q_out=None)) == S
+    assert b"workgroups" in rk.load().rk_last_error()
