@@ -620,7 +620,8 @@ size_t rk_token_logprobs_workspace_size(int64_t n_rows, int32_t vocab, rk_dtype 
  * logits: DEVICE, fp32 or bf16, row r at logits + r * row_stride elements, any
  * alignment of the type.  tokens: DEVICE int32 [n_rows]; a token outside [0, vocab)
  * (a padded row) has logprob 0 and rank 0.  Outputs may be NULL (logprob and rank
- * without tokens must be).  vocab <= 2^22, 0 <= n_top <= min(vocab, RK_MAX_TOP).
+ * without tokens must be).  n_rows < 2^24, a row counted once for each 2^20 - 16
+ * bytes of logits begun; vocab <= 2^22, 0 <= n_top <= min(vocab, RK_MAX_TOP).
  * Entries of -inf have probability 0.  A row whose largest entry is not finite, or
  * with a NaN, has NaN logprob, entropy and top_logprobs; a NaN ranks as -inf.     */
 rk_status rk_token_logprobs(const void *logits, rk_dtype dtype, int64_t n_rows, int32_t vocab, int64_t row_stride,

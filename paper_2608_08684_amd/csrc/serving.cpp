@@ -269,9 +269,10 @@ struct LogprobPlan {
 
 static LogprobPlan logprob_plan(int64_t n_rows, int32_t vocab, rk_dtype dtype, int32_t n_top) {
   LogprobPlan p{};
-  if (n_rows < 0 || n_rows > kMaxGrid / 64 || vocab < 1 || vocab > kMaxVocab) return p;
+  if (n_rows < 0 || n_rows > kMaxWorkgroups || vocab < 1 || vocab > kMaxVocab) return p;
   if (n_top < 0 || n_top > RK_MAX_TOP || n_top > vocab || (dtype != RK_F32 && dtype != RK_BF16)) return p;
   logprob_parts(n_rows, vocab, dtype == RK_BF16, &p.parts, &p.part_logits);
+  if (n_rows * p.parts > kMaxWorkgroups) return p;
   const size_t parts = p.parts > 1 ? (size_t)n_rows * p.parts : 0;
   p.top = align256(parts * sizeof(float4));
   p.total = std::max<size_t>(256, p.top + align256(parts * n_top * 8));
@@ -292,7 +293,8 @@ rk_status rk_token_logprobs(const void *logits, rk_dtype dtype, int64_t n_rows, 
   if (dtype != RK_F32 && dtype != RK_BF16) return bad(RK_ERR_ARG, "unknown dtype");
   const LogprobPlan p = logprob_plan(n_rows, vocab, dtype, n_top);
   if (p.total == 0) {
-    set_error("n_rows must be in [0, 2^25), vocab in [1, 2^22], n_top in [0, min(vocab, %d)]", RK_MAX_TOP);
+    set_error("n_rows (times the parts of a long row) must be in [0, 2^24), vocab in [1, 2^22], n_top in [0, min(vocab, %d)]",
+              RK_MAX_TOP);
     return RK_ERR_ARG;
   }
   if (row_stride < vocab) return bad(RK_ERR_ARG, "row_stride below vocab");

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 import paper_2608_08684_amd as rk
-from test_paged_host import A, S, append, attention
+from test_paged_host import A, S, append, attention, logprobs
 
 
 @pytest.mark.parametrize("status, kw", [
@@ -36,3 +36,18 @@ def test_prompts_of_too_many_workgroups():
     assert append(seqs=dict(n_seqs=1, max_pages=1 << 26, page_stride=1 << 26),
                   rows=dict(offsets=offs.ctypes.data, q=None, q_out=None)) == S
     assert b"workgroups" in rk.load().rk_last_error()
+
+
+@pytest.mark.parametrize("rows, vocab", [(1 << 24, 10), ((1 << 24) + 1, 2), (1 << 24, 1 << 22), (1 << 22, 1 << 22)])
+def test_log_probabilities_of_too_many_rows(rows, vocab):
+    for dtype in (rk.RK_F32, rk.RK_BF16):
+        if (rows, vocab, dtype) == (1 << 22, 1 << 22, rk.RK_BF16):
+            rows *= 2
+        assert logprobs(rows=rows, vocab=vocab, stride=vocab, dtype=dtype, size=1 << 60) == A
+        assert b"n_rows" in rk.load().rk_last_error()
+        assert rk.load().rk_token_logprobs_workspace_size(rows, vocab, dtype, 0) == 0
+
+
+def test_log_probabilities_of_the_most_rows():
+    assert rk.token_logprobs_workspace_size((1 << 24) - 1, 10) > 0
+    assert logprobs(rows=(1 << 24) - 1, vocab=10, stride=10, size=0) == rk.RK_ERR_WORKSPACE
