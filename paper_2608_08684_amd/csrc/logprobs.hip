@@ -5,10 +5,11 @@
 //   log p_tok = (x_tok - c) - log S,   H = log S - T / S
 //   rank = 1 + #{v : x_v > x_tok, or x_v = x_tok and v < tok}
 //
-// The sums lose nothing with c below the maximum as long as nothing overflows, so c
-// follows a thread's maximum when that has run 32 ahead, and at the end (log S keeps
-// its digits next to 0).  The difference is formed before the factor log2(e) of the
-// exponential: x log2(e) would overflow at the type's lowest value, a common mask.
+// c is a thread's largest logit so far, moved up before a pass of four vectors is added.  S
+// would lose nothing with c below it, but T, moved up by D at the end, would be left as the
+// small difference of D S and T (the entropy 2e-6 off with D = 20).  The difference x - c is
+// formed before the factor log2(e) of the exponential: x log2(e) would overflow at the type's
+// lowest value, a common mask.
 //
 // A workgroup reads each logit of a row (of a part of a long row, where rows are few)
 // once: a running (c, S, T) per thread, joined in a fixed order.  The alternatives come
@@ -64,8 +65,6 @@ template <> struct Logit<bf16_t> {
     }
   }
 };
-
-constexpr float kLazy = 32.f;
 
 // Softmax sums relative to e^c; s and t are 0 while c is -inf.
 struct Sums {
@@ -390,7 +389,7 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
   const int bits = __float_as_int(xt);
   const float below = xt == 0.f ? __int_as_float((int)0x80000001) : __int_as_float(bits < 0 ? bits + 1 : bits - 1);
   Sums q{-INFINITY, 0.f, 0.f};
-  float largest = -INFINITY, c = 0.f;   // c: q.ref()
+  float c = 0.f;                        // q.ref()
   int count = 0;                        // wave-uniform
   uint32_t best_key = 0;
   const auto load = [&](v4u* raw, int b) {
@@ -408,7 +407,18 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
   for (int b0 = 0; b0 < x.n_vec; b0 += NT * U) {   // the first vector of U passes
     const int b = b0 + w * 64;                     // .. of this wave's
     if (b0 + NT * U < x.n_vec) load(next, b + NT * U);
-    float best = -INFINITY;
+    float best = -INFINITY;               // what is outside the row is -inf
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float f[N];
+      Logit<T>::get(raw[u], f);
+#pragma unroll
+      for (int e = 0; e < N; ++e) best = fmaxf(best, f[e]);
+    }
+    if (best > q.c) {
+      q.raise(best);
+      c = q.ref();
+    }
     // these passes' own sums: chains of 16 or 32 terms, then one of the passes (a chain of a
     // thread's 500 terms left the entropy 2e-6 off)
     float s = 0.f, t = 0.f;
@@ -418,17 +428,6 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
       if (vb >= x.n_vec) break;
       float f[N];
       Logit<T>::get(raw[u], f);
-      float vm = f[0];
-#pragma unroll
-      for (int e = 1; e < N; ++e) vm = fmaxf(vm, f[e]);
-      best = fmaxf(best, vm);
-      if (vm > q.c + kLazy) {
-        q.s += s;
-        q.t += t;
-        s = t = 0.f;
-        q.raise(vm);
-        c = q.ref();
-      }
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         const float d = f[e] - c, p = __builtin_amdgcn_exp2f(d * kLog2e);
@@ -452,7 +451,6 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
     }
     q.s += s;
     q.t += t;
-    largest = fmaxf(largest, best);
     if constexpr (TOP) {
       // a group holds logits if its first vector does
       uint32_t key = quad_max(order_bits(best));
@@ -463,7 +461,6 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
 #pragma unroll
     for (int u = 0; u < U; ++u) raw[u] = next[u];
   }
-  if (largest > q.c) q.raise(largest);
   q = wave_sums(q);
   if (lane == 0) { sums[w] = q; counts[w] = count; }
   if constexpr (TOP) {
