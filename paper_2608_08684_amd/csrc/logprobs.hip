@@ -20,11 +20,16 @@
 // is the n-th largest of the groups' largest logits: the logits above it come from the
 // groups above it, and the rest are the first logits of the row that equal it.
 //
-// Bound: memory for many fp32 rows, arithmetic for bf16 ones (98 issue slots for 8 logits,
-// 32 of them the exponentials'), the chain of dependent steps for few.  With the 20 best:
-// 1024 rows of 128256 fp32 100 us (5.2 TB/s, a copy of as many bytes 106), 1500 of 128256
-// bf16 90 us (4.3 TB/s), 301 of 50257 bf16 18.6 us (45 of 256 CUs have two rows; 22.7 with
-// rows in two parts), 16 of 32000 fp32 9.7 us.
+// The exponentials' arguments carry the rounding of their product with log2(e): results are
+// 6e-8 .. 1e-7 off on a language model's logits, as far as fp32 sums are; making it good would
+// take 4 more instructions a logit.
+//
+// Bound: memory for many fp32 rows, a chain of short sections for few.  With the 20 best: 1024
+// rows of 128256 fp32 101 us (5.2 TB/s, a copy of as many bytes 106), 1500 of 128256 bf16 93
+// (4.1 TB/s).  301 of 50257 bf16 20.4 us in a graph: 4.7 for a launch and the joins (a row of
+// 500), 8.8 for S and T, 2.2 for the rank, 4.7 for the 20 best; the vector units are busy 6.7
+// of them in the mean, 11 on the 45 of 256 CUs that have two rows.  16 of 32000 fp32, 5 best,
+// 10.0: 4.1, 1.7, 1.1 and 3.1.
 #include <math.h>
 
 #include <algorithm>
@@ -521,8 +526,8 @@ void logprob_parts(int64_t n_rows, int vocab, bool bf16, int* parts, int* part_l
 }
 
 // Threads per row: the widest workgroups for few rows, so that every CU of 256 has 16
-// waves with four loads each in flight (301 rows of 50257 bf16: 18.6 us with 512 threads,
-// 22.9 with 1024, 23.6 with 256).
+// waves with four loads each in flight (301 rows of 50257 bf16: 20.4 us with 512 threads,
+// 24.8 with 1024, 24.3 with 256; in two parts a row 23.8).
 hipError_t launch_logprobs(const LogprobArgs& a, bool bf16, hipStream_t s) {
   if (a.n_rows <= 0) return hipSuccess;
   const int64_t blocks = a.n_rows * a.parts;

@@ -85,15 +85,16 @@ __device__ __forceinline__ int max_i(int a, int b) { return a > b ? a : b; }
 //   y[x]         = k[x] cos a - k[x + d/2] sin a
 //   y[x + d/2]   = k[x + d/2] cos a + k[x] sin a,   a = pos theta^(-2x/d).
 // The angle is a fraction of a turn in 32 bits, the upper half of pos times theta^(-2x/d)
-// / (2 pi) in 64 fixed-point bits: whole turns drop out exactly, and 2^-32 of a turn is
-// right for any 32-bit position (fp32 would leave a position of 10^6 four digits).  Its
-// sine and cosine are fp32.
+// / (2 pi) in 64 fixed-point bits: whole turns drop out exactly (fp32 would leave a position
+// of 10^6 four digits).  The frequency comes from doubles, 53 bits, so the angle is off by
+// 2^-24 of a turn at a position of 2^31 and in proportion less below, then by its rounding to
+// fp32 for sine and cosine, at most 2^-26 of a turn.
 // Three kinds of workgroups: keys of all new rows of a page for some KV heads, whose
 // bounds so take them in a fixed order without atomics; values of 16 entries; queries
 // of up to 8 rows.  The first loads go out before the angles are formed.
-// Bound: memory (each value read once, written once); 28112 rows, 32 / 8 heads of 128:
-// 92 us (4.8 TB/s), a copy of as many bytes 89.  A step's rows (64 sequences): the latency
-// of one pass, 6 us.
+// Bound: memory (each value read once, written once); 17928 rows, 32 / 8 heads of 128:
+// 92 us (4.8 TB/s), a copy of as many bytes 89; 12 fp32 heads of 64: 72 us (4.6).  A step's
+// rows (64 sequences): the latency of one pass, 6 us.
 constexpr int kAppendThreads = 256, kAppendRows = 16, kAppendQueryRows = 8;
 
 // cosine and sine of channel pair x at position pos
@@ -721,8 +722,8 @@ __global__ __launch_bounds__(kSelectThreads) void page_select_kernel(PagedView c
 // Entries on pages outside the cache and entries past the length weigh nothing; their
 // scores are replaced by -inf and their values by 0, whatever memory holds there.
 // Bound: memory.  8 KV heads of 128, 32 query heads, with the join: 64 sequences of 4096
-// 195 us (5.5 TB/s, a plain read of as much 6), 32 of 100 .. 8192 113 us (5.2), 2 of up to
-// 32768 55 us (4.6: the join and the first tile's way, lengths to pages to keys, are 9 of
+// 191 us (5.6 TB/s, a plain read of as much 6), 32 of 100 .. 8192 112 us (5.3), 2 of up to
+// 32768 50 us (5.1: the join and the first tile's way, lengths to pages to keys, are 9 of
 // them).  8 waves a workgroup, three workgroups per CU, equal runs of tiles for every
 // workgroup whatever the sequences' lengths: all slower or the same.
 constexpr int kDecodeWaves = 4, kTile = 32;
@@ -1156,15 +1157,17 @@ __global__ __launch_bounds__(256) void decode_join_kernel(PagedTable tab, Decode
 // gains where rows leave CUs idle or, being of unequal length, end at different times.  us
 // for 8 KV heads of 128 in bf16, all of that length | lengths from 100 up to it:
 //   up to 512 one part: a workgroup's 512 entries take as long as the join (1 row of 8 heads
-//     9.0, two parts 9.9; 256 rows 14.5 | 12.0 and 19.7 | 17.1);
+//     9.0, two parts 9.9; 256 rows 14.5 | 12.0 and 19.6 | 17.0);
 //   up to 1024 for 256 workgroups, but one part from 96 rows on (128 rows 15.2 | 14.7, two
-//     parts 17.9 | 15.3; 32 rows 14.3 | 14.0, four 11.3 | 10.8);
-//   below 4096 for 256, one to a CU (64 rows of 2048: 4 parts 18.0 | 14.8, 8 20.0 | 17.7;
-//     256 rows: 1 part 51.5 | 36.2, 4 58.2 | 40.9), but two where one would leave some CUs two
-//     rows and the others one (288 rows of 64 channels: 39.9 | 24.7, two parts 37.8 | 22.2);
+//     parts 18.0 | 15.3; 32 rows 14.4 | 14.2, four 11.4 | 11.1);
+//   below 4096 for 256, one to a CU (64 rows of 2048: 4 parts 18.0 | 14.6, 8 19.8 | 17.5;
+//     256 rows: 1 part 49.4 | 35.0, 4 58.1 | 41.0), but two where one would leave some CUs two
+//     rows and the others one (288 rows of 64 channels: 40.0 | 25.0, two parts 38.5 | 22.5);
 //   from 4096 for 256, and four as long as that is no more than 1280 workgroups: unequal
-//     lengths cost more than the join (8192, 256 rows: 1 part 187 | 125, 4 191 | 108, 512
-//     rows 365 | 235, 2 parts 372 | 197; 32 rows: 8 parts 32.6 | 21.4, 32 35.7 | 27.6).
+//     lengths cost more than the join (8192, 256 rows: 1 part 188 | 120, 4 195 | 106, 512
+//     rows 367 | 227, 2 parts 379 | 195; 32 rows: 8 parts 32.7 | 21.1, 32 36.0 | 26.3).
+// The longest that a sequence may be is the width of its table: see the price of a table
+// with room at launch_decode.
 int decode_parts(int n_seqs, int n_heads, int n_kv, int64_t max_entries) {
   const int64_t rows = (int64_t)n_seqs * n_kv * ((n_heads / n_kv + 15) / 16);
   int64_t want = 256 / rows;
@@ -1174,12 +1177,17 @@ int decode_parts(int n_seqs, int n_heads, int n_kv, int64_t max_entries) {
   return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, max_entries / 256), kMaxDecodeParts));
 }
 
+// The lengths lie on the device, so everything here goes by the table's width.  With 4 and 16
+// times the width that the sequences need: 4 sequences of 300, 8 KV heads of 128: 7.9 us, then
+// 9.5 and 10.4; 64 of 100 .. 300: 15.4, 15.3, 27.1; 16 of 1500 .. 2048, 12 heads of 64: 18.5,
+// 22.1, 21.8; 2 of up to 32768: 48, 49, 47.  Selected pages: 8 of 2048, 26 pages of 16: 14.6,
+// 16.3, 20.4; 4 of up to 32768, 64 pages of 64: 31, 38, 53 (the choice in a launch of its own).
 hipError_t launch_decode(const PagedView& cache, const PagedTable& tab, DecodeArgs a, hipStream_t s) {
   const int64_t blocks =
       (int64_t)tab.n_seqs * cache.n_kv * ((a.n_heads / cache.n_kv + 15) / 16) * a.n_parts;
   // more workgroups than run at a time: the longest sequences' first, so that the last to
-  // start are short (32 sequences of 100 .. 8192 entries, 8 KV heads: 128 -> 117 us; equal
-  // lengths pay 1 %, 16 short fp32 sequences 43 -> 46 us; 64 lanes know 64 sequences)
+  // start are short (32 sequences of 100 .. 8192 entries, 8 KV heads: 118 -> 109 us; 64 equal
+  // ones 188 -> 191; more than 64 are taken in their order, a wave has 64 lanes to know them)
   a.longest_first = blocks > 512 && tab.n_seqs <= 64 && !tab.per_head;
 #define RK_DECODE(T, DH)                                                                                           \
   do {                                                                                                             \
@@ -1194,10 +1202,10 @@ hipError_t launch_decode(const PagedView& cache, const PagedTable& tab, DecodeAr
 
 // Bounds of a row up to which the attention's workgroups score the pages themselves: a CU
 // reads them in less time than another launch takes.  8 sequences of 2048 in pages of 16,
-// 12 heads of 64, 32 KB of bounds a row: 13.9 us, with the scores in a launch of their own
-// 14.5; half as many pages 9.2 and 11.0; twice as many, 64 KB, 20.0 and 17.3.  Not where more
+// 12 heads of 64, 32 KB of bounds a row: 14.6 us, with the scores in a launch of their own
+// 15.0; half as many pages 12.1 and 14.0; twice as many, 64 KB, 18.9 and 16.7.  Not where more
 // than two parts of a row outnumber the places that 256 CUs have for them: 32 sequences of
-// 16384 in pages of 256, 16 of them read, 8 KV heads of 128, 4 parts: 117 and 110.  Nor
+// 16384 in pages of 256, 16 of them read, 8 KV heads of 128, 4 parts: 117 and 112.  Nor
 // where more than 16 query heads share a KV head: they would be scored by several
 // workgroups, one of which may have written its outputs over the queries that another
 // still reads.
