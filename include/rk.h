@@ -60,7 +60,10 @@ typedef enum {
                                produced for another model, batch or window start   */
 } rk_status;
 
-typedef enum { RK_F32 = 0, RK_BF16 = 1 } rk_dtype;
+typedef enum { RK_F32 = 0, RK_BF16 = 1,
+               RK_E4M3 = 2               /* 8 bits (4 exponent and 3 mantissa bits, largest
+                                            448, no infinity): paged caches only           */
+} rk_dtype;
 
 typedef enum {
   RK_ROUND_LARGEST_REMAINDER = 0,  /* keeps sum(b) = B exactly (default reading)  */
@@ -494,19 +497,30 @@ rk_status rk_spearman(const double *x, const double *y, int32_t n, double *rho);
  * rk_paged_cache is one layer's; the layers of a model may share one pool of pages.
  *   k, v:       DEVICE [n_pages, n_kv_heads, page_size, head_dim] in dtype, the
  *               rotated Keys and the Values;
- *   key_bounds: DEVICE [n_pages, n_kv_heads, 2, head_dim] in dtype, or NULL: for
+ *   key_bounds: DEVICE [n_pages, n_kv_heads, 2, head_dim] in dtype (bf16 for RK_E4M3), or NULL: for
  *               each page, KV head and channel the least and the largest value over
  *               the Keys written to the page since its entry 0 was last written (both
  *               NaN where one of those is).
  *               rk_paged_append keeps them, rk_paged_attention_selected reads them.
  * page_size: a power of two, 16 .. 256.  head_dim: as in rk_model_config.  All
- * buffers 16-byte aligned.                                                        */
+ * buffers 16-byte aligned.
+ * RK_E4M3: k and v hold 8-bit values and each row (one entry of one KV head) has a scale,
+ * a power of two; head_dim as for RK_BF16, and what goes in and out (new rows, queries,
+ * outputs, key_bounds) is bf16.
+ *   k_scales, v_scales: DEVICE uint8 [n_pages, n_kv_heads, page_size]; byte b stands for
+ *               2^(b - 127), 1 <= b <= 254.  NULL (unused) for the other types.
+ * rk_paged_append rounds a row's rotated Key, and its Value, once to nearest even, in units
+ * of the least power of two, 2^-117 at least, of which its largest finite magnitude is at
+ * most 448.  Infinities and NaN become NaN, what would round to 2^128 becomes 1.875 2^127.
+ * The values that are left are bf16 numbers, and every call that reads the cache does so as
+ * if it held those.                                                                */
 typedef struct {
   void *k, *v;
   void *key_bounds;
   int64_t n_pages;
   int32_t page_size, n_kv_heads, head_dim;
   rk_dtype dtype;
+  uint8_t *k_scales, *v_scales;
 } rk_paged_cache;
 
 /* The sequences of a call.
@@ -530,7 +544,7 @@ typedef struct {
 /* New rows.  offsets: HOST int64 [n_seqs + 1] as in rk_batch (sequence i brings rows
  * offsets[i] .. offsets[i + 1] - 1, any number of them; n_seqs <=
  * RK_MAX_BATCH_SEQS), or NULL: one row per sequence, row i to sequence i, n_seqs <= 2^23.
- *   k, v:      DEVICE, dtype of the cache, row r of KV head g at k + r *
+ *   k, v:      DEVICE, dtype of the cache (bf16 for RK_E4M3), row r of KV head g at k + r *
  *              k_row_stride + g * k_head_stride (elements), head_dim contiguous
  *              values; 16-byte aligned, strides whole 16-byte pieces.  The columns
  *              of a fused q|k|v row and the blocks of rk_snapkv_compress both fit.
@@ -562,6 +576,16 @@ typedef struct {
 rk_status rk_paged_append(const rk_paged_cache *cache, const rk_paged_seqs *seqs, const rk_paged_rows *rows,
                           void *stream);
 
+/* Rows back out of the cache, the inverse of rk_paged_append without its rotation: sequence
+ * i's rows offsets[i] .. offsets[i + 1] - 1 (m_i of them; offsets NULL: one row each) are
+ * its entries lengths[i] - m_i .. lengths[i] - 1.  offsets, row and head strides as in
+ * rk_paged_rows; k_out, v_out in the cache's dtype (bf16 for RK_E4M3), overlapping neither
+ * each other nor the cache.  Either may be NULL.  Entries that are negative or lie on no
+ * page are read as 0.                                                             */
+rk_status rk_paged_read(const rk_paged_cache *cache, const rk_paged_seqs *seqs, const int64_t *offsets, void *k_out,
+                        int64_t k_row_stride, int64_t k_head_stride, void *v_out, int64_t v_row_stride,
+                        int64_t v_head_stride, void *stream);
+
 /* Workspace bytes of rk_paged_attention (n_select = 0) or of both it and
  * rk_paged_attention_selected with that many pages, for up to n_seqs sequences and
  * max_pages pages; 0 for invalid arguments.                                      */
@@ -571,8 +595,8 @@ size_t rk_paged_workspace_size(const rk_paged_cache *cache, int32_t n_seqs, int3
 /* Attention of one new token of each sequence over its cache:
  *   out_i,h = sum_u softmax_u(scale q_i,h . k_u) v_u,  u < lengths[i],
  * query head h reading KV head h / (n_heads / n_kv_heads).
- *   q, out: DEVICE, dtype of the cache, sequence i at q + i * q_row_stride elements,
- *           n_heads contiguous heads; 16-byte aligned rows.  out may be q itself with
+ *   q, out: DEVICE, dtype of the cache (bf16 for RK_E4M3), sequence i at q + i *
+ *           q_row_stride elements, n_heads contiguous heads; 16-byte aligned rows.  out may be q itself with
  *           its stride, and overlaps nothing else that the call reads.
  *   scale:  0 for 1 / sqrt(head_dim).
  *   lse:    DEVICE fp32 [n_seqs, n_heads] or NULL: log sum_u e^(scale q . k_u).
@@ -602,6 +626,89 @@ rk_status rk_paged_attention_selected(const rk_paged_cache *cache, const rk_page
                                       const rk_page_selection *selection, const void *q, int64_t q_row_stride,
                                       int32_t n_heads, float scale, void *out, int64_t out_row_stride, float *lse,
                                       void *workspace, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------- drafted tokens */
+
+/* Most drafted rows of one sequence. */
+#define RK_MAX_DRAFTS 64
+
+/* Workspace bytes of rk_paged_attention_tree for up to n_seqs sequences, n_rows rows and
+ * max_pages pages; 0 for invalid arguments.                                       */
+size_t rk_paged_tree_workspace_size(const rk_paged_cache *cache, int32_t n_seqs, int64_t n_rows, int32_t max_pages,
+                                    int32_t n_heads);
+
+/* Attention of a tree of drafted tokens of each sequence over its cache, all drafts of a
+ * sequence in one pass.  Its m_i = offsets[i + 1] - offsets[i] drafts are its last entries,
+ * appended like other rows: row r = offsets[i] + j is entry b + j, b = lengths[i] - m_i, and
+ *   out_r,h = sum_u softmax_u(scale q_r,h . k_u) v_u   over the entries u < b of the text
+ *             and the drafts u = b + t with bit t of masks[r] set.
+ *   offsets: HOST int64 [n_seqs + 1] from 0; n_seqs <= RK_MAX_BATCH_SEQS, m_i in [0, RK_MAX_DRAFTS].
+ *   masks:   DEVICE uint64 [rows], for a tree a row's ancestors and itself; any bits may be
+ *            set, those from m_i on mean nothing.  NULL: the drafts are a chain, row j sees
+ *            the drafts 0 .. j.
+ *   q, out, scale, lse [rows, n_heads]: as for rk_paged_attention, a row for each draft.
+ * A row that sees nothing gets zeros and a log-sum-exp of -inf; what is said of infinite and
+ * NaN Values, tables and lengths there holds here (weights below e^-50 may count as 0).   */
+rk_status rk_paged_attention_tree(const rk_paged_cache *cache, const rk_paged_seqs *seqs, const int64_t *offsets,
+                                  const uint64_t *masks, const void *q, int64_t q_row_stride, int32_t n_heads,
+                                  float scale, void *out, int64_t out_row_stride, float *lse, void *workspace,
+                                  size_t ws_bytes, void *stream);
+
+/* The accepted drafts to where the sequence goes on: of sequence i's drafts (entries b .. b +
+ * m_i - 1 as above) those of its path move to the entries b, b + 1, .. in order, in the cache
+ * of one layer.  lengths are those of before; the caller then sets lengths[i] to b plus the
+ * length of the path.
+ *   kept: DEVICE int32, row i at kept + i * kept_stride, n_kept of them (1 .. RK_MAX_DRAFTS):
+ *         the drafts of the path, increasing; the first that is negative, not below m_i or
+ *         not above the one before it ends the path.
+ * Entries that are negative or lie on no page are not moved.  The key bounds of a page take
+ * in the Keys that are moved to it (or stay where they are on the path), and begin anew with
+ * them where the path reaches the page's entry 0.                                   */
+rk_status rk_paged_keep(const rk_paged_cache *cache, const rk_paged_seqs *seqs, const int64_t *offsets,
+                        const int32_t *kept, int64_t kept_stride, int32_t n_kept, void *stream);
+
+/* ---------------------------------------------------------------- beams */
+
+/* Most beams of a group. */
+#define RK_MAX_BEAMS 32
+
+/* Workspace bytes of rk_beam_select for up to n_groups groups; 0 for invalid arguments. */
+size_t rk_beam_select_workspace_size(int32_t n_groups, int32_t n_beams, int32_t vocab, rk_dtype dtype, int32_t n_out);
+
+/* The best continuations of each group's beams: of the candidates (beam b, token v)
+ *   score = scores[b] + x_b,v - logsumexp(x_b)
+ * the n_out best, falling.  A beam that has ended has one candidate, end_token with the score
+ * scores[b].  A candidate without a score above -inf (a masked logit, a beam whose score is
+ * -inf or NaN, a row without a finite largest logit or with a NaN) is none; where there are
+ * fewer than n_out the rest is parent -1, token -1, score -inf.
+ *   logits:  DEVICE, fp32 or bf16, row group * n_beams + b as in rk_token_logprobs; those of
+ *            ended beams and of beams without a score are not read.
+ *   scores:  DEVICE fp32 [n_groups, n_beams]; ended: DEVICE uint8 [n_groups, n_beams] (0: goes
+ *            on) or NULL.
+ *   parents (the beam, within the group), tokens, scores_out: DEVICE [n_groups, n_out], int32,
+ *            int32 and fp32; scores_out may be scores where n_out = n_beams.
+ * Between beams the scores are compared in double precision, ties to the lower beam; within a
+ * beam the logits, ties to the lower token.  n_beams <= RK_MAX_BEAMS, 1 <= n_out <=
+ * RK_MAX_TOP; rows and vocab as for rk_token_logprobs.                               */
+rk_status rk_beam_select(const void *logits, rk_dtype dtype, int32_t n_groups, int32_t n_beams, int32_t vocab,
+                         int64_t row_stride, const float *scores, const uint8_t *ended, int32_t end_token,
+                         int32_t n_out, int32_t *parents, int32_t *tokens, float *scores_out, void *workspace,
+                         size_t ws_bytes, void *stream);
+
+/* The beams' caches after a selection: sequence i = group * n_beams + b goes on from sequence
+ * p = group * n_beams + parents[i] (itself where parents[i] is outside [0, n_beams)).  All
+ * sequences of a group have the length of its first, T; with f = T / page_size whole pages
+ *   pages_out[i][x] = pages[p][x] for x < f (they are shared, never written again), and
+ *   pages[i][x] from there on: the sequence's own,
+ * and the T % page_size entries of p's page in progress, pages[p][f], with its key bounds, are
+ * copied to pages[i][f].  A page of number f of a group may be in no other row of the call.
+ *   parents:   DEVICE int32 [n_seqs]; n_seqs a multiple of n_beams.
+ *   pages_out: DEVICE int32, row i at pages_out + i * pages_out_stride, max_pages of them, or NULL
+ *              (entries only: layers that share a table, all but the last of them).  The same
+ *              address as seqs->pages with its stride: in place; otherwise apart from it.
+ * The group's parents 0 fork a prompt that its first sequence holds.                  */
+rk_status rk_paged_reorder(const rk_paged_cache *cache, const rk_paged_seqs *seqs, int32_t n_beams,
+                           const int32_t *parents, int32_t *pages_out, int64_t pages_out_stride, void *stream);
 
 /* ---------------------------------------------------------------- token log probabilities */
 
@@ -635,6 +742,7 @@ rk_status rk_token_logprobs(const void *logits, rk_dtype dtype, int64_t n_rows, 
  * (families: "rmsnorm", "gemm_qkv", "noise", "attention", "gemm_o",
  * "gemm_gate_up", "gemm_down", "lm_lse", "lm_kl", "kl_logits", "lm_logits",
  * "local", "snap_scores", "snap_select", "paged_append", "paged_attention",
+ * "paged_read", "paged_tree", "paged_keep", "paged_reorder", "beam_select",
  * "token_logprobs").
  * rk_timing_end waits for the recorded events, returns the number of launches
  * and their summed duration in milliseconds, and stops recording.  Host-side

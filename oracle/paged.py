@@ -1,4 +1,4 @@
-"""Paged key-value cache and token log probabilities in float64, position by position.
+"""Paged key-value cache, token log probabilities and beams in float64, position by position.
 
 Written from the definitions of ``include/rk.h``; shares nothing with the library.
 """
@@ -8,7 +8,8 @@ import math
 
 import numpy as np
 
-__all__ = ["rotate", "entries", "append_rows", "attend", "page_scores", "choose_pages", "logprobs"]
+__all__ = ["rotate", "entries", "append_rows", "attend", "page_scores", "choose_pages", "logprobs", "e4m3", "visible",
+           "kept_moves", "reordered", "beam_select"]
 
 
 def rotate(x, position, theta):
@@ -89,3 +90,75 @@ def logprobs(x, token, n_top):
     has = token is not None and 0 <= token < len(x)
     return (logp[token] if has else 0.0, 1 + order.index(token) if has else 0, entropy, order[:n_top],
             logp[order[:n_top]])
+
+
+def _round_e4m3(y):
+    """The nearest of the 8-bit values, ties to the even one; |y| at most 448."""
+    if y == 0 or y != y:
+        return y
+    step = 2.0 ** (max(math.frexp(y)[1], -5) - 4)      # 4 significant bits, whole steps of 2^-9 below 2^-6
+    return round(y / step) * step                        # Python rounds halves to even
+
+
+def e4m3(row):
+    """(values in units of the scale, scale byte) of one row: the least power of two, 2^-117 at least, of which the
+    largest finite magnitude is at most 448; infinities and NaN are NaN, what would round to 2^128 stays below."""
+    row = np.asarray(row, np.float64)
+    finite = np.isfinite(row)
+    top = float(np.abs(row[finite]).max()) if finite.any() else 0.0
+    e = -117
+    while top > 448.0 * 2.0 ** e:
+        e += 1
+    most = 240.0 if e == 120 else 448.0
+    return [_round_e4m3(min(max(x / 2.0 ** e, -most), most)) if f else math.nan for x, f in zip(row, finite)], e + 127
+
+
+def visible(length, m, mask, n_entries):
+    """Entries (below n_entries) that a draft of the last m sees; mask None: all."""
+    b = int(length) - m
+    return [u for u in range(max(0, min(int(length), n_entries))) if u < b or mask is None or mask >> (u - b) & 1]
+
+
+def kept_moves(length, m, kept):
+    """(new entry, old entry) of the path of a sequence's drafts."""
+    b, moves, last = int(length) - m, [], -1
+    for j, t in enumerate(kept):
+        if not last < t < m:
+            break
+        moves.append((b + j, b + int(t)))
+        last = t
+    return moves
+
+
+def reordered(pages, lengths, parents, n_beams, page_size):
+    """(new table, [(page, source page, entries)]) of the sequences after a selection."""
+    new, copies = [list(map(int, row)) for row in pages], []
+    for i, p in enumerate(parents):
+        first = i // n_beams * n_beams
+        src = first + p if 0 <= p < n_beams else i
+        length = max(0, min(int(lengths[first]), len(pages[i]) * page_size))
+        full, rest = length // page_size, length % page_size
+        new[i][:full] = [int(x) for x in pages[src][:full]]
+        if rest and src != i:
+            copies.append((int(pages[i][full]), int(pages[src][full]), rest))
+    return new, copies
+
+
+def beam_select(logits, scores, ended, end_token, n_out):
+    """(parent, token, score) of the n_out best candidates of a group's beams."""
+    found = []
+    for b, (x, s) in enumerate(zip(logits, scores)):
+        if not s > -math.inf:
+            continue
+        if ended is not None and ended[b]:
+            found.append((-float(s), b, 0.0, end_token))
+            continue
+        x = np.asarray(x, np.float64)
+        m = x.max() if not np.isnan(x).any() else math.nan
+        if not math.isfinite(m):
+            continue
+        logp = (x - m) - math.log(np.sum(np.exp(x - m)))
+        best = [int(v) for v in np.argsort(-x, kind="stable")[:n_out]]
+        found += [(-(float(s) + logp[v]), b, -x[v], v) for v in best if x[v] > -math.inf]
+    found = sorted(found)[:n_out]
+    return [(b, v, -s) for s, b, _, v in found] + [(-1, -1, -math.inf)] * (n_out - len(found))

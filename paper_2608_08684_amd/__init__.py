@@ -28,12 +28,13 @@ import numpy as np
 __all__ = ["RKError", "load", "Model", "Batch", "layer_budgets", "timing_begin", "timing_end", "LIB_PATH", "RK_FLAG_FULL_RECOMPUTE",
            "RK_FLAG_UNFUSED_KL", "RK_FLAG_CACHED_WINDOW", "RK_FLAG_GRAPH", "RK_FLAG_LOCAL_SIGNAL", "RK_FLAG_CHECK_STATE", "RK_WS_CLEAN_STATE", "RK_MAX_BATCH_SEQS", "RK_MAX_GROUP",
            "RK_POOL_MAX", "RK_POOL_AVG", "RK_SNAPKV_MAX_PREFIX", "RK_STATIC_SCRATCH_BYTES", "snapkv_layout", "spearman",
-           "PagedCache", "PagedSeqs", "token_logprobs", "token_logprobs_workspace_size", "RK_MAX_TOP"]
+           "PagedCache", "PagedSeqs", "token_logprobs", "token_logprobs_workspace_size", "RK_MAX_TOP",
+           "beam_select", "beam_select_workspace_size", "RK_MAX_BEAMS", "RK_MAX_DRAFTS"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "librk.so")
 
 RK_OK, RK_ERR_ARG, RK_ERR_SHAPE, RK_ERR_WORKSPACE, RK_ERR_HIP, RK_ERR_UNSUPPORTED, RK_ERR_STATE = 0, -1, -2, -3, -4, -5, -6
-RK_F32, RK_BF16 = 0, 1
+RK_F32, RK_BF16, RK_E4M3 = 0, 1, 2
 RK_ROUND_LARGEST_REMAINDER, RK_ROUND_NEAREST_EVEN = 0, 1
 RK_FLAG_FULL_RECOMPUTE = 0x1
 RK_FLAG_UNFUSED_KL = 0x2
@@ -48,7 +49,7 @@ RK_POOL_MAX = 0
 RK_POOL_AVG = 1
 RK_SNAPKV_MAX_PREFIX = 36864
 RK_STATIC_SCRATCH_BYTES = 128 << 20
-RK_MAX_TOP = 32
+RK_MAX_TOP, RK_MAX_BEAMS, RK_MAX_DRAFTS = 32, 32, 64
 
 _STATUS = {0: "RK_OK", -1: "RK_ERR_ARG", -2: "RK_ERR_SHAPE", -3: "RK_ERR_WORKSPACE", -4: "RK_ERR_HIP",
            -5: "RK_ERR_UNSUPPORTED", -6: "RK_ERR_STATE"}
@@ -93,7 +94,8 @@ class _SnapParams(ctypes.Structure):
 class _PagedCache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("key_bounds", ctypes.c_void_p),
                 ("n_pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
-                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int)]
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int), ("k_scales", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p)]
 
 
 class _PagedSeqs(ctypes.Structure):
@@ -172,6 +174,15 @@ def load() -> ctypes.CDLL:
         "rk_paged_attention_selected": (st, [ctypes.POINTER(_PagedCache), ctypes.POINTER(_PagedSeqs),
                                              ctypes.POINTER(_PageSelection), vp, i64, i32, f32, vp, i64, vp, vp, sz,
                                              vp]),
+        "rk_paged_read": (st, [ctypes.POINTER(_PagedCache), ctypes.POINTER(_PagedSeqs), vp, vp, i64, i64, vp, i64, i64,
+                               vp]),
+        "rk_paged_tree_workspace_size": (sz, [ctypes.POINTER(_PagedCache), i32, i64, i32, i32]),
+        "rk_paged_attention_tree": (st, [ctypes.POINTER(_PagedCache), ctypes.POINTER(_PagedSeqs), vp, vp, vp, i64, i32,
+                                         f32, vp, i64, vp, vp, sz, vp]),
+        "rk_paged_keep": (st, [ctypes.POINTER(_PagedCache), ctypes.POINTER(_PagedSeqs), vp, vp, i64, i32, vp]),
+        "rk_paged_reorder": (st, [ctypes.POINTER(_PagedCache), ctypes.POINTER(_PagedSeqs), i32, vp, vp, i64, vp]),
+        "rk_beam_select_workspace_size": (sz, [i32, i32, i32, st, i32]),
+        "rk_beam_select": (st, [vp, st, i32, i32, i32, i64, vp, vp, i32, i32, vp, vp, vp, vp, sz, vp]),
         "rk_token_logprobs_workspace_size": (sz, [i64, i32, st, i32]),
         "rk_token_logprobs": (st, [vp, st, i64, i32, i64, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]),
     }
@@ -470,6 +481,14 @@ def _launch(dev: int, stream, fn, *args):
         _check(status)
 
 
+def _host_offsets(row_offsets, n_seqs: int):
+    """(int64 array, rows) of the host offsets of the sequences' rows."""
+    offsets = np.ascontiguousarray(np.asarray(row_offsets, dtype=np.int64))
+    if offsets.shape != (n_seqs + 1,):
+        raise ValueError(f"row_offsets: {n_seqs + 1} entries")
+    return offsets, int(offsets[-1])
+
+
 class PagedSeqs:
     """rk_paged_seqs.  ``pages``: int32 [n_seqs, max_pages] (rows may be strided); ``lengths``: int32 [n_seqs],
     entries of each sequence with the step's new rows counted.  Both stay the caller's and are read by the kernels:
@@ -493,20 +512,30 @@ class PagedSeqs:
 
 
 class PagedCache:
-    """rk_paged_cache over the caller's tensors: ``k``, ``v`` [n_pages, n_kv_heads, page_size, head_dim] in bfloat16 or
-    float32, ``key_bounds`` [n_pages, n_kv_heads, 2, head_dim] or None."""
+    """rk_paged_cache over the caller's tensors: ``k``, ``v`` [n_pages, n_kv_heads, page_size, head_dim] in bfloat16,
+    float32 or float8_e4m3fn, ``key_bounds`` [n_pages, n_kv_heads, 2, head_dim] or None.  A float8_e4m3fn cache has
+    ``k_scales``, ``v_scales`` uint8 [n_pages, n_kv_heads, page_size], and its bounds, rows, queries and outputs are
+    bfloat16 (``dtype`` is the type of those)."""
 
-    def __init__(self, k, v, key_bounds=None):
+    def __init__(self, k, v, key_bounds=None, k_scales=None, v_scales=None):
+        import torch
         self.device = dev = _need_cuda(k, "k")
         if k.dim() != 4:
             raise ValueError("k: [n_pages, n_kv_heads, page_size, head_dim]")
-        dtype = _dtype_id(k, "k")
+        scaled = k.dtype is torch.float8_e4m3fn
+        dtype = RK_E4M3 if scaled else _dtype_id(k, "k")
+        self.dtype = torch.bfloat16 if scaled else k.dtype
         n_pages, n_kv, page, d = k.shape
-        at = [_need(t, what, dev, k.dtype, shape) for t, what, shape in
-              ((k, "k", k.shape), (v, "v", k.shape), (key_bounds, "key_bounds", (n_pages, n_kv, 2, d)))]
-        self.k, self.v, self.key_bounds, self.dtype = k, v, key_bounds, k.dtype
+        if scaled != (k_scales is not None) or scaled != (v_scales is not None):
+            raise ValueError("k_scales and v_scales go with a float8_e4m3fn cache")
+        at = [_need(t, what, dev, kind, shape) for t, what, kind, shape in
+              ((k, "k", k.dtype, k.shape), (v, "v", k.dtype, k.shape),
+               (key_bounds, "key_bounds", self.dtype, (n_pages, n_kv, 2, d)),
+               (k_scales, "k_scales", torch.uint8, (n_pages, n_kv, page)),
+               (v_scales, "v_scales", torch.uint8, (n_pages, n_kv, page)))]
+        self.k, self.v, self.key_bounds, self.k_scales, self.v_scales = k, v, key_bounds, k_scales, v_scales
         self.n_kv_heads, self.page_size, self.head_dim = n_kv, page, d
-        self._c = _PagedCache(*at, n_pages, page, n_kv, d, dtype)
+        self._c = _PagedCache(*at[:3], n_pages, page, n_kv, d, dtype, *at[3:])
         self._ref = ctypes.byref(self._c)
 
     def workspace_size(self, n_seqs: int, max_pages: int, n_heads: int, n_select: int = 0) -> int:
@@ -525,10 +554,7 @@ class PagedCache:
         import torch
         dev, dtype, n_rows, offsets = self._own(seqs), self.dtype, seqs.n_seqs, None
         if row_offsets is not None:
-            offsets = np.ascontiguousarray(np.asarray(row_offsets, dtype=np.int64))
-            if offsets.shape != (seqs.n_seqs + 1,):
-                raise ValueError(f"row_offsets: {seqs.n_seqs + 1} entries")
-            n_rows = int(offsets[-1])
+            offsets, n_rows = _host_offsets(row_offsets, seqs.n_seqs)
         shape = (n_rows, self.n_kv_heads, self.head_dim)
         for t, what in ((k, "k"), (v, "v")):
             if t.get_device() != dev or t.dtype is not dtype or t.shape != shape:
@@ -549,6 +575,30 @@ class PagedCache:
         rows = _PagedRows(None if offsets is None else offsets.ctypes.data, k.data_ptr(), v.data_ptr(), k_row, k_head,
                           v_row, v_head, q_at, qo_at, q_row, qo_row, n_heads, rope_theta, pos_at)
         _launch(dev, stream, load().rk_paged_append, self._ref, seqs._ref, ctypes.byref(rows))
+
+    def read(self, seqs: PagedSeqs, k=None, v=None, row_offsets: Optional[Sequence[int]] = None, stream=None):
+        """rk_paged_read into k, v [rows, n_kv_heads, head_dim] (either may be None), any strides of whole 16-byte
+        pieces; row_offsets: host offsets of the sequences' rows, or None for one row each."""
+        dev, dtype, n_rows, offsets = self._own(seqs), self.dtype, seqs.n_seqs, None
+        if row_offsets is not None:
+            offsets, n_rows = _host_offsets(row_offsets, seqs.n_seqs)
+        if k is None and v is None:
+            raise ValueError("k or v")
+        shape, at = (n_rows, self.n_kv_heads, self.head_dim), []
+        for t, what in ((k, "k"), (v, "v")):
+            if t is None:
+                at += [None, 0, 0]
+                continue
+            if t.get_device() != dev or t.dtype is not dtype or t.shape != shape:
+                _refuse(t, what, dev, dtype, shape, False)
+            row, head, one = t.stride()
+            if n_rows and one != 1:
+                raise ValueError("k, v: a head's values must be contiguous")
+            at += [t.data_ptr(), row, head]
+        if n_rows == 0 and not offsets.any():
+            return
+        _launch(dev, stream, load().rk_paged_read, self._ref, seqs._ref, None if offsets is None else offsets.ctypes.data,
+                *at)
 
     def _attend(self, fn, head, seqs, q, out, workspace, scale, lse, stream):
         import torch
@@ -576,6 +626,98 @@ class PagedCache:
                                                                     (seqs.n_seqs, self.n_kv_heads, n_select)))
         self._attend(load().rk_paged_attention_selected, (ctypes.byref(sel),), seqs, q, out, workspace, scale, lse,
                      stream)
+
+    def tree_workspace_size(self, n_seqs: int, n_rows: int, max_pages: int, n_heads: int) -> int:
+        return int(load().rk_paged_tree_workspace_size(self._ref, int(n_seqs), int(n_rows), int(max_pages),
+                                                       int(n_heads)))
+
+    def attention_tree(self, seqs: PagedSeqs, q, out, workspace, row_offsets: Sequence[int], masks=None,
+                       scale: float = 0.0, lse=None, stream=None):
+        """rk_paged_attention_tree: q, out [rows, n_heads, head_dim], lse float32 [rows, n_heads]; row_offsets: host
+        offsets of the sequences' drafts; masks int64 (or uint64) [rows], bit t for draft t, or None for chains."""
+        import torch
+        dev, dtype = self._own(seqs), self.dtype
+        offsets, n_rows = _host_offsets(row_offsets, seqs.n_seqs)
+        if q.dim() != 3:
+            raise ValueError("q: [rows, n_heads, head_dim]")
+        n_heads = q.shape[1]
+        shape = (n_rows, n_heads, self.head_dim)
+        q_at, q_row = _need_rows(q, "q", dev, dtype, shape)
+        out_at, out_row = _need_rows(out, "out", dev, dtype, shape)
+        words = torch.uint64 if masks is not None and masks.dtype is torch.uint64 else torch.int64
+        masks_at = _need(masks, "masks", dev, words, (n_rows,))
+        lse_at = _need(lse, "lse", dev, torch.float32, (n_rows, n_heads))
+        ws_at, ws_bytes = _need_workspace(workspace, dev)
+        _launch(dev, stream, load().rk_paged_attention_tree, self._ref, seqs._ref, offsets.ctypes.data, masks_at, q_at,
+                q_row, n_heads, scale, out_at, out_row, lse_at, ws_at, ws_bytes)
+
+    def keep(self, seqs: PagedSeqs, row_offsets: Sequence[int], kept, stream=None):
+        """rk_paged_keep: kept int32 [n_seqs, n_kept], rows may be strided; row_offsets: host offsets of the
+        sequences' drafts."""
+        import torch
+        dev = self._own(seqs)
+        offsets, _ = _host_offsets(row_offsets, seqs.n_seqs)
+        if kept.dim() != 2 or kept.get_device() != dev or kept.dtype is not torch.int32 or len(kept) != seqs.n_seqs:
+            raise ValueError(f"kept: int32 [{seqs.n_seqs}, n_kept] on cuda:{dev}")
+        n_kept = kept.shape[1]
+        if n_kept > 1 and kept.stride(1) != 1:
+            raise ValueError("kept: a row must be contiguous")
+        stride = kept.stride(0) if seqs.n_seqs > 1 else max(kept.stride(0), n_kept)
+        _launch(dev, stream, load().rk_paged_keep, self._ref, seqs._ref, offsets.ctypes.data, kept.data_ptr(), stride,
+                n_kept)
+
+    def reorder(self, seqs: PagedSeqs, parents, pages_out=None, stream=None):
+        """rk_paged_reorder: parents int32 [n_groups, n_beams]; pages_out int32 [n_seqs, max_pages] (``seqs.pages``
+        itself: in place) or None."""
+        import torch
+        dev = self._own(seqs)
+        if parents.dim() != 2 or parents.shape[0] * parents.shape[1] != seqs.n_seqs:
+            raise ValueError(f"parents: [n_groups, n_beams] of {seqs.n_seqs} sequences")
+        parents_at = _need(parents, "parents", dev, torch.int32, parents.shape)
+        out_at, stride = None, 0
+        if pages_out is not None:
+            shape = (seqs.n_seqs, seqs.max_pages)
+            if pages_out.get_device() != dev or pages_out.dtype is not torch.int32 or pages_out.shape != shape:
+                _refuse(pages_out, "pages_out", dev, torch.int32, shape, False)
+            if seqs.max_pages > 1 and pages_out.stride(1) != 1:
+                raise ValueError("pages_out: a row must be contiguous")
+            out_at, stride = pages_out.data_ptr(), pages_out.stride(0) if seqs.n_seqs > 1 else max(
+                pages_out.stride(0), seqs.max_pages)
+        _launch(dev, stream, load().rk_paged_reorder, self._ref, seqs._ref, parents.shape[1], parents_at, out_at, stride)
+
+
+def beam_select_workspace_size(n_groups: int, n_beams: int, vocab: int, n_out: int, dtype: str = "f32") -> int:
+    """rk_beam_select_workspace_size; dtype "f32" or "bf16"."""
+    return int(load().rk_beam_select_workspace_size(int(n_groups), int(n_beams), int(vocab),
+                                                    RK_BF16 if dtype == "bf16" else RK_F32, int(n_out)))
+
+
+def beam_select(logits, scores, parents, tokens, scores_out, workspace, ended=None, end_token: int = -1, stream=None):
+    """rk_beam_select.  logits: [n_groups * n_beams, vocab] float32 or bfloat16, rows may be strided; scores float32
+    and ended bool or uint8 (or None) [n_groups, n_beams]; parents, tokens int32 and scores_out float32 [n_groups,
+    n_out]."""
+    import torch
+    dev = _need_cuda(logits, "logits")
+    if logits.dim() != 2 or scores.dim() != 2 or parents.dim() != 2:
+        raise ValueError("logits: [rows, vocab], scores: [n_groups, n_beams], parents: [n_groups, n_out]")
+    dtype = _dtype_id(logits, "logits")
+    (n, vocab), (groups, beams), n_out = logits.shape, scores.shape, parents.shape[1]
+    if n != groups * beams:
+        raise ValueError(f"logits: {n} rows, not {groups} x {beams}")
+    row, one = logits.stride()
+    if n and vocab > 1 and one != 1:
+        raise ValueError("logits: a row must be contiguous")
+    f32, i32, shape = torch.float32, torch.int32, (groups, n_out)
+    scores_at = _need(scores, "scores", dev, f32, (groups, beams))
+    if ended is not None and ended.dtype is torch.bool:
+        ended_at = _need(ended, "ended", dev, torch.bool, (groups, beams))
+    else:
+        ended_at = _need(ended, "ended", dev, torch.uint8, (groups, beams))
+    outs = (_need(parents, "parents", dev, i32, shape), _need(tokens, "tokens", dev, i32, shape),
+            _need(scores_out, "scores_out", dev, f32, shape))
+    ws_at, ws_bytes = _need_workspace(workspace, dev)
+    _launch(dev, stream, load().rk_beam_select, logits.data_ptr(), dtype, groups, beams, vocab,
+            row if n > 1 else max(row, vocab), scores_at, ended_at, end_token, n_out, *outs, ws_at, ws_bytes)
 
 
 def token_logprobs_workspace_size(n_rows: int, vocab: int, n_top: int = 0, dtype: str = "f32") -> int:

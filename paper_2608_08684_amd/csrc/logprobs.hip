@@ -372,14 +372,21 @@ struct RowResult {
   }
 };
 
-template <typename T, int NT, bool TOP>
-__global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
+// A beam that can go on.
+__device__ __forceinline__ bool beam_open(const BeamArgs& b, int64_t r) {
+  return b.scores[r] > -INFINITY && !(b.ended && b.ended[r]);
+}
+
+// BEAM: sums and best logits always go to the workspace, for the join over a group's beams.
+template <typename T, int NT, bool TOP, bool BEAM = false>
+__global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a, BeamArgs beam) {
   constexpr int N = Logit<T>::N, NW = NT / 64, U = kPasses;
   __shared__ Sums sums[NW];
   __shared__ int counts[NW];
   __shared__ std::conditional_t<TOP, TopShared<NT>, int> sh;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t r = blockIdx.x / a.parts;
+  if (BEAM && !beam_open(beam, r)) return;
   const int part = (int)(blockIdx.x - r * a.parts), first = part * a.part_logits;
   const T* row = (const T*)a.logits + r * a.row_stride;
   const RowView<T> x(row + first, min(a.part_logits, a.vocab - first));
@@ -475,7 +482,7 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a) {
   __syncthreads();
   q = wave_sums(lane < NW ? sums[lane] : Sums{-INFINITY, 0.f, 0.f});
   count = wave_count(lane < NW ? counts[lane] : 0);
-  if (a.parts > 1) {
+  if (BEAM || a.parts > 1) {
     if (tid == 0) a.part[r * a.parts + part] = make_float4(q.c, q.s, q.t, __int_as_float(count));
     if constexpr (TOP)
       top_logits<T, NT>(x, a.n_top, (x.n_vec + NT * U - 1) / (NT * U) * (NT / 4), sh, [&](int i, uint32_t k, int id) {
@@ -533,14 +540,150 @@ hipError_t launch_logprobs(const LogprobArgs& a, bool bf16, hipStream_t s) {
   const int64_t blocks = a.n_rows * a.parts;
 #define RK_LOGPROBS(T, TOP)                                                                     \
   do {                                                                                          \
-    if (blocks <= 256) logprob_kernel<T, 1024, TOP><<<(uint32_t)blocks, 1024, 0, s>>>(a);       \
-    else if (blocks <= 512) logprob_kernel<T, 512, TOP><<<(uint32_t)blocks, 512, 0, s>>>(a);    \
-    else logprob_kernel<T, 256, TOP><<<(uint32_t)blocks, 256, 0, s>>>(a);                       \
+    if (blocks <= 256) logprob_kernel<T, 1024, TOP><<<(uint32_t)blocks, 1024, 0, s>>>(a, BeamArgs{});      \
+    else if (blocks <= 512) logprob_kernel<T, 512, TOP><<<(uint32_t)blocks, 512, 0, s>>>(a, BeamArgs{});   \
+    else logprob_kernel<T, 256, TOP><<<(uint32_t)blocks, 256, 0, s>>>(a, BeamArgs{});                      \
     if (a.parts > 1) logprob_join_kernel<T><<<(uint32_t)a.n_rows, 256, 0, s>>>(a);              \
   } while (0)
   if (bf16) { if (a.n_top) RK_LOGPROBS(bf16_t, true); else RK_LOGPROBS(bf16_t, false); }
   else { if (a.n_top) RK_LOGPROBS(float, true); else RK_LOGPROBS(float, false); }
 #undef RK_LOGPROBS
+  return hipGetLastError();
+}
+
+// --------------------------------------------------------------------------- beams
+// Of a group's candidates (beam b, token v) with score_b + x_v - c_b - log S_b the n_out best.
+// A candidate of the group's n_out best is one of its own row's: logprob_kernel leaves each
+// row's (each part's) best logits in falling order, and one workgroup per group chooses among
+// these lists.  Scores between beams are doubles of the logit, so that the order hangs on
+// nothing but log S; within a beam the logits themselves decide.
+//
+// A candidate's place is the number of candidates before it, counted against all of them at
+// once.  For more than 256 candidates, a bound first: with L lists the first k = ceil(n_out /
+// L) of each are n_out at least, so the n_out-th of those has n_out - 1 before it, and what
+// comes after it is out.  No more than n_out lists then have any left (or, where L < n_out,
+// there are L), n_out at most of each: 1024.
+// Bound: latency, a chain of loads, joins and counts, 4 us; the rows' kernel before it reads
+// every logit once.
+// (lists: 256 where rows are split to fill the card, 17 a row of 2^22 fp32 logits)
+constexpr int kMaxLists = 17 * RK_MAX_BEAMS, kMaxLeft = RK_MAX_TOP * RK_MAX_TOP;
+
+struct Candidates {
+  double score[kMaxLeft];
+  uint64_t key[kMaxLeft];    // order of the logit and complement of the token
+  int beam[kMaxLeft];
+  __device__ __forceinline__ bool before(int i, double s, int b, uint64_t k) const {
+    return score[i] > s || (score[i] == s && (beam[i] < b || (beam[i] == b && key[i] > k)));
+  }
+};
+
+__global__ __launch_bounds__(256) void beam_join_kernel(LogprobArgs a, BeamArgs p) {
+  constexpr int NT = 256;
+  __shared__ Candidates left;
+  __shared__ float4 sums[kMaxLists];
+  // a logit's score is its difference to ref, plus shift; -inf: no candidates
+  __shared__ double ref[RK_MAX_BEAMS], shift[RK_MAX_BEAMS];
+  __shared__ int n_left;
+  __shared__ double bound_score;
+  __shared__ uint64_t bound_key;
+  __shared__ int bound_beam;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int nb = p.n_beams, n = a.n_top, lists = nb * a.parts;
+  const int64_t row0 = (int64_t)blockIdx.x * nb;
+  for (int i = tid; i < lists; i += NT) {
+    const int64_t r = row0 + i / a.parts;
+    sums[i] = beam_open(p, r) ? a.part[row0 * a.parts + i] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+  }
+  if (tid == 0) { n_left = 0; bound_score = -INFINITY; bound_beam = 0; bound_key = 0; }
+  __syncthreads();
+  for (int b = w; b < nb; b += NT / 64) {
+    Sums q{-INFINITY, 0.f, 0.f};
+    if (lane < a.parts) { const float4 f = sums[b * a.parts + lane]; q = Sums{f.x, f.y, f.z}; }
+    q = wave_sums(q);
+    if (lane == 0) {
+      // without a finite largest logit S is 0 or NaN
+      ref[b] = q.ref();
+      shift[b] = q.s > 0.f ? (double)p.scores[row0 + b] - log((double)q.s) : -INFINITY;
+    }
+  }
+  __syncthreads();
+  // candidate i of list l; its score is not above -inf where there is none
+  const auto get = [&](int l, int i, double* s, uint64_t* k) {
+    const int b = l / a.parts;
+    const int64_t r = row0 + b;
+    if (p.ended && p.ended[r]) {
+      *s = l % a.parts == 0 && i == 0 ? (double)p.scores[r] : -INFINITY;
+      *k = (uint32_t)~p.end_token;
+    } else if (shift[b] > -INFINITY) {
+      *k = a.part_top[(row0 * a.parts + l) * n + i];
+      *s = ((double)from_order((uint32_t)(*k >> 32)) - ref[b]) + shift[b];
+    } else {
+      *s = -INFINITY;
+      *k = 0;
+    }
+  };
+  const int total = lists * n;
+  if (total > NT) {
+    const int k1 = (p.n_out + lists - 1) / lists, firsts = lists * k1;   // at most max(kMaxLists, 2 n_out)
+    for (int i = tid; i < firsts; i += NT) {
+      const int l = i / k1;
+      left.beam[i] = l / a.parts;
+      if (i - l * k1 < n) get(l, i - l * k1, &left.score[i], &left.key[i]);
+      else { left.score[i] = -INFINITY; left.key[i] = 0; }
+    }
+    __syncthreads();
+    for (int i = tid; i < firsts; i += NT) {
+      const double s = left.score[i];
+      if (!(s > -INFINITY)) continue;
+      int before = 0;
+      for (int j = 0; j < firsts; ++j) before += left.before(j, s, left.beam[i], left.key[i]);
+      if (before == p.n_out - 1) { bound_score = s; bound_beam = left.beam[i]; bound_key = left.key[i]; }
+    }
+    __syncthreads();
+  }
+  for (int i = tid; i < total; i += NT) {
+    const int l = i / n, b = l / a.parts;
+    double s;
+    uint64_t k;
+    get(l, i - l * n, &s, &k);
+    const bool after = s < bound_score || (s == bound_score && (b > bound_beam || (b == bound_beam && k < bound_key)));
+    if (!(s > -INFINITY) || (bound_score > -INFINITY && after)) continue;
+    const int at = atomicAdd(&n_left, 1);
+    if (at < kMaxLeft) { left.score[at] = s; left.key[at] = k; left.beam[at] = b; }
+  }
+  __syncthreads();
+  const int m = min(n_left, kMaxLeft);
+  const int64_t out = (int64_t)blockIdx.x * p.n_out;
+  for (int i = tid; i < m; i += NT) {
+    const double s = left.score[i];
+    const uint64_t k = left.key[i];
+    const int b = left.beam[i];
+    int before = 0;
+    for (int j = 0; j < m; ++j) before += left.before(j, s, b, k);
+    if (before >= p.n_out) continue;
+    p.parents[out + before] = b;
+    p.tokens[out + before] = (int)~(uint32_t)k;
+    p.scores_out[out + before] = (float)s;
+  }
+  for (int i = m + tid; i < p.n_out; i += NT) {
+    p.parents[out + i] = -1;
+    p.tokens[out + i] = -1;
+    p.scores_out[out + i] = -INFINITY;
+  }
+}
+
+hipError_t launch_beam_select(const LogprobArgs& a, const BeamArgs& b, bool bf16, hipStream_t s) {
+  if (a.n_rows <= 0) return hipSuccess;
+  const int64_t blocks = a.n_rows * a.parts;
+#define RK_BEAMS(T)                                                                                           \
+  do {                                                                                                        \
+    if (blocks <= 256) logprob_kernel<T, 1024, true, true><<<(uint32_t)blocks, 1024, 0, s>>>(a, b);           \
+    else if (blocks <= 512) logprob_kernel<T, 512, true, true><<<(uint32_t)blocks, 512, 0, s>>>(a, b);        \
+    else logprob_kernel<T, 256, true, true><<<(uint32_t)blocks, 256, 0, s>>>(a, b);                           \
+  } while (0)
+  if (bf16) RK_BEAMS(bf16_t); else RK_BEAMS(float);
+#undef RK_BEAMS
+  beam_join_kernel<<<(uint32_t)(a.n_rows / b.n_beams), 256, 0, s>>>(a, b);
   return hipGetLastError();
 }
 

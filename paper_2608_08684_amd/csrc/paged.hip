@@ -8,76 +8,11 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
-#include "rk_internal.h"
+#include "paged_tile.h"
 
 namespace rk {
-
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
-typedef short s16x4_t __attribute__((ext_vector_type(4)));
-typedef uint32_t v2u __attribute__((ext_vector_type(2)));
-typedef __attribute__((address_space(3))) s16x4_t lds_s16x4;
-
-constexpr float kLog2e = 1.4426950408889634f;
-
-// 16 bytes of cache elements as floats and back (one rounding to nearest even)
-template <typename T> struct Pack;
-template <> struct Pack<bf16_t> {
-  static constexpr int N = 8;
-  static __device__ __forceinline__ void get(v4u u, float* f) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f[2 * i] = __uint_as_float(u[i] << 16);
-      f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-    }
-  }
-  static __device__ __forceinline__ v4u put(const float* f) {
-    v4u u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) u[i] = (uint32_t)f2bf(f[2 * i]) | ((uint32_t)f2bf(f[2 * i + 1]) << 16);
-    return u;
-  }
-};
-template <> struct Pack<float> {
-  static constexpr int N = 4;
-  static __device__ __forceinline__ void get(v4u u, float* f) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(u[i]);
-  }
-  static __device__ __forceinline__ v4u put(const float* f) {
-    v4u u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(f[i]);
-    return u;
-  }
-};
-
-// e^x of a difference to a running maximum.  The difference is formed before the factor
-// log2(e): scaling the scores themselves would put that factor's rounding, times a
-// score of 50, into the weights.
-__device__ __forceinline__ float exp_diff(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
-// unit e^x with the product's rounding and log2(e)'s made good, for the weights of fp32
-// caches, whose outputs show them: e^-10 is off by 5e-7 without.  (Rescales and joins do
-// without: what they are off by is no more than the rounding of a score as large.)
-__device__ __forceinline__ float exp_diff_exact(float x, float unit) {
-  x = x < -200.f ? -200.f : x;   // 0 either way; a NaN stays
-  const float t = x * kLog2e, r = fmaf(x, kLog2e, -t) + x * 1.925963033500e-8f;
-  return __builtin_amdgcn_exp2f(t) * fmaf(r, 0.6931471806f * unit, unit);
-}
-
-// The largest bf16 below a positive x, as the bits of a float; 0 of 0.  What is left, x minus
-// it, is positive again, never 0 (at the least one step of x).
-__device__ __forceinline__ uint32_t bf16_below(float x) {
-  return __builtin_elementwise_sub_sat(__float_as_uint(x), 1u) & 0xffff0000u;
-}
-
-// Bounds keep a NaN.
-__device__ __forceinline__ float least(float a, float b) { return __builtin_elementwise_minimum(a, b); }
-__device__ __forceinline__ float largest(float a, float b) { return __builtin_elementwise_maximum(a, b); }
-
-__device__ __forceinline__ int min_i(int a, int b) { return a < b ? a : b; }
-__device__ __forceinline__ int max_i(int a, int b) { return a > b ? a : b; }
 
 // --------------------------------------------------------------------------- append
 // New row r = off[i] + j of sequence i (m_i of them) is entry lengths[i] - m_i + j of
@@ -107,6 +42,24 @@ __device__ __forceinline__ float2 turn(const AppendArgs& a, int pos, int x) {
   sincospif((float)(int32_t)t * 0x1p-31f, &s, &c);
   return make_float2(c, s);
 }
+// The same with the rounding of the angle made good, for keys of 8 bits: a key next to the
+// border of two of them goes to the wrong one that much less often.  The whole eighths of a
+// turn come off in whole numbers, and sine and cosine take up what the rest lost on its way to
+// fp32 as a first-order term.
+__device__ __forceinline__ float2 turn_exact(const AppendArgs& a, int pos, int x) {
+  if (!a.rotate) return make_float2(1.f, 0.f);
+  const uint32_t lo = (uint32_t)a.freq[x], hi = (uint32_t)(a.freq[x] >> 32);
+  uint32_t t = __umulhi((uint32_t)pos, lo) + (uint32_t)pos * hi;
+  if (pos < 0) t -= lo;
+  const uint32_t quarter = (t + 0x20000000u) >> 30;
+  const int32_t r = (int32_t)(t - (quarter << 30));   // -1/8 .. 1/8 of a turn
+  const float f = (float)r, rest = (float)(r - (int32_t)f) * 1.462918079e-9f;   // 2 pi / 2^32
+  float s, c;
+  sincospif(f * 0x1p-31f, &s, &c);
+  const float s1 = fmaf(rest, c, s), c1 = fmaf(-rest, s, c);
+  const float y = quarter & 1 ? c1 : s1, z = quarter & 1 ? s1 : c1;
+  return make_float2((quarter + 1) & 2 ? -z : z, quarter & 2 ? -y : y);
+}
 
 // A pair of 16-byte pieces, x .. and x + d/2 .., rotated.
 template <typename T, int HALF>
@@ -116,9 +69,9 @@ struct Pair {
     lo = *(const v4u*)src;
     hi = *(const v4u*)(src + HALF);
   }
-  __device__ __forceinline__ void rotate(const float2* cs) {
+  __device__ __forceinline__ void rotated(const float2* cs, float* y, float* z) const {
     constexpr int VE = Pack<T>::N;
-    float a[VE], b[VE], y[VE], z[VE];
+    float a[VE], b[VE];
     Pack<T>::get(lo, a);
     Pack<T>::get(hi, b);
 #pragma unroll
@@ -127,6 +80,10 @@ struct Pair {
       y[e] = a[e] * c.x - b[e] * c.y;
       z[e] = b[e] * c.x + a[e] * c.y;
     }
+  }
+  __device__ __forceinline__ void rotate(const float2* cs) {
+    float y[Pack<T>::N], z[Pack<T>::N];
+    rotated(cs, y, z);
     lo = Pack<T>::put(y);
     hi = Pack<T>::put(z);
   }
@@ -169,10 +126,19 @@ struct NewEntries {
   }
 };
 
-template <typename T, int DH>
+// The largest of a row's values, held by groups of W lanes.
+template <int W>
+__device__ __forceinline__ float row_max(float x) {
+#pragma unroll
+  for (int d = 1; d < W; d <<= 1) x = fmaxf(x, __shfl_xor(x, d, 64));
+  return x;
+}
+
+template <typename T, typename C, int DH>
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedView cache, PagedTable tab, AppendArgs a,
                                                                 SeqTable st) {
   constexpr int VE = Pack<T>::N, HALF = DH / 2, UPH = HALF / VE, NT = kAppendThreads, U = 4;
+  constexpr bool kScaled = std::is_same<C, e4m3_t>::value;
   __shared__ float2 cs[kAppendRows][HALF];
   const int tid = threadIdx.x, G = cache.n_kv, ps = 1 << cache.page_shift;
   int block = blockIdx.x;
@@ -245,8 +211,20 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedView cache,
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int i = i0 + u * NT, rr = i / per_row, c = i - rr * per_row;
-        if (i < total)
-          *(v4u*)((T*)cache.v + (((int64_t)w.page * G + c / CPH) * ps + e0 + rr) * DH + c % CPH * VE) = raw[u];
+        if (i < total) {
+          const int64_t row = ((int64_t)w.page * G + c / CPH) * ps + e0 + rr;
+          if constexpr (kScaled) {   // the lanes of a head's row side by side
+            float x[VE], m = 0.f;
+            Pack<T>::get(raw[u], x);
+#pragma unroll
+            for (int e = 0; e < VE; ++e) m = fmaxf(m, finite_abs(x[e]));
+            const uint32_t b = e4m3_scale_of(row_max<CPH>(m));
+            *(v2u*)((uint8_t*)cache.v + row * DH + c % CPH * VE) = to_e4m3(x, b);
+            if (c % CPH == 0) cache.v_scales[row] = (uint8_t)b;
+          } else {
+            *(v4u*)((T*)cache.v + row * DH + c % CPH * VE) = raw[u];
+          }
+        }
       }
     }
     return;
@@ -258,7 +236,8 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedView cache,
   __shared__ float red[NT][2 * VE];
   const int units = heads * UPH, RP = NT / units, rp = tid / units, u = tid - rp * units;   // RP >= 4 rows at a time
   const int h = h0 + u / UPH, x = u % UPH * VE;
-  T* kc = (T*)cache.k + (((int64_t)w.page * G + h) * ps + w.in_page) * DH + x;
+  const int64_t first_row = ((int64_t)w.page * G + h) * ps + w.in_page;
+  C* kc = (C*)cache.k + first_row * DH + x;
   const T* src = (const T*)a.k + (int64_t)w.row * a.k_rs + (int64_t)h * a.k_hs + x;
   float bl[2 * VE], bh[2 * VE];
 #pragma unroll
@@ -273,7 +252,8 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedView cache,
     __syncthreads();   // the last rows' angles are done with
     for (int i = tid; i < nb * HALF; i += NT) {
       const int rr = b + i / HALF;
-      cs[i / HALF][i % HALF] = turn(a, a.positions ? a.positions[w.row + rr] : w.entry + rr, i % HALF);
+      const int pos = a.positions ? a.positions[w.row + rr] : w.entry + rr;
+      cs[i / HALF][i % HALF] = kScaled ? turn_exact(a, pos, i % HALF) : turn(a, pos, i % HALF);
     }
     __syncthreads();
     if (rp < RP) {
@@ -281,12 +261,31 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedView cache,
       for (int q = 0; q < U; ++q) {
         const int rr = rp + q * RP;
         if (rr < nb) {
-          raw[q].rotate(&cs[rr][x]);
-          raw[q].store(kc + (int64_t)(b + rr) * DH);
-          if (cache.bounds) {   // of the keys as stored
-            float y[2 * VE];
+          float y[2 * VE];       // the key as stored
+          if constexpr (kScaled) {
+            float m = 0.f;
+            if (a.rotate) {
+              raw[q].rotated(&cs[rr][x], y, y + VE);
+            } else {   // an infinity stays with its own channel
+              Pack<T>::get(raw[q].lo, y);
+              Pack<T>::get(raw[q].hi, y + VE);
+            }
+#pragma unroll
+            for (int e = 0; e < 2 * VE; ++e) m = fmaxf(m, finite_abs(y[e]));
+            const uint32_t sb = e4m3_scale_of(row_max<UPH>(m));
+            const v2u lo = to_e4m3(y, sb), hi = to_e4m3(y + VE, sb);
+            *(v2u*)(kc + (int64_t)(b + rr) * DH) = lo;
+            *(v2u*)(kc + (int64_t)(b + rr) * DH + HALF) = hi;
+            if (x == 0) cache.k_scales[first_row + b + rr] = (uint8_t)sb;
+            from_e4m3(lo, sb, y);
+            from_e4m3(hi, sb, y + VE);
+          } else {
+            raw[q].rotate(&cs[rr][x]);
+            raw[q].store(kc + (int64_t)(b + rr) * DH);
             Pack<T>::get(raw[q].lo, y);
             Pack<T>::get(raw[q].hi, y + VE);
+          }
+          if (cache.bounds) {
 #pragma unroll
             for (int e = 0; e < 2 * VE; ++e) {
               bl[e] = least(bl[e], y[e]);
@@ -329,17 +328,6 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(PagedView cache,
   }
 }
 
-// Dispatch on the cache's element type and head size.
-#define RK_PAGED_DISPATCH(bf16, dh, CALL)                                 \
-  do {                                                                    \
-    if (bf16) {                                                           \
-      if (dh == 64) { CALL(bf16_t, 64); } else { CALL(bf16_t, 128); }     \
-    } else {                                                              \
-      if (dh == 32) { CALL(float, 32); }                                  \
-      else if (dh == 64) { CALL(float, 64); }                             \
-      else { CALL(float, 128); }                                          \
-    }                                                                     \
-  } while (0)
 
 // Page blocks: the pages that the new rows of a sequence may touch, one sequence after the other.
 int64_t append_plan(const PagedView& cache, const PagedTable& tab, const SeqTable& st, AppendArgs* a) {
@@ -374,8 +362,8 @@ hipError_t launch_append(const PagedView& cache, const PagedTable& tab, const Ap
                          int64_t workgroups, hipStream_t s) {
   if (workgroups <= 0) return hipSuccess;
   const uint32_t blocks = (uint32_t)workgroups;
-#define RK_APPEND(T, DH) append_kernel<T, DH><<<blocks, kAppendThreads, 0, s>>>(cache, tab, a, st)
-  RK_PAGED_DISPATCH(cache.bf16, cache.head_dim, RK_APPEND);
+#define RK_APPEND(T, C, DH) append_kernel<T, C, DH><<<blocks, kAppendThreads, 0, s>>>(cache, tab, a, st)
+  RK_PAGED_DISPATCH(cache, RK_APPEND);
 #undef RK_APPEND
   return hipGetLastError();
 }
@@ -398,9 +386,6 @@ __device__ __forceinline__ uint64_t score_key(double x) {
   return u >> 63 ? ~u : u | 0x8000000000000000ull;
 }
 
-__device__ __forceinline__ int table_length(const PagedTable& tab, int row, int page_shift) {
-  return max_i(0, (int)min((int64_t)tab.lengths[row], (int64_t)tab.max_pages << page_shift));
-}
 
 constexpr int kSelectThreads = 256;
 constexpr int kWavePages = 1024;    // pages whose keys one wave holds in registers
@@ -726,180 +711,6 @@ __global__ __launch_bounds__(kSelectThreads) void page_select_kernel(PagedView c
 // 32768 50 us (5.1: the join and the first tile's way, lengths to pages to keys, are 9 of
 // them).  8 waves a workgroup, three workgroups per CU, equal runs of tiles for every
 // workgroup whatever the sequences' lengths: all slower or the same.
-constexpr int kDecodeWaves = 4, kTile = 32;
-
-template <typename T, int DH> struct DecodeTile;
-
-template <int DH> struct DecodeTile<bf16_t, DH> {
-  static constexpr int CH = DH / 8;          // 16-byte pieces of a row
-  static constexpr int NC = DH / 32;         // k-steps of the scores
-  static constexpr int NV = kTile * CH / 64; // 16-byte loads of V per lane
-  static constexpr int ND = DH / 16;         // 16-row blocks of O^T
-  static constexpr int LDS = kTile * DH * 2; // bytes per wave
-  bf16x8_t q[NC];
-  v4u k[2][NC], v[NV];
-
-  // the 32-byte pair of pieces that ds_read_b64_tr_b16 takes from a row, placed so
-  // that eight consecutive rows use all 64 banks
-  static __device__ __forceinline__ int swz(int row) { return DH == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1; }
-
-  __device__ __forceinline__ void load_q(const bf16_t* qp, int lane) {   // row of this lane's head
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-      q[c] = __builtin_bit_cast(bf16x8_t, *(const v4u*)(qp + c * 32 + (lane >> 4) * 8));
-  }
-  // rows of the tile's two 16-entry halves
-  __device__ __forceinline__ void load_k(const bf16_t* k0, const bf16_t* k1, int lane) {
-    const uint32_t at = (lane & 15) * DH + (lane >> 4) * 8;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      k[0][c] = *(const v4u*)(k0 + at + c * 32);
-      k[1][c] = *(const v4u*)(k1 + at + c * 32);
-    }
-  }
-  __device__ __forceinline__ void load_v(const bf16_t* v0, const bf16_t* v1, int lane) {
-    // a load covers 64 / CH rows, all of one half
-    const uint32_t at = lane * 8;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] = *(const v4u*)((i < NV / 2 ? v0 : v1) + at + i % (NV / 2) * 512);
-  }
-  __device__ __forceinline__ void clear_values(uint32_t seen, int lane) {   // bit r: row r counts
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (!(seen >> ((i * 64 + lane) / CH) & 1)) v[i] = v4u{0, 0, 0, 0};
-  }
-  __device__ __forceinline__ void scores(f32x4_t s[2]) const {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k[t][c]), q[c], s[t], 0, 0, 0);
-    }
-  }
-  // the values' registers are free after stage_v
-  __device__ __forceinline__ void stage_v(char* lds, int lane) const {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int slot = i * 64 + lane, row = slot / CH, ch = slot % CH;
-      *(v4u*)(lds + (row * CH + (ch ^ swz(row))) * 16) = v[i];
-    }
-    wave_sync();
-  }
-  static constexpr bool kStaged = true;
-  __device__ __forceinline__ void values(const f32x4_t p[2], f32x4_t* o, char* lds, int lane) const {
-    v4u part[3];
-#pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-      const float x = p[e >> 2][e & 3], y = p[e >> 2][(e & 3) + 1];
-      const uint32_t x0 = bf16_below(x), y0 = bf16_below(y);
-      const float x1 = x - __uint_as_float(x0), y1 = y - __uint_as_float(y0);
-      const uint32_t x2 = bf16_below(x1), y2 = bf16_below(y1);
-      part[0][e / 2] = __builtin_amdgcn_perm(y0, x0, 0x07060302u);   // the upper halves
-      part[1][e / 2] = __builtin_amdgcn_perm(y2, x2, 0x07060302u);
-      part[2][e / 2] = (uint32_t)f2bf(x1 - __uint_as_float(x2)) | ((uint32_t)f2bf(y1 - __uint_as_float(y2)) << 16);
-    }
-    const int g = lane >> 4, jj = lane & 15, r = 4 * g + (jj >> 2);
-#pragma unroll
-    for (int b = 0; b < ND; ++b) {
-      const int ch = 2 * b + ((jj & 3) >> 1);
-      const char* at = lds + (r * CH + (ch ^ swz(r))) * 16 + (jj & 1) * 8;   // swz(r + 16) = swz(r)
-      const s16x4_t a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-      const s16x4_t a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * CH * 16));
-      const v4u a = {__builtin_bit_cast(v2u, a0)[0], __builtin_bit_cast(v2u, a0)[1], __builtin_bit_cast(v2u, a1)[0],
-                     __builtin_bit_cast(v2u, a1)[1]};
-#pragma unroll
-      for (int i = 0; i < 3; ++i)
-        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a),
-                                                       __builtin_bit_cast(bf16x8_t, part[i]), o[b], 0, 0, 0);
-    }
-    wave_sync();
-  }
-  // channel of element i of output block b in 16-lane group g
-  static __device__ __forceinline__ int channel(int b, int g, int i) { return b * 16 + 4 * g + i; }
-};
-
-template <int DH> struct DecodeTile<float, DH> {
-  static constexpr int NC = DH / 16;
-  static constexpr int VEC = DH >= 64 ? 4 : 2;   // channels per lane and load of V
-  static constexpr int NP = DH / (16 * VEC);     // loads per entry
-  static constexpr int ND = DH / 16;
-  static constexpr int LDS = 0;
-  typedef float vecf __attribute__((ext_vector_type(VEC)));
-  f32x4_t q[NC], k[2][NC];
-  vecf v[2][4][NP];
-
-  __device__ __forceinline__ void load_q(const float* qp, int lane) {
-#pragma unroll
-    for (int c = 0; c < NC; ++c) q[c] = *(const f32x4_t*)(qp + c * 16 + (lane >> 4) * 4);
-  }
-  __device__ __forceinline__ void load_k(const float* k0, const float* k1, int lane) {
-    const uint32_t at = (lane & 15) * DH + (lane >> 4) * 4;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      k[0][c] = *(const f32x4_t*)(k0 + at + c * 16);
-      k[1][c] = *(const f32x4_t*)(k1 + at + c * 16);
-    }
-  }
-  __device__ __forceinline__ void load_v(const float* v0, const float* v1, int lane) {
-    const uint32_t at = (lane >> 4) * 4 * DH + (lane & 15) * VEC;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int c = 0; c < NP; ++c) {
-        v[0][i][c] = *(const vecf*)(v0 + at + i * DH + c * 16 * VEC);
-        v[1][i][c] = *(const vecf*)(v1 + at + i * DH + c * 16 * VEC);
-      }
-  }
-  static constexpr bool kStaged = false;
-  __device__ __forceinline__ void stage_v(char*, int) const {}
-  __device__ __forceinline__ void clear_values(uint32_t seen, int lane) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (!(seen >> (t * 16 + 4 * (lane >> 4) + i) & 1))
-#pragma unroll
-          for (int c = 0; c < NP; ++c)
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) v[t][i][c][e] = 0.f;
-  }
-  __device__ __forceinline__ void scores(f32x4_t s[2]) const {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      // four sums over a quarter of the channels each: shorter chains, and none waits for another
-      f32x4_t a[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        a[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int c = 0; c < NC; ++c) a[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[t][c][e], q[c][e], a[e], 0, 0, 0);
-      }
-      s[t] = (a[0] + a[1]) + (a[2] + a[3]);
-    }
-  }
-  __device__ __forceinline__ void values(const f32x4_t p[2], f32x4_t* o, char*, int) const {
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int c = 0; c < NP; ++c)
-#pragma unroll
-          for (int e = 0; e < VEC; ++e)
-            o[c * VEC + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[t][i][c][e], p[t][i], o[c * VEC + e], 0, 0, 0);
-  }
-  static __device__ __forceinline__ int channel(int b, int g, int i) {
-    return (b / VEC) * 16 * VEC + VEC * (4 * g + i) + b % VEC;
-  }
-};
-
-// Entries of one part of a length: whole tiles for every wave, at most n_parts parts.
-__device__ __forceinline__ int part_entries(int len, int n_parts) {
-  constexpr int unit = kTile * kDecodeWaves;
-  const int per = (len + n_parts - 1) / n_parts;
-  return max_i((per + unit - 1) / unit, 1) * unit;
-}
 
 // SEL: attention over selected pages.  kKeys: their keys are in the workspace; kScores:
 // the workgroup forms them; either way its first wave then makes the choice, the same
@@ -907,10 +718,10 @@ __device__ __forceinline__ int part_entries(int len, int n_parts) {
 // and the way through memory).
 enum class Sel { kNone, kKeys, kScores };
 
-template <typename T, int DH, Sel SEL>
+template <typename T, typename C, int DH, Sel SEL>
 __global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cache, PagedTable tab, DecodeArgs a,
                                                                    SelectArgs sel) {
-  using Tile = DecodeTile<T, DH>;
+  using Tile = CacheTile<C, DH>;
   constexpr int NW = kDecodeWaves, SP = DH + 4;
   constexpr int AREA0 = Tile::LDS * NW > NW * 16 * SP * 4 ? Tile::LDS * NW : NW * 16 * SP * 4;
   constexpr int SCORES = SEL == Sel::kScores ? 2 * DH * 8 + kWavePages * 8 : 0;
@@ -974,11 +785,12 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cac
   const int64_t head_at = (int64_t)hk << shift, page_rows = (int64_t)G << shift;
 
   Tile tile;
+  typename Tile::Query query[1];
   const int col = lane & 15, g = lane >> 4;
-  tile.load_q((const T*)a.q + (int64_t)seq * a.q_rs + (int64_t)(h0 + min_i(col, nh - 1)) * DH, lane);
-  f32x4_t o[Tile::ND];
+  Tile::load_q(query[0], (const T*)a.q + (int64_t)seq * a.q_rs + (int64_t)(h0 + min_i(col, nh - 1)) * DH, lane);
+  f32x4_t o[1][Tile::ND];
 #pragma unroll
-  for (int i = 0; i < Tile::ND; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < Tile::ND; ++i) o[0][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
   // Weights count in units of a power of two above the part's entries: their sum stays below
   // 1, and that of weighted values below the largest, however large they are.
@@ -989,7 +801,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cac
     int k0, p0, p1;
   };
   struct Where {
-    int64_t at0, at1;   // element offsets of the two halves
+    int64_t r0, r1;     // rows of the cache at which the two halves begin
     uint32_t seen;      // entries that count
   };
   const int step = NW * kTile, first = start + w * kTile;
@@ -1002,14 +814,12 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cac
     const int p0 = __builtin_amdgcn_readfirstlane(p.p0), p1 = __builtin_amdgcn_readfirstlane(p.p1);
     const bool ok0 = p0 >= 0 && p0 < cache.n_pages, ok1 = p1 >= 0 && p1 < cache.n_pages;
     Where wh;
-    wh.at0 = ((ok0 ? p0 : 0) * page_rows + head_at + (p.k0 & in_mask)) * DH;
-    wh.at1 = ((ok1 ? p1 : 0) * page_rows + head_at + ((p.k0 + 16) & in_mask)) * DH;
+    wh.r0 = (ok0 ? p0 : 0) * page_rows + head_at + (p.k0 & in_mask);
+    wh.r1 = (ok1 ? p1 : 0) * page_rows + head_at + ((p.k0 + 16) & in_mask);
     wh.seen = (ok0 ? 0xffffu : 0u) | (ok1 ? 0xffff0000u : 0u);
     if (end - p.k0 < 32) wh.seen &= (1u << (end - p.k0)) - 1u;
     return wh;
   };
-  const T* kc = (const T*)cache.k;
-  const T* vc = (const T*)cache.v;
   // The next tile's rows are asked for as soon as this one's leave their registers: its
   // keys after the scores, its values once they are in LDS; their pages a tile earlier.
   // After the last tile these loads repeat it, so that no wait depends on a branch.
@@ -1017,37 +827,37 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cac
   Pages ahead{};
   if (first < end) {
     cur = where(pages_of(first));
-    tile.load_k(kc + cur.at0, kc + cur.at1, lane);
-    tile.load_v(vc + cur.at0, vc + cur.at1, lane);
+    tile.load_k(cache, cur.r0, cur.r1, lane);
+    tile.load_v(cache, cur.r0, cur.r1, lane);
     nxt = where(pages_of(first + step));
     ahead = pages_of(first + 2 * step);
   }
   for (int k0 = first; k0 < end; k0 += step) {
     const uint32_t seen = cur.seen;
-    f32x4_t s[2];
-    tile.scores(s);
-    tile.load_k(kc + nxt.at0, kc + nxt.at1, lane);
+    f32x4_t s[1][2];
+    tile.template scores<1>(query, s);
+    tile.load_k(cache, nxt.r0, nxt.r1, lane);
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[t][i] *= a.scale;
+      for (int i = 0; i < 4; ++i) s[0][t][i] *= a.scale;
     if (seen != 0xffffffffu) {
       tile.clear_values(seen, lane);
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (!(seen >> (t * 16 + 4 * g + i) & 1)) s[t][i] = -INFINITY;
+          if (!(seen >> (t * 16 + 4 * g + i) & 1)) s[0][t][i] = -INFINITY;
     }
     cur = nxt;
     if constexpr (Tile::kStaged) {
       tile.stage_v(area + w * Tile::LDS, lane);
-      tile.load_v(vc + cur.at0, vc + cur.at1, lane);
+      tile.load_v(cache, cur.r0, cur.r1, lane);
     }
     nxt = where(ahead);
     ahead = pages_of(k0 + 3 * step);
-    float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
-                     fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+    float mx = fmaxf(fmaxf(fmaxf(s[0][0][0], s[0][0][1]), fmaxf(s[0][0][2], s[0][0][3])),
+                     fmaxf(fmaxf(s[0][1][0], s[0][1][1]), fmaxf(s[0][1][2], s[0][1][3])));
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
     const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.f : m_new;
@@ -1055,16 +865,16 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cac
     m = m_new;
     l *= corr;
 #pragma unroll
-    for (int i = 0; i < Tile::ND; ++i) o[i] *= corr;
+    for (int i = 0; i < Tile::ND; ++i) o[0][i] *= corr;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        s[t][i] = sizeof(T) == 4 ? exp_diff_exact(s[t][i] - ref, unit) : exp_diff(s[t][i] - ref) * unit;
-        l += s[t][i];
+        s[0][t][i] = sizeof(T) == 4 ? exp_diff_exact(s[0][t][i] - ref, unit) : exp_diff(s[0][t][i] - ref) * unit;
+        l += s[0][t][i];
       }
-    tile.values(s, o, area + w * Tile::LDS, lane);
-    if constexpr (!Tile::kStaged) tile.load_v(vc + cur.at0, vc + cur.at1, lane);
+    tile.template values<1, 3>(s, o, area + w * Tile::LDS, lane);
+    if constexpr (!Tile::kStaged) tile.load_v(cache, cur.r0, cur.r1, lane);
   }
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
@@ -1074,7 +884,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cac
 #pragma unroll
   for (int i = 0; i < Tile::ND; ++i)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) so[(w * 16 + col) * SP + Tile::channel(i, g, e)] = o[i][e];
+    for (int e = 0; e < 4; ++e) so[(w * 16 + col) * SP + Tile::channel(i, g, e)] = o[0][i][e];
   __syncthreads();
   for (int i = tid; i < nh * DH; i += 64 * NW) {
     const int h = i / DH, x = i % DH;
@@ -1189,13 +999,13 @@ hipError_t launch_decode(const PagedView& cache, const PagedTable& tab, DecodeAr
   // start are short (32 sequences of 100 .. 8192 entries, 8 KV heads: 118 -> 109 us; 64 equal
   // ones 188 -> 191; more than 64 are taken in their order, a wave has 64 lanes to know them)
   a.longest_first = blocks > 512 && tab.n_seqs <= 64 && !tab.per_head;
-#define RK_DECODE(T, DH)                                                                                           \
+#define RK_DECODE(T, C, DH)                                                                                        \
   do {                                                                                                             \
-    decode_kernel<T, DH, Sel::kNone><<<(uint32_t)blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, a, SelectArgs{});  \
+    decode_kernel<T, C, DH, Sel::kNone><<<(uint32_t)blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, a, SelectArgs{});  \
     if (a.n_parts > 1)                                                                                             \
       decode_join_kernel<T, DH><<<tab.n_seqs * a.n_heads, 256, 0, s>>>(tab, a, cache.n_kv, cache.page_shift);      \
   } while (0)
-  RK_PAGED_DISPATCH(cache.bf16, cache.head_dim, RK_DECODE);
+  RK_PAGED_DISPATCH(cache, RK_DECODE);
 #undef RK_DECODE
   return hipGetLastError();
 }
@@ -1225,9 +1035,9 @@ hipError_t launch_decode_selected(const PagedView& cache, const PagedTable& tab,
     // a workgroup's threads four times over, split further while CUs are idle
     const int per_pass = kSelectThreads * 16 * 4 / page_bytes;
     const int chunks = std::max(1, std::min((tab.max_pages + per_pass - 1) / per_pass, std::max(1, 2048 / rows)));
-#define RK_SCORES(T, DH) \
+#define RK_SCORES(T, C, DH) \
   page_scores_kernel<T, DH><<<(uint32_t)rows * chunks, kSelectThreads, 0, s>>>(cache, tab, sel, chunks)
-    RK_PAGED_DISPATCH(cache.bf16, cache.head_dim, RK_SCORES);
+    RK_PAGED_DISPATCH(cache, RK_SCORES);
 #undef RK_SCORES
   }
   if (!held) {
@@ -1237,14 +1047,14 @@ hipError_t launch_decode_selected(const PagedView& cache, const PagedTable& tab,
   DecodeArgs d = a;
   d.longest_first = false;
   const uint32_t blocks = (uint32_t)((int64_t)rows * head_tiles * a.n_parts);
-#define RK_DECODE(T, DH)                                                                                              \
+#define RK_DECODE(T, C, DH)                                                                                           \
   do {                                                                                                                \
-    if (alone) decode_kernel<T, DH, Sel::kScores><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, d, sel);           \
-    else decode_kernel<T, DH, Sel::kKeys><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, d, sel);                   \
+    if (alone) decode_kernel<T, C, DH, Sel::kScores><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, d, sel);           \
+    else decode_kernel<T, C, DH, Sel::kKeys><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, d, sel);                   \
     if (a.n_parts > 1)                                                                                                \
       decode_join_kernel<T, DH><<<tab.n_seqs * a.n_heads, 256, 0, s>>>(lists, d, cache.n_kv, cache.page_shift);       \
   } while (0)
-  RK_PAGED_DISPATCH(cache.bf16, cache.head_dim, RK_DECODE);
+  RK_PAGED_DISPATCH(cache, RK_DECODE);
 #undef RK_DECODE
   return hipGetLastError();
 }

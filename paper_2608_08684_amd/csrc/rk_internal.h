@@ -225,9 +225,11 @@ constexpr int64_t kMaxWorkgroups = 0xffffffffll / 256;
 // --------------------------------------------------------------------------- paged cache
 struct PagedView {
   void *k, *v, *bounds;   // [n_pages, n_kv, 1 << page_shift, head_dim]; bounds [n_pages, n_kv, 2, head_dim] or NULL
+  uint8_t *k_scales, *v_scales;   // [n_pages, n_kv, 1 << page_shift], e4m3 only
   int64_t n_pages;
   int page_shift, n_kv, head_dim;
-  bool bf16;
+  bool bf16;                      // type of the rows that come and go: bf16, or fp32
+  bool e4m3;                      // k and v in 8 bits (rows in bf16); otherwise they have the rows' type
 };
 // Pages and entries of each sequence, or (per_head) of each (sequence, KV head).
 struct PagedTable {
@@ -282,6 +284,47 @@ struct SelectArgs {
 hipError_t launch_decode_selected(const PagedView& cache, const PagedTable& tab, const DecodeArgs& a,
                                   const SelectArgs& sel, hipStream_t s);
 
+// --------------------------------------------------------------------------- drafted tokens
+struct TreeArgs {
+  const void* q;
+  void* out;
+  float* lse;
+  const uint64_t* masks;    // or NULL: chains
+  int64_t q_rs, out_rs;     // elements
+  int n_heads, n_parts;
+  int col_blocks;           // of the launcher
+  float scale;
+  float* part_o;            // [rows * n_heads, n_parts, head_dim], n_parts > 1 only
+  float* part_lse;          // [rows * n_heads, n_parts]
+};
+constexpr int kMaxTreeParts = 64;
+// Parts that the length is split into, for trees of up to max_drafts rows.
+int tree_parts(const PagedView& cache, int n_seqs, int max_drafts, int n_heads, int64_t max_entries);
+int64_t tree_blocks(const PagedView& cache, const SeqTable& st, const TreeArgs& a);   // workgroups
+// st: the drafts' rows, max_len the most of a sequence (at least 1).
+hipError_t launch_tree(const PagedView& cache, const PagedTable& tab, const SeqTable& st, TreeArgs a, hipStream_t s);
+
+// Moves of entries within the cache and out of it.
+struct ReadArgs {
+  void *k, *v;                        // or NULL
+  int64_t k_rs, k_hs, v_rs, v_hs;     // elements
+  int n_rows;
+  bool one_row;                       // one row per sequence; otherwise the rows of a SeqTable
+};
+int64_t read_blocks(int n_rows);      // workgroups
+hipError_t launch_read(const PagedView& cache, const PagedTable& tab, const ReadArgs& a, const SeqTable& st,
+                       hipStream_t s);
+hipError_t launch_keep(const PagedView& cache, const PagedTable& tab, const SeqTable& st, const int32_t* kept,
+                       int64_t kept_stride, int n_kept, hipStream_t s);
+struct ReorderArgs {
+  const int32_t* parents;
+  int32_t* pages_out;                 // or NULL
+  int64_t out_stride;
+  int n_beams;
+};
+int64_t reorder_blocks(const PagedView& cache, int n_seqs, int n_beams, int max_pages);   // workgroups
+hipError_t launch_reorder(const PagedView& cache, const PagedTable& tab, const ReorderArgs& a, hipStream_t s);
+
 // --------------------------------------------------------------------------- token log probabilities
 struct LogprobArgs {
   const void* logits;
@@ -298,6 +341,15 @@ struct LogprobArgs {
 constexpr int kMaxVocab = 1 << 22;
 void logprob_parts(int64_t n_rows, int vocab, bool bf16, int* parts, int* part_logits);
 hipError_t launch_logprobs(const LogprobArgs& a, bool bf16, hipStream_t s);
+// Beams: a row of logits each, a.part and a.part_top [rows, parts (, n_top)] whatever parts is.
+struct BeamArgs {
+  const float* scores;      // [n_groups, n_beams]
+  const uint8_t* ended;     // or NULL
+  int n_beams, n_out, end_token;
+  int32_t *parents, *tokens;
+  float* scores_out;
+};
+hipError_t launch_beam_select(const LogprobArgs& a, const BeamArgs& b, bool bf16, hipStream_t s);
 
 hipError_t launch_finalize(const double* s_acc, int n, double inv_n, float* s_out, hipStream_t s);
 hipError_t launch_zero_f64(double* p, int n, hipStream_t s);
