@@ -119,6 +119,53 @@ __device__ __forceinline__ void from_e4m3(v2u u, uint32_t b, float* x) {
   }
 }
 
+// 16 bytes of values: infinities and NaN become 0 (sign 0), or all others do, and those of that
+// sign and NaN become 2 or -2 (sign 1 or -1); whether there are any.
+template <typename C> __device__ __forceinline__ bool take_out(v4u& v, int sign);
+template <> __device__ __forceinline__ bool take_out<bf16_t>(v4u& v, int sign) {
+  bool any = false;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    uint32_t r = 0;
+#pragma unroll
+    for (int at = 0; at < 32; at += 16) {
+      const uint32_t x = v[w] >> at & 0xffffu;
+      const bool bad = (x & 0x7f80u) == 0x7f80u, mine = bad && ((x & 0x7fu) || (x >> 15) == (sign < 0));
+      any |= bad;
+      r |= (sign == 0 ? (bad ? 0u : x) : mine ? (sign < 0 ? 0xc000u : 0x4000u) : 0u) << at;
+    }
+    v[w] = r;
+  }
+  return any;
+}
+template <> __device__ __forceinline__ bool take_out<e4m3_t>(v4u& v, int sign) {   // NaN alone: of either sign
+  bool any = false;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    uint32_t r = 0;
+#pragma unroll
+    for (int at = 0; at < 32; at += 8) {
+      const uint32_t x = v[w] >> at & 0xffu;
+      const bool bad = (x & 0x7fu) == 0x7fu;
+      any |= bad;
+      r |= (sign == 0 ? (bad ? 0u : x) : bad ? (sign < 0 ? 0xc0u : 0x40u) : 0u) << at;
+    }
+    v[w] = r;
+  }
+  return any;
+}
+template <> __device__ __forceinline__ bool take_out<float>(v4u& v, int sign) {
+  bool any = false;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float x = __uint_as_float(v[w]);
+    const bool bad = !(fabsf(x) < INFINITY), mine = bad && (x != x || (x < 0.f) == (sign < 0));
+    any |= bad;
+    v[w] = __float_as_uint(sign == 0 ? (bad ? 0.f : x) : mine ? 2.f * sign : 0.f);
+  }
+  return any;
+}
+
 // Bounds keep a NaN.
 __device__ __forceinline__ float least(float a, float b) { return __builtin_elementwise_minimum(a, b); }
 __device__ __forceinline__ float largest(float a, float b) { return __builtin_elementwise_maximum(a, b); }
@@ -153,10 +200,19 @@ template <int DH> struct StagedValues {
   // that eight consecutive rows use all 64 banks
   static __device__ __forceinline__ int swz(int row) { return DH == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1; }
 
+  // 16 channels of 32 entries, as the A operand
+  static __device__ __forceinline__ v4u transposed(int b, const char* lds, int lane) {
+    const int g = lane >> 4, jj = lane & 15, r = 4 * g + (jj >> 2), ch = 2 * b + ((jj & 3) >> 1);
+    const char* at = lds + (r * CH + (ch ^ swz(r))) * 16 + (jj & 1) * 8;   // swz(r + 16) = swz(r)
+    const s16x4_t a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+    const s16x4_t a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * CH * 16));
+    return v4u{__builtin_bit_cast(v2u, a0)[0], __builtin_bit_cast(v2u, a0)[1], __builtin_bit_cast(v2u, a1)[0],
+               __builtin_bit_cast(v2u, a1)[1]};
+  }
+  // a lane's weights as the B operand
   template <int N, int PIECES>
-  static __device__ __forceinline__ void accumulate(const f32x4_t (*p)[2], f32x4_t (*o)[ND], char* lds, int lane) {
+  static __device__ __forceinline__ void pieces(const f32x4_t (*p)[2], v4u (*part)[PIECES]) {
     static_assert(PIECES == 2 || PIECES == 3, "weights");
-    v4u part[N][PIECES];
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -174,15 +230,12 @@ template <int DH> struct StagedValues {
           part[n][1][e / 2] = (uint32_t)f2bf(x1) | ((uint32_t)f2bf(y1) << 16);
         }
       }
-    const int g = lane >> 4, jj = lane & 15, r = 4 * g + (jj >> 2);
+  }
+  template <int N, int PIECES>
+  static __device__ __forceinline__ void add(const v4u (*part)[PIECES], f32x4_t (*o)[ND], const char* lds, int lane) {
 #pragma unroll
     for (int b = 0; b < ND; ++b) {
-      const int ch = 2 * b + ((jj & 3) >> 1);
-      const char* at = lds + (r * CH + (ch ^ swz(r))) * 16 + (jj & 1) * 8;   // swz(r + 16) = swz(r)
-      const s16x4_t a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-      const s16x4_t a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * CH * 16));
-      const v4u a = {__builtin_bit_cast(v2u, a0)[0], __builtin_bit_cast(v2u, a0)[1], __builtin_bit_cast(v2u, a1)[0],
-                     __builtin_bit_cast(v2u, a1)[1]};
+      const v4u a = transposed(b, lds, lane);
 #pragma unroll
       for (int i = 0; i < PIECES; ++i)
 #pragma unroll
@@ -190,6 +243,12 @@ template <int DH> struct StagedValues {
           o[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a),
                                                             __builtin_bit_cast(bf16x8_t, part[n][i]), o[n][b], 0, 0, 0);
     }
+  }
+  template <int N, int PIECES>
+  static __device__ __forceinline__ void accumulate(const f32x4_t (*p)[2], f32x4_t (*o)[ND], char* lds, int lane) {
+    v4u part[N][PIECES];
+    pieces<N, PIECES>(p, part);
+    add<N, PIECES>(part, o, lds, lane);
     wave_sync();
   }
   // channel of element i of output block b in 16-lane group g
@@ -245,26 +304,10 @@ template <int DH> struct CacheTile<bf16_t, DH> : StagedValues<DH> {
                                                             0, 0, 0);
     }
   }
-  // Infinite and NaN values become 0, or (sign 1 or -1) all others do and those of that sign,
-  // and NaN, 2 or -2; whether there are any.
-  __device__ __forceinline__ bool take_out(int sign) {
+  __device__ __forceinline__ bool take_out_values(int sign) {   // see take_out
     bool any = false;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const uint32_t u = v[i][w];
-        uint32_t r = 0;
-#pragma unroll
-        for (int half = 0; half < 32; half += 16) {
-          const uint32_t x = u >> half & 0xffffu;
-          const bool bad = (x & 0x7f80u) == 0x7f80u;
-          any |= bad;
-          const uint32_t y = sign == 0 ? (bad ? 0u : x) : bad && ((x & 0x7fu) || (x >> 15) == (sign < 0)) ? (sign < 0 ? 0xc000u : 0x4000u) : 0u;
-          r |= y << half;
-        }
-        v[i][w] = r;
-      }
+    for (int i = 0; i < NV; ++i) any |= take_out<bf16_t>(v[i], sign);
     return any;
   }
   // the values' registers are free after stage_v
@@ -326,23 +369,11 @@ template <int DH> struct CacheTile<e4m3_t, DH> : StagedValues<DH> {
     for (int i = 0; i < NV; ++i)
       if (!(seen >> ((i * 64 + lane) / CB) & 1)) { v[i] = v4u{0, 0, 0, 0}; vs[i] = 127; }
   }
-  // NaN alone: it is of either sign
-  __device__ __forceinline__ bool take_out(int sign) {
+  __device__ __forceinline__ bool take_out_values(int sign) {
     bool any = false;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        uint32_t r = 0;
-#pragma unroll
-        for (int b = 0; b < 32; b += 8) {
-          const uint32_t x = v[i][w] >> b & 0xffu;
-          const bool bad = (x & 0x7fu) == 0x7fu;
-          any |= bad;
-          r |= (sign == 0 ? (bad ? 0u : x) : bad ? (sign < 0 ? 0xc0u : 0x40u) : 0u) << b;
-        }
-        v[i][w] = r;
-      }
+      any |= take_out<e4m3_t>(v[i], sign);
       if (sign != 0) vs[i] = 127;
     }
     return any;
@@ -429,21 +460,21 @@ template <int DH> struct CacheTile<float, DH> {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) v[t][i][c][e] = 0.f;
   }
-  __device__ __forceinline__ bool take_out(int sign) {
+  __device__ __forceinline__ bool take_out_values(int sign) {
     bool any = false;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int c = 0; c < NP; ++c)
+        for (int c = 0; c < NP; ++c) {
+          v4u u = {0, 0, 0, 0};
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) {
-            const float x = v[t][i][c][e];
-            const bool bad = !(fabsf(x) < INFINITY);
-            any |= bad;
-            v[t][i][c][e] = sign == 0 ? (bad ? 0.f : x) : bad && (x != x || (x < 0.f) == (sign < 0)) ? 2.f * sign : 0.f;
-          }
+          for (int e = 0; e < VEC; ++e) u[e] = __float_as_uint(v[t][i][c][e]);
+          any |= take_out<float>(u, sign);
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) v[t][i][c][e] = __uint_as_float(u[e]);
+        }
     return any;
   }
   template <int N>

@@ -1,36 +1,82 @@
 // Attention of a tree of drafted tokens of each sequence over its paged cache.
+//
+// Sequence i's m drafts are its last m entries, b .. b + m - 1, and draft j of query head h
+//   o_j,h = sum_u softmax_u(scale q_j,h . k_u) v_u,  u < b, or u = b + t with bit t of mask_j.
+// The m x H / H_kv query rows of a KV head are the columns of one pass over its cache, so that
+// an entry is read once for 16 .. 128 of them.  Two kernels:
+//   up to 16 columns (fp32: 32 of any number): the waves of a workgroup take the tiles of its
+//     part of the length in turn, as in the attention of one token (tree_narrow_kernel);
+//   more: all waves go through the same tiles, which LDS holds for them, each with columns of
+//     its own (tree_wide_kernel).
+//
+// A column keeps a reference R, the sum l of its weights e^(s - R) and its output.  R is
+// moved only when a score has passed it by kRaise: the output's rescale, a multiplication of
+// every accumulator, is then rare.  bf16 and 8-bit caches: R is held times log2(e) and a
+// weight's exponent is one fma of the score; what its rounding puts into a weight, 2^-24 of a
+// score, is far below the output's bf16.  R also holds the power of two above the part's entries
+// (the weights' sum stays below 1, and no weighted sum overflows).
+//
+// A value that is infinite or NaN must not reach the columns whose mask leaves its draft out,
+// but 0 times it would: in the tiles that hold drafts such values are taken out of the
+// product, and added afterwards to the columns that see them, by products of their own.
 #include <algorithm>
 #include <type_traits>
 
 #include "paged_tile.h"
 
 namespace rk {
+namespace {
 
-// Sequence i's m drafts are its last m entries, b .. b + m - 1, and draft j of query head h
-//   o_j,h = sum_u softmax_u(scale q_j,h . k_u) v_u,  u < b, or u = b + t with bit t of mask_j.
-// The m x H / H_kv query rows of a KV head are the columns of one pass over its cache: a
-// workgroup of 4 waves takes 16 N of them and a part of the length, its waves the part's
-// 32-entry tiles in turn, so that keys and values go from memory to registers once for all
-// of the columns (N = 1, 2 or 4 by how many there are).  Column blocks of one part follow each
-// other on the same XCD: the second finds the cache in its L2.
-// A column keeps a reference R, the sum l of its weights e^(s - R) and its output.  R is
-// moved only when a score has passed it by kRaise: the output's rescale, a multiplication of
-// every accumulator, is then rare, and the accumulators stay where the matrix unit has them.
-// bf16 and 8-bit caches: R is held times log2(e) and the weight's exponent is one fma of the
-// score; what its rounding puts into a weight, 2^-24 of a score, is far below the output's
-// bf16.  R also holds the power of two above the part's entries (the weights' sum stays below
-// 1, and no weighted sum overflows).  Weights enter the second product as two bf16 numbers, 16
-// bits and more, where a tile has several column blocks: the third of paged_attention's would
-// cost as much again in the matrix unit and changes the output by 2^-17 of itself.
-// A value that is infinite or NaN must not reach the columns whose mask leaves its draft out,
-// but 0 times it would: in the tiles that hold drafts such values are taken out of the
-// product, and added to the columns that see them by products of their own.
 constexpr float kRaise = 8.f;            // of a score, natural units
 constexpr float kUnset = -3.0e38f;       // R of a column that has seen nothing
+constexpr float kHuge = 3.3e38f;         // the weight that makes an infinity of 2
+constexpr uint32_t kHugeBits = 0x7f78u;  // and in bf16
 
+// A workgroup's share: item = (rank of the sequence by falling length * parts + part) * G + KV
+// head, and a column block of it.  The column blocks of an item follow each other on the same
+// XCD, so that the second finds the cache in its L2; the longest sequences come first, so that
+// the last to start are short; and neighbours are heads, which have the same to do, not parts,
+// of which short sequences have fewer (they would leave every other XCD idle).
+struct Share {
+  int seq, hk, part, parts, cb, len, row0, m, base, start, end;   // parts: of this sequence
+  bool none;
+  __device__ __forceinline__ Share(const PagedView& cache, const PagedTable& tab, const SeqTable& st, const TreeArgs& a,
+                                   int lane, int width) {
+    const int G = cache.n_kv, y = blockIdx.x >> 3;
+    cb = y % a.col_blocks;
+    int item = (y / a.col_blocks) * 8 + (blockIdx.x & 7);
+    none = item >= st.n * G * a.n_parts;
+    if (none) return;
+    hk = item % G; item /= G;
+    part = item % a.n_parts;
+    const int rank = item / a.n_parts;
+    const int mine = lane < st.n ? table_length(tab, lane, cache.page_shift) : -1;
+    int before = 0;
+    for (int j = 0; j < st.n; ++j) {
+      const int other = __builtin_amdgcn_readlane(mine, j);
+      before += other > mine || (other == mine && j < lane);
+    }
+    seq = __builtin_ctzll(__ballot(before == rank && lane < st.n));
+    len = __builtin_amdgcn_readlane(mine, seq);
+    row0 = st.off[seq];
+    m = st.off[seq + 1] - row0;
+    base = (int)((uint32_t)tab.lengths[seq] - (uint32_t)m);
+    const int per = part_entries(len, a.n_parts);
+    start = part * per;
+    end = min_i(len, start + per);
+    parts = max_i(1, (len + per - 1) / per);
+    // without columns; or a part past the end, which the joining kernel knows of (part 0 of an
+    // empty sequence stays)
+    none = cb * width >= m * (a.n_heads / G) || (part > 0 && start >= len);
+  }
+};
+
+__device__ __forceinline__ bool sees(uint64_t word, int draft) { return draft < 0 || (word >> (draft & 63) & 1); }
+
+// --------------------------------------------------------------------------- few columns
 template <typename T, typename C, int DH, int N>
-__global__ __launch_bounds__(64 * kDecodeWaves) void tree_kernel(PagedView cache, PagedTable tab, SeqTable st,
-                                                                 TreeArgs a) {
+__global__ __launch_bounds__(64 * kDecodeWaves) void tree_narrow_kernel(PagedView cache, PagedTable tab, SeqTable st,
+                                                                        TreeArgs a) {
   using Tile = CacheTile<C, DH>;
   constexpr int NW = kDecodeWaves, SP = DH + 4, PIECES = N == 1 ? 3 : 2;
   constexpr bool kFp32 = std::is_same<T, float>::value;
@@ -38,31 +84,13 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void tree_kernel(PagedView cache
   __shared__ __attribute__((aligned(16))) char area[AREA];
   __shared__ float sm[NW][16], sl[NW][16];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int G = cache.n_kv, grp = a.n_heads / G;
-  // an XCD's workgroups: the column blocks of one item, then those of the next.  item =
-  // (rank of the sequence by falling length * G + KV head) * parts + part
-  const int y = blockIdx.x >> 3, cb = y % a.col_blocks;
-  int item = (y / a.col_blocks) * 8 + (blockIdx.x & 7);
-  if (item >= st.n * G * a.n_parts) return;
-  const int part = item % a.n_parts; item /= a.n_parts;
-  const int hk = item % G, rank = item / G;
-  const int mine = lane < st.n ? table_length(tab, lane, cache.page_shift) : -1;
-  int before = 0;
-  for (int j = 0; j < st.n; ++j) {
-    const int other = __builtin_amdgcn_readlane(mine, j);
-    before += other > mine || (other == mine && j < lane);
-  }
-  const int seq = __builtin_ctzll(__ballot(before == rank && lane < st.n));
-  const int len = __builtin_amdgcn_readlane(mine, seq);
-  const int row0 = st.off[seq], m = st.off[seq + 1] - row0, cols = m * grp, c0 = cb * 16 * N;
-  if (c0 >= cols) return;
-  const int base = (int)((uint32_t)tab.lengths[seq] - (uint32_t)m);
-  const int per = part_entries(len, a.n_parts);
-  const int start = part * per, end = min_i(len, start + per);
-  if (part > 0 && start >= len) return;   // the joining kernel knows; part 0 of an empty sequence stays
-  const int32_t* pages = tab.pages + (int64_t)seq * tab.stride;
+  const Share sh(cache, tab, st, a, lane, 16 * N);
+  if (sh.none) return;
+  const int G = cache.n_kv, grp = a.n_heads / G, cols = sh.m * grp, c0 = sh.cb * 16 * N;
+  const int start = sh.start, end = sh.end, base = sh.base;
+  const int32_t* pages = tab.pages + (int64_t)sh.seq * tab.stride;
   const int shift = cache.page_shift, in_mask = (1 << shift) - 1;
-  const int64_t head_at = (int64_t)hk << shift, page_rows = (int64_t)G << shift;
+  const int64_t head_at = (int64_t)sh.hk << shift, page_rows = (int64_t)G << shift;
 
   Tile tile;
   typename Tile::Query query[N];
@@ -71,8 +99,9 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void tree_kernel(PagedView cache
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     const int c = min_i(c0 + n * 16 + col, cols - 1), j = c / grp;
-    Tile::load_q(query[n], (const T*)a.q + (int64_t)(row0 + j) * a.q_rs + (int64_t)(hk * grp + c - j * grp) * DH, lane);
-    word[n] = a.masks ? a.masks[row0 + j] : (2ull << j) - 1;
+    Tile::load_q(query[n], (const T*)a.q + (int64_t)(sh.row0 + j) * a.q_rs + (int64_t)(sh.hk * grp + c - j * grp) * DH,
+                 lane);
+    word[n] = a.masks ? a.masks[sh.row0 + j] : (2ull << j) - 1;
   }
   f32x4_t o[N][Tile::ND];
   float R[N], l[N];
@@ -110,6 +139,21 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void tree_kernel(PagedView cache
     if (end - p.k0 < 32) wh.seen &= (1u << (end - p.k0)) - 1u;
     return wh;
   };
+  // scores of what is not seen, or by the mask not seen by the column, are -inf
+  const auto hide = [&](f32x4_t (*s)[2], int k0, uint32_t seen) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int at = k0 + t * 16 + 4 * g - base;   // draft of the lane's first entry of this half
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!(seen >> (t * 16 + 4 * g + i) & 1) || !sees(word[n], at + i)) s[n][t][i] = -INFINITY;
+    }
+  };
+  const auto weight = [&](float s, float ref) {
+    return kFp32 ? exp_diff_exact(s * a.scale - ref, unit) : __builtin_amdgcn_exp2f(fmaf(s, c2, -ref));
+  };
   // loads run a tile ahead, their pages two, as in the attention of one token
   Where cur{}, nxt{};
   Pages ahead{};
@@ -120,42 +164,15 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void tree_kernel(PagedView cache
     nxt = where(pages_of(first + step));
     ahead = pages_of(first + 2 * step);
   }
+  bool poison = false;
   for (int k0 = first; k0 < end; k0 += step) {
-    const Where was = cur;
+    const uint32_t seen = cur.seen;
     f32x4_t s[N][2];
     tile.template scores<N>(query, s);
     tile.load_k(cache, nxt.r0, nxt.r1, lane);
-    if constexpr (kFp32) {
-#pragma unroll
-      for (int n = 0; n < N; ++n)
-#pragma unroll
-        for (int t = 0; t < 2; ++t) s[n][t] *= a.scale;
-    }
-    bool poison = false;
-    if (was.seen != 0xffffffffu) {
-      tile.clear_values(was.seen, lane);
-#pragma unroll
-      for (int n = 0; n < N; ++n)
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (!(was.seen >> (t * 16 + 4 * g + i) & 1)) s[n][t][i] = -INFINITY;
-    }
-    if (k0 + 32 > base) {   // drafts among the entries
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int at = k0 + t * 16 + 4 * g - base;   // draft of the lane's first entry of this half
-#pragma unroll
-        for (int n = 0; n < N; ++n)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int d = at + i;
-            if (d >= 0 && !(word[n] >> (d & 63) & 1)) s[n][t][i] = -INFINITY;
-          }
-      }
-      poison = __ballot(tile.take_out(0)) != 0;
-    }
+    if (seen != 0xffffffffu) tile.clear_values(seen, lane);
+    if (seen != 0xffffffffu || k0 + 32 > base) hide(s, k0, seen);
+    if (k0 + 32 > base) poison |= tile.take_out_values(0);   // drafts among the entries
     cur = nxt;
     if constexpr (Tile::kStaged) {
       tile.stage_v(area + w * Tile::LDS, lane);
@@ -163,24 +180,21 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void tree_kernel(PagedView cache
     }
     nxt = where(ahead);
     ahead = pages_of(k0 + 3 * step);
-    // weights
+    float mx[N];
     bool above = false;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      float mx = s[n][0][0];
+      mx[n] = s[n][0][0];
 #pragma unroll
-      for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[n][i >> 2][i & 3]);
-      above |= kFp32 ? mx > R[n] + kRaise : fmaf(mx, c2, -R[n]) > kRaise * kLog2e - (float)bits;
+      for (int i = 1; i < 8; ++i) mx[n] = fmaxf(mx[n], s[n][i >> 2][i & 3]);
+      above |= kFp32 ? mx[n] * a.scale > R[n] + kRaise : fmaf(mx[n], c2, -R[n]) > kRaise * kLog2e - (float)bits;
     }
     if (__ballot(above)) {
 #pragma unroll
       for (int n = 0; n < N; ++n) {
-        float mx = s[n][0][0];
-#pragma unroll
-        for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[n][i >> 2][i & 3]);
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        const float to = fmaxf(R[n], kFp32 ? mx : fmaf(mx, c2, (float)bits));
+        float x = fmaxf(mx[n], __shfl_xor(mx[n], 16, 64));
+        x = fmaxf(x, __shfl_xor(x, 32, 64));
+        const float to = fmaxf(R[n], kFp32 ? x * a.scale : fmaf(x, c2, (float)bits));
         const float corr = kFp32 ? exp_diff(R[n] - to) : __builtin_amdgcn_exp2f(R[n] - to);
         R[n] = to;
         l[n] *= corr;
@@ -194,36 +208,42 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void tree_kernel(PagedView cache
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          s[n][t][i] = kFp32 ? exp_diff_exact(s[n][t][i] - R[n], unit)
-                             : __builtin_amdgcn_exp2f(fmaf(s[n][t][i], c2, -R[n]));
+          s[n][t][i] = weight(s[n][t][i], R[n]);
           l[n] += s[n][t][i];
         }
     tile.template values<N, PIECES>(s, o, area + w * Tile::LDS, lane);
-    if (poison) {
+    if constexpr (!Tile::kStaged) tile.load_v(cache, cur.r0, cur.r1, lane);
+  }
+  if (__ballot(poison)) {
+    for (int k0 = first; k0 < end; k0 += step) {
+      if (k0 + 32 <= base) continue;
+      const Where wh = where(pages_of(k0));
+      tile.load_k(cache, wh.r0, wh.r1, lane);
+      f32x4_t s[N][2];
+      tile.template scores<N>(query, s);
+      hide(s, k0, wh.seen);
 #pragma unroll
       for (int n = 0; n < N; ++n)
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[n][t][i] = s[n][t][i] > 0.f ? 3.3e38f : 0.f;   // times 2: an infinity
+          for (int i = 0; i < 4; ++i) s[n][t][i] = weight(s[n][t][i], R[n]) > 0.f ? kHuge : 0.f;
       for (int sign = 1; sign >= -1; sign -= 2) {
-        Tile x;
-        x.load_v(cache, was.r0, was.r1, lane);
-        if (was.seen != 0xffffffffu) x.clear_values(was.seen, lane);
-        x.take_out(sign);
-        if constexpr (Tile::kStaged) x.stage_v(area + w * Tile::LDS, lane);
+        tile.load_v(cache, wh.r0, wh.r1, lane);
+        tile.clear_values(wh.seen, lane);
+        tile.take_out_values(sign);
+        if constexpr (Tile::kStaged) tile.stage_v(area + w * Tile::LDS, lane);
 #pragma unroll
         for (int n = 0; n < N; ++n) {   // sums of their own: an infinity in o would swallow the other one
           f32x4_t add[1][Tile::ND];
 #pragma unroll
           for (int i = 0; i < Tile::ND; ++i) add[0][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-          x.template values<1, PIECES>(s + n, add, area + w * Tile::LDS, lane);
+          tile.template values<1, PIECES>(s + n, add, area + w * Tile::LDS, lane);
 #pragma unroll
           for (int i = 0; i < Tile::ND; ++i) o[n][i] += add[0][i];
         }
       }
     }
-    if constexpr (!Tile::kStaged) tile.load_v(cache, cur.r0, cur.r1, lane);
   }
   float* so = (float*)area;
 #pragma unroll
@@ -254,15 +274,340 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void tree_kernel(PagedView cache
       // nothing seen: 0, with a log-sum-exp of -inf (a NaN sum stays NaN)
       v = L == 0.f ? 0.f : v / L;
       const float lse = L == 0.f ? -INFINITY : kFp32 ? M + logf(L / unit) : fmaf(M, 0.6931471805599453f, logf(L));
-      const int j = c / grp, h = hk * grp + c - j * grp;
-      const int64_t at = (int64_t)(row0 + j) * a.n_heads + h;
-      if (a.n_parts == 1) {
-        Act<T>::store((T*)a.out + (int64_t)(row0 + j) * a.out_rs + (int64_t)h * DH + x, v);
+      const int j = c / grp, h = sh.hk * grp + c - j * grp;
+      const int64_t at = (int64_t)(sh.row0 + j) * a.n_heads + h;
+      if (sh.parts == 1) {
+        Act<T>::store((T*)a.out + (int64_t)(sh.row0 + j) * a.out_rs + (int64_t)h * DH + x, v);
         if (a.lse && x == 0) a.lse[at] = lse;
       } else {
-        a.part_o[(at * a.n_parts + part) * DH + x] = v;
-        if (x == 0) a.part_lse[at * a.n_parts + part] = lse;
+        a.part_o[(at * a.n_parts + sh.part) * DH + x] = v;
+        if (x == 0) a.part_lse[at * a.n_parts + sh.part] = lse;
       }
+    }
+  }
+}
+
+// --------------------------------------------------------------------------- many columns
+// A workgroup's tile of 64 entries in LDS as bf16, K and V, 8-bit rows widened on the way.  Each
+// thread brings the same pieces of every tile; the 16 entries of a granule lie on one page, and a
+// wave's i-th piece lies in one granule.
+template <typename C, int DH> struct WideTile {
+  static constexpr int ROWS = 64, NT = 64 * kDecodeWaves;
+  static constexpr int CH = DH / 8;                         // 16-byte pieces of a row in LDS
+  static constexpr int PB = DH * (int)sizeof(C) / 16;       // and of the cache
+  static constexpr int NP = ROWS * PB / NT;                 // pieces of a thread
+  static constexpr int BYTES = ROWS * DH * 2;               // of K, and of V
+  static constexpr bool kScaled = std::is_same<C, e4m3_t>::value;
+  v4u k[NP], v[NP];
+  uint32_t ks[kScaled ? NP : 1], vs[kScaled ? NP : 1];
+
+  static __device__ __forceinline__ int row_of(int i, int tid) { return (i * NT + tid) / PB; }
+  static __device__ __forceinline__ int granule(int i, int w) { return (i * NT + w * 64) / PB / 16; }
+  static __device__ __forceinline__ int k_swz(int row) { return DH == 128 ? row & 15 : (row >> 1) & 7; }
+
+  // at[i]: the cache's row at which granule(i, w) begins
+  __device__ __forceinline__ void load(const PagedView& cache, const int64_t* at, int tid) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int in = row_of(i, tid) & 15, piece = tid % PB;
+      const uint32_t off = (uint32_t)(in * PB + piece) * 16;
+      k[i] = *(const v4u*)((const char*)cache.k + at[i] * (PB * 16) + off);
+      v[i] = *(const v4u*)((const char*)cache.v + at[i] * (PB * 16) + off);
+      if constexpr (kScaled) {
+        ks[i] = (cache.k_scales + at[i])[in];
+        vs[i] = (cache.v_scales + at[i])[in];
+      }
+    }
+  }
+  __device__ __forceinline__ void clear_values(uint64_t seen, int tid) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+      if (!(seen >> row_of(i, tid) & 1)) {
+        v[i] = v4u{0, 0, 0, 0};
+        if constexpr (kScaled) vs[i] = 127;
+      }
+  }
+  __device__ __forceinline__ bool take_out_values(int sign) {
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      any |= take_out<C>(v[i], sign);
+      if constexpr (kScaled)
+        if (sign != 0) vs[i] = 127;
+    }
+    return any;
+  }
+  __device__ __forceinline__ void store(char* lds, int tid) const {
+    char *lk = lds, *lv = lds + BYTES;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int row = row_of(i, tid), piece = tid % PB;
+      const int kx = k_swz(row), vx = StagedValues<DH>::swz(row);
+      if constexpr (kScaled) {
+        const float sk = e4m3_scale(ks[i]), sv = e4m3_scale(vs[i]);
+        *(v4u*)(lk + (row * CH + ((2 * piece) ^ kx)) * 16) = e4m3_to_bf16(k[i][0], k[i][1], sk);
+        *(v4u*)(lk + (row * CH + ((2 * piece + 1) ^ kx)) * 16) = e4m3_to_bf16(k[i][2], k[i][3], sk);
+        *(v4u*)(lv + (row * CH + ((2 * piece) ^ vx)) * 16) = e4m3_to_bf16(v[i][0], v[i][1], sv);
+        *(v4u*)(lv + (row * CH + ((2 * piece + 1) ^ vx)) * 16) = e4m3_to_bf16(v[i][2], v[i][3], sv);
+      } else {
+        *(v4u*)(lk + (row * CH + (piece ^ kx)) * 16) = k[i];
+        *(v4u*)(lv + (row * CH + (piece ^ vx)) * 16) = v[i];
+      }
+    }
+  }
+};
+
+// A wave has 16 N columns.  For each 32 entries it forms the weights of the scores (vector unit)
+// and then multiplies them with the values, and the next 32 entries' keys with its queries
+// (matrix unit).  The waves read all of K and V from LDS; 32 columns a wave keep that below what
+// the products take.
+template <typename C, int DH, int N>
+__global__ __launch_bounds__(64 * kDecodeWaves, 2) void tree_wide_kernel(PagedView cache, PagedTable tab, SeqTable st,
+                                                                         TreeArgs a) {
+  using Tile = WideTile<C, DH>;
+  using Values = StagedValues<DH>;
+  constexpr int NW = kDecodeWaves, ND = DH / 16, NC = DH / 32, CH = DH / 8, ROWS = Tile::ROWS;
+  __shared__ __attribute__((aligned(16))) char area[2][2 * Tile::BYTES];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Share sh(cache, tab, st, a, lane, 16 * N * NW);
+  if (sh.none) return;
+  const int G = cache.n_kv, grp = a.n_heads / G, cols = sh.m * grp, c0 = (sh.cb * NW + w) * 16 * N;
+  const int start = sh.start, end = sh.end, base = sh.base;
+  const int32_t* pages = tab.pages + (int64_t)sh.seq * tab.stride;
+  const int shift = cache.page_shift, in_mask = (1 << shift) - 1;
+  const int64_t head_at = (int64_t)sh.hk << shift, page_rows = (int64_t)G << shift;
+  const bool busy = c0 < cols;   // the other waves only bring their pieces
+  const int col = lane & 15, g = lane >> 4;
+
+  v4u query[N][NC];
+  uint64_t word[N];
+  f32x4_t o[N][ND];
+  float R[N], l[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int c = min_i(c0 + n * 16 + col, cols - 1), j = c / grp;
+    const bf16_t* q = (const bf16_t*)a.q + (int64_t)(sh.row0 + j) * a.q_rs + (int64_t)(sh.hk * grp + c - j * grp) * DH;
+#pragma unroll
+    for (int x = 0; x < NC; ++x) query[n][x] = *(const v4u*)(q + x * 32 + g * 8);
+    word[n] = a.masks ? a.masks[sh.row0 + j] : (2ull << j) - 1;
+    R[n] = kUnset;
+    l[n] = 0.f;
+#pragma unroll
+    for (int i = 0; i < ND; ++i) o[n][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  const int bits = 32 - __builtin_clz(max_i(end - start, 1)) + 12;
+  const float c2 = a.scale * kLog2e;
+  // the pages of a tile's granules, one in each of lanes 0 .. 3 (past the end: the last one's)
+  const auto pages_of = [&](int k0) { return pages[min_i(k0 + 16 * (lane & 3), end - 1) >> shift]; };
+  const auto seen_of = [&](int page, int k0) {
+    const uint64_t b = __ballot(page >= 0 && page < cache.n_pages);
+    uint64_t seen = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) seen |= (b >> j & 1 ? 0xffffull : 0ull) << (16 * j);
+    return end - k0 < 64 ? seen & ((1ull << (end - k0)) - 1) : seen;
+  };
+  const auto rows_of = [&](int page, int k0, int64_t* at) {
+#pragma unroll
+    for (int i = 0; i < Tile::NP; ++i) {
+      const int gr = Tile::granule(i, w), p = __builtin_amdgcn_readlane(page, gr);
+      at[i] = (p >= 0 && p < cache.n_pages ? p : 0) * page_rows + head_at + ((k0 + 16 * gr) & in_mask);
+    }
+  };
+  // scores of 32 entries, rows `first` .. of the tile in LDS
+  const auto scores = [&](f32x4_t (*s)[2], const char* lds, int first) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int row = first + t * 16 + col;
+#pragma unroll
+      for (int n = 0; n < N; ++n) s[n][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < NC; ++x) {
+        const v4u key = *(const v4u*)(lds + (row * CH + ((x * 4 + g) ^ Tile::k_swz(row))) * 16);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+          s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, key),
+                                                            __builtin_bit_cast(bf16x8_t, query[n][x]), s[n][t], 0, 0, 0);
+      }
+    }
+  };
+  // .. of entries k0 .. of which `seen` count
+  const auto hide = [&](f32x4_t (*s)[2], int k0, uint32_t seen) {
+    if (seen == 0xffffffffu && k0 + 32 <= base) return;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int at = k0 + t * 16 + 4 * g - base;
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (!(seen >> (t * 16 + 4 * g + i) & 1) || !sees(word[n], at + i)) s[n][t][i] = -INFINITY;
+    }
+  };
+  const auto raise = [&](const f32x4_t (*s)[2]) {
+    float mx[N];
+    bool above = false;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      mx[n] = s[n][0][0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) mx[n] = fmaxf(mx[n], s[n][i >> 2][i & 3]);
+      above |= fmaf(mx[n], c2, -R[n]) > kRaise * kLog2e - (float)bits;
+    }
+    if (!__ballot(above)) return;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      float x = fmaxf(mx[n], __shfl_xor(mx[n], 16, 64));
+      x = fmaxf(x, __shfl_xor(x, 32, 64));
+      const float to = fmaxf(R[n], fmaf(x, c2, (float)bits));
+      const float corr = __builtin_amdgcn_exp2f(R[n] - to);
+      R[n] = to;
+      l[n] *= corr;
+#pragma unroll
+      for (int i = 0; i < ND; ++i) o[n][i] *= corr;
+    }
+  };
+  const auto weights = [&](f32x4_t (*s)[2], v4u (*part)[2]) {
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[n][t][i] = __builtin_amdgcn_exp2f(fmaf(s[n][t][i], c2, -R[n]));
+          l[n] += s[n][t][i];
+        }
+    Values::template pieces<N, 2>(s, part);
+  };
+  Tile tile;
+  bool poison = false;
+  const auto bring = [&](char* lds, int k0, uint64_t seen, int sign) {   // the tile's registers to LDS
+    if (seen != ~0ull) tile.clear_values(seen, tid);
+    if (k0 + ROWS > base) poison |= tile.take_out_values(sign);
+    tile.store(lds, tid);
+  };
+  int64_t at[Tile::NP];
+  uint64_t seen = 0, seen_next = 0;
+  int ahead = 0;
+  if (start < end) {
+    const int page = pages_of(start);
+    seen = seen_of(page, start);
+    rows_of(page, start, at);
+    tile.load(cache, at, tid);
+    ahead = pages_of(start + ROWS);
+    bring(area[0], start, seen, 0);
+  }
+  // the queries have arrived: left to the loop, the wait for them would be one for the next
+  // tile's loads, in every turn
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int x = 0; x < NC; ++x) asm volatile("" : "+v"(query[n][x]));
+  __syncthreads();
+  f32x4_t s[N][2];      // scores of 32 entries
+  v4u part[N][2];       // their weights
+  if (busy && start < end) scores(s, area[0], 0);
+  int buf = 0;
+  // half 0 or 1 of the tile in area[buf]
+  const auto weigh = [&](int k0, int half) {
+    hide(s, k0 + 32 * half, (uint32_t)(seen >> 32 * half));
+    raise(s);
+    weights(s, part);
+  };
+  const auto load_next = [&](int k0) {    // the tile at k0 to registers, if there is one
+    if (k0 >= end) return;
+    seen_next = seen_of(ahead, k0);
+    rows_of(ahead, k0, at);
+    tile.load(cache, at, tid);
+    ahead = pages_of(k0 + ROWS);
+  };
+  load_next(start + ROWS);
+  for (int k0 = start; k0 < end; k0 += ROWS, buf ^= 1) {
+    const bool more = k0 + ROWS < end;
+    const char* values = area[buf] + Tile::BYTES;
+    if (busy) {
+      weigh(k0, 0);
+      __builtin_amdgcn_s_setprio(1);
+      scores(s, area[buf], 32);
+      Values::template add<N, 2>(part, o, values, lane);
+      __builtin_amdgcn_s_setprio(0);
+    }
+    const uint64_t then = seen_next;
+    if (more) bring(area[buf ^ 1], k0 + ROWS, then, 0);
+    load_next(k0 + 2 * ROWS);
+    __syncthreads();
+    if (busy) {
+      weigh(k0, 1);
+      __builtin_amdgcn_s_setprio(1);
+      if (more) scores(s, area[buf ^ 1], 0);
+      Values::template add<N, 2>(part, o, values + Tile::BYTES / 2, lane);
+      __builtin_amdgcn_s_setprio(0);
+    }
+    seen = then;
+    __syncthreads();   // the tile is done with
+  }
+  if (__syncthreads_or(poison)) {
+    for (int k0 = start; k0 < end; k0 += ROWS) {
+      if (k0 + ROWS <= base) continue;
+      const int page = pages_of(k0);
+      seen = seen_of(page, k0);
+      rows_of(page, k0, at);
+      for (int sign = 1; sign >= -1; sign -= 2) {
+        tile.load(cache, at, tid);
+        bring(area[0], k0, seen, sign);
+        __syncthreads();
+        if (busy) {
+          for (int half = 0; half < 2; ++half) {
+            scores(s, area[0], 32 * half);
+            hide(s, k0 + 32 * half, (uint32_t)(seen >> 32 * half));
+#pragma unroll
+            for (int n = 0; n < N; ++n) {   // sums of their own: an infinity in o would swallow the other one
+              v4u huge[1][1];
+              f32x4_t sum[1][ND];
+#pragma unroll
+              for (int e = 0; e < 8; e += 2) {
+                const float x = __builtin_amdgcn_exp2f(fmaf(s[n][e >> 2][e & 3], c2, -R[n]));
+                const float y = __builtin_amdgcn_exp2f(fmaf(s[n][e >> 2][(e & 3) + 1], c2, -R[n]));
+                huge[0][0][e / 2] = (x > 0.f ? kHugeBits : 0u) | (y > 0.f ? kHugeBits << 16 : 0u);
+              }
+#pragma unroll
+              for (int i = 0; i < ND; ++i) sum[0][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+              Values::template add<1, 1>(huge, sum, area[0] + Tile::BYTES + half * (Tile::BYTES / 2), lane);
+#pragma unroll
+              for (int i = 0; i < ND; ++i) o[n][i] += sum[0][i];
+            }
+          }
+        }
+        __syncthreads();
+      }
+    }
+  }
+  if (!busy) return;
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    l[n] += __shfl_xor(l[n], 16, 64);
+    l[n] += __shfl_xor(l[n], 32, 64);
+    const int c = c0 + n * 16 + col;
+    if (c >= cols) continue;
+    const float L = l[n], inv = L == 0.f ? 0.f : 1.f / L;   // nothing seen: 0, with a log-sum-exp of -inf
+    const float lse = L == 0.f ? -INFINITY : fmaf(R[n], 0.6931471805599453f, logf(L));
+    const int j = c / grp, h = sh.hk * grp + c - j * grp;
+    const int64_t row = (int64_t)(sh.row0 + j) * a.n_heads + h;
+    if (sh.parts == 1) {
+      bf16_t* out = (bf16_t*)a.out + (int64_t)(sh.row0 + j) * a.out_rs + (int64_t)h * DH + 4 * g;
+#pragma unroll
+      for (int i = 0; i < ND; ++i) {
+        v2u u;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          u[e] = (uint32_t)f2bf(o[n][i][2 * e] * inv) | ((uint32_t)f2bf(o[n][i][2 * e + 1] * inv) << 16);
+        *(v2u*)(out + 16 * i) = u;
+      }
+      if (a.lse && g == 0) a.lse[row] = lse;
+    } else {
+      float* out = a.part_o + (row * a.n_parts + sh.part) * DH + 4 * g;
+#pragma unroll
+      for (int i = 0; i < ND; ++i) *(f32x4_t*)(out + 16 * i) = o[n][i] * inv;
+      if (g == 0) a.part_lse[row * a.n_parts + sh.part] = lse;
     }
   }
 }
@@ -277,7 +622,8 @@ __global__ __launch_bounds__(256) void tree_join_kernel(PagedTable tab, SeqTable
   if (at >= (int64_t)st.rows * a.n_heads) return;
   const int row = (int)(at / a.n_heads), h = (int)(at - (int64_t)row * a.n_heads);
   const int len = table_length(tab, seq_of_row(st, row), page_shift);
-  const int per = part_entries(len, a.n_parts), n = max_i(1, (len + per - 1) / per);
+  const int per = part_entries(len, a.n_parts), n = (len + per - 1) / per;
+  if (n <= 1) return;   // the one part has written the output
   const float* lse = a.part_lse + at * a.n_parts;
   const float* po = a.part_o + at * a.n_parts * DH + x;
   float M = -INFINITY;
@@ -299,41 +645,63 @@ __global__ __launch_bounds__(256) void tree_join_kernel(PagedTable tab, SeqTable
   if (a.lse && x == 0) a.lse[at] = L == 0.f ? -INFINITY : ref + logf(L * kMaxTreeParts);
 }
 
-// Column blocks of 16 of a workgroup, for the widest tree of a call.
-int tree_width(const PagedView& cache, int max_drafts, int n_heads) {
-  const int cols = max_drafts * (n_heads / cache.n_kv);
-  return cols <= 16 ? 1 : cols <= 32 || !cache.bf16 ? 2 : 4;
+// Columns of a workgroup, for the widest tree of a call, and whether its waves share their tiles.
+struct Width {
+  int columns;
+  bool shared;
+};
+Width width_of(const PagedView& cache, int max_drafts, int n_heads) {
+  const int64_t cols = (int64_t)max_drafts * (n_heads / cache.n_kv);
+  if (cols <= 16) return {16, false};
+  if (!cache.bf16) return {32, false};
+  return {cols <= 64 ? 64 : 128, true};
 }
 
-// Parts of a length: enough for the CUs, none shorter than 512 entries.
+}  // namespace
+
+// Parts of a length: two workgroups to a CU, in parts of 256 entries or more (of a workgroup whose
+// waves share their tiles; 512 otherwise, as in the attention of one token); and twice as many
+// of 1024 or more (512 of 64 channels), so that unequal lengths level out: what a part costs,
+// its fp32 outputs written and read again, has to be little beside its entries.
+//   2 x 8192 entries, 64 columns of 128: 16 parts of 512 29.0, 32 of 256 28.5; 16 columns: 23.6 and 32.1;
+//   4 x 1000, 104 columns: 1 part 54.5, 3 30.1; 16 x 4096, 64 columns: 4 parts 72, 8 84;
+//   16 x 100 .. 8192, 256 columns: 2 parts 190, 4 150, 8 180 (all of 4096: 146, 157, 185);
+//   16 x 100 .. 2048, 32 columns of 64: 2 parts 29.2, 4 22.2.
 int tree_parts(const PagedView& cache, int n_seqs, int max_drafts, int n_heads, int64_t max_entries) {
-  const int width = 16 * tree_width(cache, max_drafts, n_heads), cols = max_drafts * (n_heads / cache.n_kv);
-  const int64_t rows = (int64_t)n_seqs * cache.n_kv * ((cols + width - 1) / width);
-  const int64_t want = 512 / std::max<int64_t>(rows, 1);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, max_entries / 512), kMaxTreeParts));
+  const Width width = width_of(cache, max_drafts, n_heads);
+  const int64_t cols = (int64_t)max_drafts * (n_heads / cache.n_kv);
+  const int64_t rows = (int64_t)n_seqs * cache.n_kv * ((cols + width.columns - 1) / width.columns);
+  const int64_t least = std::max(512, 8 * cache.head_dim);
+  const int64_t fill = std::min(512 / rows, max_entries / (width.shared ? 256 : 512));
+  const int64_t level = std::min(1024 / rows, max_entries / least);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::max(fill, level), kMaxTreeParts));
 }
 
 int64_t tree_blocks(const PagedView& cache, const SeqTable& st, const TreeArgs& a) {
-  const int64_t cols = (int64_t)st.max_len * (a.n_heads / cache.n_kv), width = 16 * tree_width(cache, st.max_len, a.n_heads);
+  const int64_t cols = (int64_t)st.max_len * (a.n_heads / cache.n_kv), width = width_of(cache, st.max_len, a.n_heads).columns;
   const int64_t items = (int64_t)st.n * cache.n_kv * a.n_parts;
   return (items + 7) / 8 * 8 * ((cols + width - 1) / width);
 }
 
 hipError_t launch_tree(const PagedView& cache, const PagedTable& tab, const SeqTable& st, TreeArgs a, hipStream_t s) {
-  const int cols = st.max_len * (a.n_heads / cache.n_kv), N = tree_width(cache, st.max_len, a.n_heads);
-  a.col_blocks = (cols + 16 * N - 1) / (16 * N);
+  const Width width = width_of(cache, st.max_len, a.n_heads);
+  a.col_blocks = (int)(((int64_t)st.max_len * (a.n_heads / cache.n_kv) + width.columns - 1) / width.columns);
   const uint32_t blocks = (uint32_t)tree_blocks(cache, st, a);
   const int64_t outs = (int64_t)st.rows * a.n_heads;
-#define RK_TREE(T, C, DH)                                                                                     \
-  do {                                                                                                        \
-    constexpr int kWide = std::is_same<T, float>::value ? 2 : 4;                                              \
-    if (N == 1) tree_kernel<T, C, DH, 1><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, st, a);             \
-    else if (N == 2) tree_kernel<T, C, DH, 2><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, st, a);        \
-    else tree_kernel<T, C, DH, kWide><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, st, a);                \
-    if (a.n_parts > 1) {                                                                                      \
-      const int groups = 256 / (DH / 4);                                                                      \
+#define RK_TREE(T, C, DH)                                                                                          \
+  do {                                                                                                             \
+    if constexpr (std::is_same<T, float>::value) {                                                                 \
+      if (width.columns == 16) tree_narrow_kernel<T, C, DH, 1><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, st, a); \
+      else tree_narrow_kernel<T, C, DH, 2><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, st, a);                \
+    } else {                                                                                                       \
+      if (!width.shared) tree_narrow_kernel<T, C, DH, 1><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, st, a);  \
+      else if (width.columns == 64) tree_wide_kernel<C, DH, 1><<<blocks, 256, 0, s>>>(cache, tab, st, a);       \
+      else tree_wide_kernel<C, DH, 2><<<blocks, 256, 0, s>>>(cache, tab, st, a);                                \
+    }                                                                                                              \
+    if (a.n_parts > 1) {                                                                                           \
+      const int groups = 256 / (DH / 4);                                                                           \
       tree_join_kernel<T, DH><<<(uint32_t)((outs + groups - 1) / groups), 256, 0, s>>>(tab, st, a, cache.page_shift); \
-    }                                                                                                         \
+    }                                                                                                              \
   } while (0)
   RK_PAGED_DISPATCH(cache, RK_TREE);
 #undef RK_TREE
