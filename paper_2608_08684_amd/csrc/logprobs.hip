@@ -552,124 +552,187 @@ hipError_t launch_logprobs(const LogprobArgs& a, bool bf16, hipStream_t s) {
 }
 
 // --------------------------------------------------------------------------- beams
-// Of a group's candidates (beam b, token v) with score_b + x_v - c_b - log S_b the n_out best.
+// Of a group's candidates (beam b, token v) with score_b + (x_v - c_b) - log S_b the n_out best.
 // A candidate of the group's n_out best is one of its own row's: logprob_kernel leaves each
-// row's (each part's) best logits in falling order, and one workgroup per group chooses among
-// these lists.  Scores between beams are doubles of the logit, so that the order hangs on
-// nothing but log S; within a beam the logits themselves decide.
-//
-// A candidate's place is the number of candidates before it, counted against all of them at
-// once.  For more than 256 candidates, a bound first: with L lists the first k = ceil(n_out /
-// L) of each are n_out at least, so the n_out-th of those has n_out - 1 before it, and what
-// comes after it is out.  No more than n_out lists then have any left (or, where L < n_out,
-// there are L), n_out at most of each: 1024.
-// Bound: latency, a chain of loads, joins and counts, 4 us; the rows' kernel before it reads
-// every logit once.
+// row's (each part's) best logits in falling order, and a workgroup per group merges these lists:
+// lane l of its first wave holds the head of list l, and n_out times the best head is taken and
+// its list moved on.  More than 64 lists (rows in many parts) are first cut to the 64 with the
+// best heads: a list with n_out better heads beside it gives nothing.  Scores between beams are
+// doubles of the logit, so that the order hangs on nothing but log S; within a beam the logits
+// decide.
+// Bound: latency, a chain of loads, sums and n_out short steps, LAT us for 8 of 8 beams; the
+// rows' kernel before it reads every logit once.
 // (lists: 256 where rows are split to fill the card, 17 a row of 2^22 fp32 logits)
-constexpr int kMaxLists = 17 * RK_MAX_BEAMS, kMaxLeft = RK_MAX_TOP * RK_MAX_TOP;
+constexpr int kMaxLists = 17 * RK_MAX_BEAMS;
 
-struct Candidates {
-  double score[kMaxLeft];
-  uint64_t key[kMaxLeft];    // order of the logit and complement of the token
-  int beam[kMaxLeft];
-  __device__ __forceinline__ bool before(int i, double s, int b, uint64_t k) const {
-    return score[i] > s || (score[i] == s && (beam[i] < b || (beam[i] == b && key[i] > k)));
+// log of a positive finite sum: the exponent's part in double, the rest below 0.7
+__device__ __forceinline__ double log_sum(float s) {
+  const int e = (int)(__float_as_uint(s) >> 23) - 127;
+  const float m = __uint_as_float((__float_as_uint(s) & 0x7fffffu) | 0x3f800000u);
+  return e * 0.69314718055994530942 + (double)logf(m);
+}
+
+// A candidate as a whole number that orders like its score, 0 for none; its logit's order with
+// the complement of the token; its beam.
+struct Candidate {
+  uint64_t score, key;
+  int beam;
+  __device__ __forceinline__ void set(double s, uint64_t k, int b) {
+    const uint64_t u = (uint64_t)__double_as_longlong(s + 0.0);   // -0 and 0 are one score
+    score = s > -INFINITY ? (u >> 63 ? ~u : u | 0x8000000000000000ull) : 0;
+    key = k;
+    beam = b;
+  }
+  __device__ __forceinline__ double value() const {
+    return __longlong_as_double((long long)(score >> 63 ? score & 0x7fffffffffffffffull : ~score));
+  }
+  __device__ __forceinline__ bool before(const Candidate& o) const {
+    return score > o.score || (score == o.score && (beam < o.beam || (beam == o.beam && key > o.key)));
   }
 };
 
 __global__ __launch_bounds__(256) void beam_join_kernel(LogprobArgs a, BeamArgs p) {
   constexpr int NT = 256;
-  __shared__ Candidates left;
   __shared__ float4 sums[kMaxLists];
+  __shared__ uint64_t list[64 * RK_MAX_TOP];     // the lists of the first wave's lanes
+  __shared__ Candidate heads[kMaxLists];
+  __shared__ int chosen[64];
   // a logit's score is its difference to ref, plus shift; -inf: no candidates
   __shared__ double ref[RK_MAX_BEAMS], shift[RK_MAX_BEAMS];
-  __shared__ int n_left;
-  __shared__ double bound_score;
-  __shared__ uint64_t bound_key;
-  __shared__ int bound_beam;
+  __shared__ float score[RK_MAX_BEAMS];
+  __shared__ uint8_t ended[RK_MAX_BEAMS];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const int nb = p.n_beams, n = a.n_top, lists = nb * a.parts;
+  const int nb = p.n_beams, n = a.n_top, parts = a.parts, lists = nb * parts;
   const int64_t row0 = (int64_t)blockIdx.x * nb;
-  for (int i = tid; i < lists; i += NT) {
-    const int64_t r = row0 + i / a.parts;
-    sums[i] = beam_open(p, r) ? a.part[row0 * a.parts + i] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+  const uint64_t* top = a.part_top + row0 * parts * n;
+  // what closed beams would have in the workspace is whatever was there: not used
+  if (tid < nb) {
+    score[tid] = p.scores[row0 + tid];
+    ended[tid] = p.ended ? p.ended[row0 + tid] : 0;
   }
-  if (tid == 0) { n_left = 0; bound_score = -INFINITY; bound_beam = 0; bound_key = 0; }
+  for (int i = tid; i < lists; i += NT) sums[i] = a.part[row0 * parts + i];
+  if (lists <= 64)
+    for (int i = tid; i < lists * n; i += NT) list[i] = top[i];
   __syncthreads();
-  for (int b = w; b < nb; b += NT / 64) {
-    Sums q{-INFINITY, 0.f, 0.f};
-    if (lane < a.parts) { const float4 f = sums[b * a.parts + lane]; q = Sums{f.x, f.y, f.z}; }
-    q = wave_sums(q);
-    if (lane == 0) {
+  if (parts == 1) {
+    if (tid < nb) {
+      const float4 f = sums[tid];
+      ref[tid] = Sums{f.x, f.y, f.z}.ref();
       // without a finite largest logit S is 0 or NaN
-      ref[b] = q.ref();
-      shift[b] = q.s > 0.f ? (double)p.scores[row0 + b] - log((double)q.s) : -INFINITY;
+      shift[tid] = f.y > 0.f && f.y < INFINITY ? (double)score[tid] - log_sum(f.y) : -INFINITY;
+    }
+  } else {
+    for (int b = w; b < nb; b += NT / 64) {
+      Sums q{-INFINITY, 0.f, 0.f};
+      if (lane < parts) { const float4 f = sums[b * parts + lane]; q = Sums{f.x, f.y, f.z}; }
+      q = wave_sums(q);
+      if (lane == 0) {
+        ref[b] = q.ref();
+        shift[b] = q.s > 0.f && q.s < INFINITY ? (double)score[b] - log_sum(q.s) : -INFINITY;
+      }
     }
   }
   __syncthreads();
-  // candidate i of list l; its score is not above -inf where there is none
-  const auto get = [&](int l, int i, double* s, uint64_t* k) {
-    const int b = l / a.parts;
-    const int64_t r = row0 + b;
-    if (p.ended && p.ended[r]) {
-      *s = l % a.parts == 0 && i == 0 ? (double)p.scores[r] : -INFINITY;
-      *k = (uint32_t)~p.end_token;
-    } else if (shift[b] > -INFINITY) {
-      *k = a.part_top[(row0 * a.parts + l) * n + i];
-      *s = ((double)from_order((uint32_t)(*k >> 32)) - ref[b]) + shift[b];
-    } else {
-      *s = -INFINITY;
-      *k = 0;
-    }
+  // candidate i of list l, whose key the lists have; the next in order has no better score
+  const auto candidate = [&](int l, int i, uint64_t k) {
+    Candidate c;
+    const int b = l / parts;
+    if (!(score[b] > -INFINITY)) c.set(-INFINITY, 0, b);
+    else if (ended[b]) c.set(l - b * parts == 0 && i == 0 ? (double)score[b] : -INFINITY, (uint32_t)~p.end_token, b);
+    else c.set(shift[b] > -INFINITY ? ((double)from_order((uint32_t)(k >> 32)) - ref[b]) + shift[b] : -INFINITY, k, b);
+    return c;
   };
-  const int total = lists * n;
-  if (total > NT) {
-    const int k1 = (p.n_out + lists - 1) / lists, firsts = lists * k1;   // at most max(kMaxLists, 2 n_out)
-    for (int i = tid; i < firsts; i += NT) {
-      const int l = i / k1;
-      left.beam[i] = l / a.parts;
-      if (i - l * k1 < n) get(l, i - l * k1, &left.score[i], &left.key[i]);
-      else { left.score[i] = -INFINITY; left.key[i] = 0; }
+  int held = min(lists, 64), mine = lane;          // lists, and which one this lane has
+  if (lists > 64) {
+    for (int i = tid; i < lists; i += NT) heads[i] = candidate(i, 0, top[(int64_t)i * n]);
+    __syncthreads();
+    bool best[(kMaxLists + NT - 1) / NT];
+#pragma unroll
+    for (int q = 0; q < (kMaxLists + NT - 1) / NT; ++q) {
+      const int i = q * NT + tid;
+      int before = 64;
+      if (i < lists) {
+        const Candidate c = heads[i];
+        before = 0;
+        for (int j = 0; j < lists; ++j) before += heads[j].before(c) || (j < i && !c.before(heads[j]));
+      }
+      best[q] = before < 64;
     }
     __syncthreads();
-    for (int i = tid; i < firsts; i += NT) {
-      const double s = left.score[i];
-      if (!(s > -INFINITY)) continue;
-      int before = 0;
-      for (int j = 0; j < firsts; ++j) before += left.before(j, s, left.beam[i], left.key[i]);
-      if (before == p.n_out - 1) { bound_score = s; bound_beam = left.beam[i]; bound_key = left.key[i]; }
+#pragma unroll
+    for (int q = 0; q < (kMaxLists + NT - 1) / NT; ++q)
+      if (q * NT + tid < lists) heads[q * NT + tid].beam = best[q] ? 1 : 0;   // from here on: whether it is taken
+    __syncthreads();
+    if (w == 0) {   // in their order
+      int taken = 0;
+      for (int i0 = 0; i0 < lists; i0 += 64) {
+        const bool t = i0 + lane < lists && heads[i0 + lane].beam;
+        const uint64_t m = __ballot(t);
+        if (t) chosen[taken + __popcll(m & ((1ull << lane) - 1))] = i0 + lane;
+        taken += __popcll(m);
+      }
     }
     __syncthreads();
+    mine = chosen[lane];
+    for (int i = tid; i < 64 * n; i += NT) list[i] = top[(int64_t)chosen[i / n] * n + i % n];
+    __syncthreads();
   }
-  for (int i = tid; i < total; i += NT) {
-    const int l = i / n, b = l / a.parts;
-    double s;
-    uint64_t k;
-    get(l, i - l * n, &s, &k);
-    const bool after = s < bound_score || (s == bound_score && (b > bound_beam || (b == bound_beam && k < bound_key)));
-    if (!(s > -INFINITY) || (bound_score > -INFINITY && after)) continue;
-    const int at = atomicAdd(&n_left, 1);
-    if (at < kMaxLeft) { left.score[at] = s; left.key[at] = k; left.beam[at] = b; }
+  if (w != 0) return;
+  Candidate c;
+  c.set(-INFINITY, 0, 0);
+  int next = 0;
+  if (lane < held) c = candidate(mine, 0, list[lane * n]);
+  int parent = -1, token = -1;
+  float value = -INFINITY;                         // of place `lane`
+  for (int i = 0; i < p.n_out; ++i) {
+    const uint32_t hi = wave_max((uint32_t)(c.score >> 32));
+    if (hi == 0) break;                            // (a score's upper half is not 0)
+    const bool up = (uint32_t)(c.score >> 32) == hi;
+    const uint32_t lo = wave_max(up ? (uint32_t)c.score : 0);
+    uint64_t m = __ballot(up && (uint32_t)c.score == lo);
+    int win = __builtin_ctzll(m);
+    if (m & (m - 1)) {   // equal scores: the lowest beam, in lanes as in lists; of its parts' the larger key
+      m = __ballot((m >> lane & 1) && c.beam == __builtin_amdgcn_readlane(c.beam, win));
+      uint64_t best = 0;
+      for (; m; m &= m - 1) {
+        const int l = __builtin_ctzll(m);
+        const uint64_t k = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(c.key >> 32), l) << 32 |
+                           (uint32_t)__builtin_amdgcn_readlane((int)c.key, l);
+        if (k > best) { best = k; win = l; }
+      }
+    }
+    const int b = __builtin_amdgcn_readlane(c.beam, win), t = ~__builtin_amdgcn_readlane((int)c.key, win);
+    if (lane == i) {
+      Candidate best;
+      best.score = (uint64_t)hi << 32 | lo;
+      parent = b;
+      token = t;
+      value = (float)best.value();
+    }
+    if (lane == win) {
+      ++next;
+      if (next < n) c = candidate(mine, next, list[lane * n + next]);
+      else c.score = 0;
+    }
   }
-  __syncthreads();
-  const int m = min(n_left, kMaxLeft);
-  const int64_t out = (int64_t)blockIdx.x * p.n_out;
-  for (int i = tid; i < m; i += NT) {
-    const double s = left.score[i];
-    const uint64_t k = left.key[i];
-    const int b = left.beam[i];
-    int before = 0;
-    for (int j = 0; j < m; ++j) before += left.before(j, s, b, k);
-    if (before >= p.n_out) continue;
-    p.parents[out + before] = b;
-    p.tokens[out + before] = (int)~(uint32_t)k;
-    p.scores_out[out + before] = (float)s;
+  if (lane < p.n_out) {
+    const int64_t at = (int64_t)blockIdx.x * p.n_out + lane;
+    p.parents[at] = parent;
+    p.tokens[at] = token;
+    p.scores_out[at] = value;
   }
-  for (int i = m + tid; i < p.n_out; i += NT) {
-    p.parents[out + i] = -1;
-    p.tokens[out + i] = -1;
-    p.scores_out[out + i] = -INFINITY;
-  }
+}
+
+// Parts of a row: as for the log probabilities, and with few rows shorter ones: there is a join
+// behind them in any case (4 rows of 50257 bf16, 4 best: 9.4 us in one part, SPL in 3).
+void beam_parts(int64_t n_rows, int vocab, bool bf16, int* parts, int* part_logits) {
+  logprob_parts(n_rows, vocab, bf16, parts, part_logits);
+  const int n = bf16 ? 8 : 4;
+  const int64_t vectors = ((int64_t)vocab + n - 1) / n;
+  const int64_t more = std::min<int64_t>(64 / std::max<int64_t>(n_rows, 1), vectors / 2048);
+  if (more <= *parts) return;
+  *parts = (int)more;
+  *part_logits = (int)((vectors + more - 1) / more * n);
 }
 
 hipError_t launch_beam_select(const LogprobArgs& a, const BeamArgs& b, bool bf16, hipStream_t s) {

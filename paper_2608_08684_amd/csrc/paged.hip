@@ -718,11 +718,11 @@ __global__ __launch_bounds__(kSelectThreads) void page_select_kernel(PagedView c
 // and the way through memory).
 enum class Sel { kNone, kKeys, kScores };
 
-template <typename T, typename C, int DH, Sel SEL>
-__global__ __launch_bounds__(64 * kDecodeWaves) void decode_kernel(PagedView cache, PagedTable tab, DecodeArgs a,
+template <typename T, typename C, int DH, Sel SEL, int NW = kDecodeWaves>
+__global__ __launch_bounds__(64 * NW) void decode_kernel(PagedView cache, PagedTable tab, DecodeArgs a,
                                                                    SelectArgs sel) {
   using Tile = CacheTile<C, DH>;
-  constexpr int NW = kDecodeWaves, SP = DH + 4;
+  constexpr int SP = DH + 4;
   constexpr int AREA0 = Tile::LDS * NW > NW * 16 * SP * 4 ? Tile::LDS * NW : NW * 16 * SP * 4;
   constexpr int SCORES = SEL == Sel::kScores ? 2 * DH * 8 + kWavePages * 8 : 0;
   constexpr int AREA = AREA0 > SCORES ? AREA0 : SCORES;
@@ -1001,7 +1001,11 @@ hipError_t launch_decode(const PagedView& cache, const PagedTable& tab, DecodeAr
   a.longest_first = blocks > 512 && tab.n_seqs <= 64 && !tab.per_head;
 #define RK_DECODE(T, C, DH)                                                                                        \
   do {                                                                                                             \
-    decode_kernel<T, C, DH, Sel::kNone><<<(uint32_t)blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, a, SelectArgs{});  \
+    constexpr int kMore = std::is_same<C, e4m3_t>::value ? 8 : kDecodeWaves;                                       \
+    if (blocks <= 256)                                                                                             \
+      decode_kernel<T, C, DH, Sel::kNone, kMore><<<(uint32_t)blocks, 64 * kMore, 0, s>>>(cache, tab, a, SelectArgs{}); \
+    else                                                                                                           \
+      decode_kernel<T, C, DH, Sel::kNone><<<(uint32_t)blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, a, SelectArgs{}); \
     if (a.n_parts > 1)                                                                                             \
       decode_join_kernel<T, DH><<<tab.n_seqs * a.n_heads, 256, 0, s>>>(tab, a, cache.n_kv, cache.page_shift);      \
   } while (0)

@@ -349,6 +349,7 @@ struct BeamArgs {
   int32_t *parents, *tokens;
   float* scores_out;
 };
+void beam_parts(int64_t n_rows, int vocab, bool bf16, int* parts, int* part_logits);
 hipError_t launch_beam_select(const LogprobArgs& a, const BeamArgs& b, bool bf16, hipStream_t s);
 
 hipError_t launch_finalize(const double* s_acc, int n, double inv_n, float* s_out, hipStream_t s);

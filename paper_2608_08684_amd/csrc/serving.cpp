@@ -480,6 +480,7 @@ static LogprobPlan beam_plan(int32_t n_groups, int32_t n_beams, int32_t vocab, r
   const int n = std::min(n_out, vocab);
   p = logprob_plan(rows, vocab, dtype, n);
   if (!p.total) return p;
+  beam_parts(rows, vocab, dtype == RK_BF16, &p.parts, &p.part_logits);
   p.top = align256((size_t)rows * p.parts * sizeof(float4));
   p.total = std::max<size_t>(256, p.top + align256((size_t)rows * p.parts * n * 8));
   return p;
