@@ -642,7 +642,8 @@ __global__ __launch_bounds__(256) void beam_join_kernel(LogprobArgs a, BeamArgs 
     else c.set(shift[b] > -INFINITY ? ((double)from_order((uint32_t)(k >> 32)) - ref[b]) + shift[b] : -INFINITY, k, b);
     return c;
   };
-  int held = min(lists, 64), mine = lane;          // lists, and which one this lane has
+  const int held = min(lists, 64);                 // lists in hand
+  int mine = lane;                                 // which one this lane has
   if (lists > 64) {
     for (int i = tid; i < lists; i += NT) heads[i] = candidate(i, 0, top[(int64_t)i * n]);
     __syncthreads();
@@ -682,14 +683,18 @@ __global__ __launch_bounds__(256) void beam_join_kernel(LogprobArgs a, BeamArgs 
   c.set(-INFINITY, 0, 0);
   int next = 0;
   if (lane < held) c = candidate(mine, 0, list[lane * n]);
+  uint64_t ahead = lane < held ? list[lane * n + min(1, n - 1)] : 0;
   int parent = -1, token = -1;
   float value = -INFINITY;                         // of place `lane`
   for (int i = 0; i < p.n_out; ++i) {
     const uint32_t hi = wave_max((uint32_t)(c.score >> 32));
     if (hi == 0) break;                            // (a score's upper half is not 0)
     const bool up = (uint32_t)(c.score >> 32) == hi;
-    const uint32_t lo = wave_max(up ? (uint32_t)c.score : 0);
-    uint64_t m = __ballot(up && (uint32_t)c.score == lo);
+    uint64_t m = __ballot(up);
+    if (m & (m - 1)) {
+      const uint32_t lo = wave_max(up ? (uint32_t)c.score : 0);
+      m = __ballot(up && (uint32_t)c.score == lo);
+    }
     int win = __builtin_ctzll(m);
     if (m & (m - 1)) {   // equal scores: the lowest beam, in lanes as in lists; of its parts' the larger key
       m = __ballot((m >> lane & 1) && c.beam == __builtin_amdgcn_readlane(c.beam, win));
@@ -702,6 +707,7 @@ __global__ __launch_bounds__(256) void beam_join_kernel(LogprobArgs a, BeamArgs 
       }
     }
     const int b = __builtin_amdgcn_readlane(c.beam, win), t = ~__builtin_amdgcn_readlane((int)c.key, win);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)c.score, win);
     if (lane == i) {
       Candidate best;
       best.score = (uint64_t)hi << 32 | lo;
@@ -709,10 +715,11 @@ __global__ __launch_bounds__(256) void beam_join_kernel(LogprobArgs a, BeamArgs 
       token = t;
       value = (float)best.value();
     }
-    if (lane == win) {
+    if (lane == win) {   // what comes after has been read since the list's last turn
       ++next;
-      if (next < n) c = candidate(mine, next, list[lane * n + next]);
+      if (next < n) c = candidate(mine, next, ahead);
       else c.score = 0;
+      ahead = list[lane * n + min(next + 1, n - 1)];
     }
   }
   if (lane < p.n_out) {

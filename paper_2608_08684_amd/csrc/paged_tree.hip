@@ -3,11 +3,11 @@
 // Sequence i's m drafts are its last m entries, b .. b + m - 1, and draft j of query head h
 //   o_j,h = sum_u softmax_u(scale q_j,h . k_u) v_u,  u < b, or u = b + t with bit t of mask_j.
 // The m x H / H_kv query rows of a KV head are the columns of one pass over its cache, so that
-// an entry is read once for 16 .. 128 of them.  Two kernels:
-//   up to 16 columns (fp32: 32 of any number): the waves of a workgroup take the tiles of its
-//     part of the length in turn, as in the attention of one token (tree_narrow_kernel);
-//   more: all waves go through the same tiles, which LDS holds for them, each with columns of
-//     its own (tree_wide_kernel).
+// an entry is read once for 16 .. 128 of them.  Two kernels (width_of chooses):
+//   16 columns a workgroup: its waves take the tiles of its part of the length in turn, as in
+//     the attention of one token (tree_narrow_kernel);
+//   up to 128: all waves go through the same tiles, which LDS holds for them, each with columns
+//     of its own (tree_wide_kernel).
 //
 // A column keeps a reference R, the sum l of its weights e^(s - R) and its output.  R is
 // moved only when a score has passed it by kRaise: the output's rescale, a multiplication of
@@ -74,11 +74,11 @@ struct Share {
 __device__ __forceinline__ bool sees(uint64_t word, int draft) { return draft < 0 || (word >> (draft & 63) & 1); }
 
 // --------------------------------------------------------------------------- few columns
-template <typename T, typename C, int DH, int N>
+template <typename T, typename C, int DH>
 __global__ __launch_bounds__(64 * kDecodeWaves) void tree_narrow_kernel(PagedView cache, PagedTable tab, SeqTable st,
                                                                         TreeArgs a) {
   using Tile = CacheTile<C, DH>;
-  constexpr int NW = kDecodeWaves, SP = DH + 4, PIECES = N == 1 ? 3 : 2;
+  constexpr int NW = kDecodeWaves, SP = DH + 4, N = 1, PIECES = 3;
   constexpr bool kFp32 = std::is_same<T, float>::value;
   constexpr int AREA = Tile::LDS * NW > NW * 16 * SP * 4 ? Tile::LDS * NW : NW * 16 * SP * 4;
   __shared__ __attribute__((aligned(16))) char area[AREA];
@@ -228,6 +228,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void tree_narrow_kernel(PagedVie
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) s[n][t][i] = weight(s[n][t][i], R[n]) > 0.f ? kHuge : 0.f;
+#pragma unroll 1
       for (int sign = 1; sign >= -1; sign -= 2) {
         tile.load_v(cache, wh.r0, wh.r1, lane);
         tile.clear_values(wh.seen, lane);
@@ -551,11 +552,13 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void tree_wide_kernel(PagedVi
       const int page = pages_of(k0);
       seen = seen_of(page, k0);
       rows_of(page, k0, at);
+#pragma unroll 1
       for (int sign = 1; sign >= -1; sign -= 2) {
         tile.load(cache, at, tid);
         bring(area[0], k0, seen, sign);
         __syncthreads();
         if (busy) {
+#pragma unroll 1
           for (int half = 0; half < 2; ++half) {
             scores(s, area[0], 32 * half);
             hide(s, k0 + 32 * half, (uint32_t)(seen >> 32 * half));
@@ -646,14 +649,19 @@ __global__ __launch_bounds__(256) void tree_join_kernel(PagedTable tab, SeqTable
 }
 
 // Columns of a workgroup, for the widest tree of a call, and whether its waves share their tiles.
+// Sharing pays where entries are many or workgroups are: a tile takes a workgroup 2.6 us by
+// itself, and a shared one starts 3 us later (bf16, 8 KV heads of 128: 1 sequence of 360, 148
+// columns: 12.4 us not shared, 24.3 shared; 4 of 1000, 104: 20 and 30; 8 of 2048, 32: 31.5 and
+// 24.6; 2 of 8192, 64: 41 and 29; 60 of 300, 64: 105 and 26).  fp32 has no shared kernel: its
+// products take eight times as long as its loads.
 struct Width {
   int columns;
   bool shared;
 };
-Width width_of(const PagedView& cache, int max_drafts, int n_heads) {
+Width width_of(const PagedView& cache, int n_seqs, int max_drafts, int n_heads, int64_t max_entries) {
   const int64_t cols = (int64_t)max_drafts * (n_heads / cache.n_kv);
-  if (cols <= 16) return {16, false};
-  if (!cache.bf16) return {32, false};
+  const bool few = max_entries <= 1024 && (int64_t)n_seqs * cache.n_kv * ((cols + 15) / 16) <= 256;
+  if (cols <= 16 || !cache.bf16 || few) return {16, false};
   return {cols <= 64 ? 64 : 128, true};
 }
 
@@ -668,7 +676,7 @@ Width width_of(const PagedView& cache, int max_drafts, int n_heads) {
 //   16 x 100 .. 8192, 256 columns: 2 parts 190, 4 150, 8 180 (all of 4096: 146, 157, 185);
 //   16 x 100 .. 2048, 32 columns of 64: 2 parts 29.2, 4 22.2.
 int tree_parts(const PagedView& cache, int n_seqs, int max_drafts, int n_heads, int64_t max_entries) {
-  const Width width = width_of(cache, max_drafts, n_heads);
+  const Width width = width_of(cache, n_seqs, max_drafts, n_heads, max_entries);
   const int64_t cols = (int64_t)max_drafts * (n_heads / cache.n_kv);
   const int64_t rows = (int64_t)n_seqs * cache.n_kv * ((cols + width.columns - 1) / width.columns);
   const int64_t least = std::max(512, 8 * cache.head_dim);
@@ -677,24 +685,24 @@ int tree_parts(const PagedView& cache, int n_seqs, int max_drafts, int n_heads, 
   return (int)std::max<int64_t>(1, std::min<int64_t>(std::max(fill, level), kMaxTreeParts));
 }
 
-int64_t tree_blocks(const PagedView& cache, const SeqTable& st, const TreeArgs& a) {
-  const int64_t cols = (int64_t)st.max_len * (a.n_heads / cache.n_kv), width = width_of(cache, st.max_len, a.n_heads).columns;
+int64_t tree_blocks(const PagedView& cache, const PagedTable& tab, const SeqTable& st, const TreeArgs& a) {
+  const int64_t cols = (int64_t)st.max_len * (a.n_heads / cache.n_kv);
+  const int64_t width = width_of(cache, st.n, st.max_len, a.n_heads, (int64_t)tab.max_pages << cache.page_shift).columns;
   const int64_t items = (int64_t)st.n * cache.n_kv * a.n_parts;
   return (items + 7) / 8 * 8 * ((cols + width - 1) / width);
 }
 
 hipError_t launch_tree(const PagedView& cache, const PagedTable& tab, const SeqTable& st, TreeArgs a, hipStream_t s) {
-  const Width width = width_of(cache, st.max_len, a.n_heads);
+  const Width width = width_of(cache, st.n, st.max_len, a.n_heads, (int64_t)tab.max_pages << cache.page_shift);
   a.col_blocks = (int)(((int64_t)st.max_len * (a.n_heads / cache.n_kv) + width.columns - 1) / width.columns);
-  const uint32_t blocks = (uint32_t)tree_blocks(cache, st, a);
+  const uint32_t blocks = (uint32_t)tree_blocks(cache, tab, st, a);
   const int64_t outs = (int64_t)st.rows * a.n_heads;
 #define RK_TREE(T, C, DH)                                                                                          \
   do {                                                                                                             \
     if constexpr (std::is_same<T, float>::value) {                                                                 \
-      if (width.columns == 16) tree_narrow_kernel<T, C, DH, 1><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, st, a); \
-      else tree_narrow_kernel<T, C, DH, 2><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, st, a);                \
+      tree_narrow_kernel<T, C, DH><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, st, a);                        \
     } else {                                                                                                       \
-      if (!width.shared) tree_narrow_kernel<T, C, DH, 1><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, st, a);  \
+      if (!width.shared) tree_narrow_kernel<T, C, DH><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, st, a);  \
       else if (width.columns == 64) tree_wide_kernel<C, DH, 1><<<blocks, 256, 0, s>>>(cache, tab, st, a);       \
       else tree_wide_kernel<C, DH, 2><<<blocks, 256, 0, s>>>(cache, tab, st, a);                                \
     }                                                                                                              \

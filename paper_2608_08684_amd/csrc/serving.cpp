@@ -362,7 +362,7 @@ rk_status rk_paged_attention_tree(const rk_paged_cache* cache, const rk_paged_se
   a.n_heads = n_heads; a.n_parts = p.n_parts;
   a.scale = scale > 0.f ? scale : (float)(1.0 / sqrt((double)v.head_dim));
   a.part_o = (float*)workspace; a.part_lse = (float*)((char*)workspace + p.part_lse);
-  if (tree_blocks(v, st, a) > kMaxWorkgroups) return bad(RK_ERR_SHAPE, "more heads and drafts than a launch takes");
+  if (tree_blocks(v, t, st, a) > kMaxWorkgroups) return bad(RK_ERR_SHAPE, "more heads and drafts than a launch takes");
   hipStream_t s = (hipStream_t)stream;
   if ((e = check_stream(s)) != RK_OK) return e;
   Timed timed("paged_tree", s);
