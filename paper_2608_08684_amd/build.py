@@ -30,7 +30,8 @@ ARCH = "gfx950"
 # never NaN (masked keys are -inf), so max reductions need no NaN canonicalising.
 # The paged attention does the same with its own.
 EXTRA = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form", "-fno-honor-nans"],
-         "paged.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+         "paged.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+         "paged_tree.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def hipcc() -> str:

@@ -785,12 +785,12 @@ __global__ __launch_bounds__(64 * NW) void decode_kernel(PagedView cache, PagedT
   const int64_t head_at = (int64_t)hk << shift, page_rows = (int64_t)G << shift;
 
   Tile tile;
-  typename Tile::Query query[1];
+  typename Tile::Query query;
   const int col = lane & 15, g = lane >> 4;
-  Tile::load_q(query[0], (const T*)a.q + (int64_t)seq * a.q_rs + (int64_t)(h0 + min_i(col, nh - 1)) * DH, lane);
-  f32x4_t o[1][Tile::ND];
+  Tile::load_q(query, (const T*)a.q + (int64_t)seq * a.q_rs + (int64_t)(h0 + min_i(col, nh - 1)) * DH, lane);
+  f32x4_t o[Tile::ND];
 #pragma unroll
-  for (int i = 0; i < Tile::ND; ++i) o[0][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < Tile::ND; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
   // Weights count in units of a power of two above the part's entries: their sum stays below
   // 1, and that of weighted values below the largest, however large they are.
@@ -834,20 +834,20 @@ __global__ __launch_bounds__(64 * NW) void decode_kernel(PagedView cache, PagedT
   }
   for (int k0 = first; k0 < end; k0 += step) {
     const uint32_t seen = cur.seen;
-    f32x4_t s[1][2];
-    tile.template scores<1>(query, s);
+    f32x4_t s[2];
+    tile.scores(query, s);
     tile.load_k(cache, nxt.r0, nxt.r1, lane);
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[0][t][i] *= a.scale;
+      for (int i = 0; i < 4; ++i) s[t][i] *= a.scale;
     if (seen != 0xffffffffu) {
       tile.clear_values(seen, lane);
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (!(seen >> (t * 16 + 4 * g + i) & 1)) s[0][t][i] = -INFINITY;
+          if (!(seen >> (t * 16 + 4 * g + i) & 1)) s[t][i] = -INFINITY;
     }
     cur = nxt;
     if constexpr (Tile::kStaged) {
@@ -856,8 +856,8 @@ __global__ __launch_bounds__(64 * NW) void decode_kernel(PagedView cache, PagedT
     }
     nxt = where(ahead);
     ahead = pages_of(k0 + 3 * step);
-    float mx = fmaxf(fmaxf(fmaxf(s[0][0][0], s[0][0][1]), fmaxf(s[0][0][2], s[0][0][3])),
-                     fmaxf(fmaxf(s[0][1][0], s[0][1][1]), fmaxf(s[0][1][2], s[0][1][3])));
+    float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                     fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
     const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.f : m_new;
@@ -865,15 +865,15 @@ __global__ __launch_bounds__(64 * NW) void decode_kernel(PagedView cache, PagedT
     m = m_new;
     l *= corr;
 #pragma unroll
-    for (int i = 0; i < Tile::ND; ++i) o[0][i] *= corr;
+    for (int i = 0; i < Tile::ND; ++i) o[i] *= corr;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        s[0][t][i] = sizeof(T) == 4 ? exp_diff_exact(s[0][t][i] - ref, unit) : exp_diff(s[0][t][i] - ref) * unit;
-        l += s[0][t][i];
+        s[t][i] = sizeof(T) == 4 ? exp_diff_exact(s[t][i] - ref, unit) : exp_diff(s[t][i] - ref) * unit;
+        l += s[t][i];
       }
-    tile.template values<1, 3>(s, o, area + w * Tile::LDS, lane);
+    tile.values(s, o, area + w * Tile::LDS, lane);
     if constexpr (!Tile::kStaged) tile.load_v(cache, cur.r0, cur.r1, lane);
   }
   l += __shfl_xor(l, 16, 64);
@@ -884,7 +884,7 @@ __global__ __launch_bounds__(64 * NW) void decode_kernel(PagedView cache, PagedT
 #pragma unroll
   for (int i = 0; i < Tile::ND; ++i)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) so[(w * 16 + col) * SP + Tile::channel(i, g, e)] = o[0][i][e];
+    for (int e = 0; e < 4; ++e) so[(w * 16 + col) * SP + Tile::channel(i, g, e)] = o[i][e];
   __syncthreads();
   for (int i = tid; i < nh * DH; i += 64 * NW) {
     const int h = i / DH, x = i % DH;

@@ -179,8 +179,8 @@ __device__ __forceinline__ int table_length(const PagedTable& tab, int row, int 
 
 constexpr int kDecodeWaves = 4, kTile = 32;
 
-// A wave's tile of 32 entries of one KV head, and what is done with it for N blocks of 16
-// columns (a column is a query row of one head):
+// A wave's tile of 32 entries of one KV head, and what is done with it for 16 columns (a column is
+// a query row of one head):
 //   scores  S^T[entry, column] = K Q^T: the cache's rows are the A operand as they lie
 //           in memory, so K goes from memory to the matrix unit's registers directly;
 //   values  O^T[d, column] += V^T P^T: a lane's scores are already the B operand of that
@@ -210,27 +210,25 @@ template <int DH> struct StagedValues {
                __builtin_bit_cast(v2u, a1)[1]};
   }
   // a lane's weights as the B operand
-  template <int N, int PIECES>
-  static __device__ __forceinline__ void pieces(const f32x4_t (*p)[2], v4u (*part)[PIECES]) {
+  template <int PIECES>
+  static __device__ __forceinline__ void pieces(const f32x4_t* p, v4u* part) {
     static_assert(PIECES == 2 || PIECES == 3, "weights");
 #pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        const float x = p[n][e >> 2][e & 3], y = p[n][e >> 2][(e & 3) + 1];
-        const uint32_t x0 = bf16_below(x), y0 = bf16_below(y);
-        const float x1 = x - __uint_as_float(x0), y1 = y - __uint_as_float(y0);
-        part[n][0][e / 2] = __builtin_amdgcn_perm(y0, x0, 0x07060302u);   // the upper halves
-        if constexpr (PIECES == 3) {
-          const uint32_t x2 = bf16_below(x1), y2 = bf16_below(y1);
-          part[n][1][e / 2] = __builtin_amdgcn_perm(y2, x2, 0x07060302u);
-          part[n][2][e / 2] =
-              (uint32_t)f2bf(x1 - __uint_as_float(x2)) | ((uint32_t)f2bf(y1 - __uint_as_float(y2)) << 16);
-        } else {
-          part[n][1][e / 2] = (uint32_t)f2bf(x1) | ((uint32_t)f2bf(y1) << 16);
-        }
+    for (int e = 0; e < 8; e += 2) {
+      const float x = p[e >> 2][e & 3], y = p[e >> 2][(e & 3) + 1];
+      const uint32_t x0 = bf16_below(x), y0 = bf16_below(y);
+      const float x1 = x - __uint_as_float(x0), y1 = y - __uint_as_float(y0);
+      part[0][e / 2] = __builtin_amdgcn_perm(y0, x0, 0x07060302u);   // the upper halves
+      if constexpr (PIECES == 3) {
+        const uint32_t x2 = bf16_below(x1), y2 = bf16_below(y1);
+        part[1][e / 2] = __builtin_amdgcn_perm(y2, x2, 0x07060302u);
+        part[2][e / 2] = (uint32_t)f2bf(x1 - __uint_as_float(x2)) | ((uint32_t)f2bf(y1 - __uint_as_float(y2)) << 16);
+      } else {
+        part[1][e / 2] = (uint32_t)f2bf(x1) | ((uint32_t)f2bf(y1) << 16);
       }
+    }
   }
+  // .. times the values, for N blocks of columns
   template <int N, int PIECES>
   static __device__ __forceinline__ void add(const v4u (*part)[PIECES], f32x4_t (*o)[ND], const char* lds, int lane) {
 #pragma unroll
@@ -244,11 +242,11 @@ template <int DH> struct StagedValues {
                                                             __builtin_bit_cast(bf16x8_t, part[n][i]), o[n][b], 0, 0, 0);
     }
   }
-  template <int N, int PIECES>
-  static __device__ __forceinline__ void accumulate(const f32x4_t (*p)[2], f32x4_t (*o)[ND], char* lds, int lane) {
-    v4u part[N][PIECES];
-    pieces<N, PIECES>(p, part);
-    add<N, PIECES>(part, o, lds, lane);
+  // weights of 24 bits: the matrix unit has the time
+  static __device__ __forceinline__ void accumulate(const f32x4_t* p, f32x4_t* o, char* lds, int lane) {
+    v4u part[1][3];
+    pieces<3>(p, part[0]);
+    add<1, 3>(part, reinterpret_cast<f32x4_t (*)[ND]>(o), lds, lane);
     wave_sync();
   }
   // channel of element i of output block b in 16-lane group g
@@ -290,18 +288,13 @@ template <int DH> struct CacheTile<bf16_t, DH> : StagedValues<DH> {
     for (int i = 0; i < NV; ++i)
       if (!(seen >> ((i * 64 + lane) / CH) & 1)) v[i] = v4u{0, 0, 0, 0};
   }
-  template <int N>
-  __device__ __forceinline__ void scores(const Query* q, f32x4_t (*s)[2]) const {
+  __device__ __forceinline__ void scores(const Query& q, f32x4_t* s) const {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-#pragma unroll
-      for (int n = 0; n < N; ++n) s[n][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int n = 0; n < N; ++n)
-          s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k[t][c]), q[n].q[c], s[n][t],
-                                                            0, 0, 0);
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k[t][c]), q.q[c], s[t], 0, 0, 0);
     }
   }
   __device__ __forceinline__ bool take_out_values(int sign) {   // see take_out
@@ -320,9 +313,8 @@ template <int DH> struct CacheTile<bf16_t, DH> : StagedValues<DH> {
     wave_sync();
   }
   static constexpr bool kStaged = true;
-  template <int N, int PIECES>
-  __device__ __forceinline__ void values(const f32x4_t (*p)[2], f32x4_t (*o)[Base::ND], char* lds, int lane) const {
-    Base::template accumulate<N, PIECES>(p, o, lds, lane);
+  __device__ __forceinline__ void values(const f32x4_t* p, f32x4_t* o, char* lds, int lane) const {
+    Base::accumulate(p, o, lds, lane);
   }
 };
 
@@ -378,19 +370,15 @@ template <int DH> struct CacheTile<e4m3_t, DH> : StagedValues<DH> {
     }
     return any;
   }
-  template <int N>
-  __device__ __forceinline__ void scores(const Query* q, f32x4_t (*s)[2]) const {
+  __device__ __forceinline__ void scores(const Query& q, f32x4_t* s) const {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const float scale = e4m3_scale(ks[t]);
-#pragma unroll
-      for (int n = 0; n < N; ++n) s[n][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      s[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
         const v4u a = e4m3_to_bf16(k[t][c / 2][c % 2 * 2], k[t][c / 2][c % 2 * 2 + 1], scale);
-#pragma unroll
-        for (int n = 0; n < N; ++n)
-          s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), q[n].q[c], s[n][t], 0, 0, 0);
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), q.q[c], s[t], 0, 0, 0);
       }
     }
   }
@@ -406,9 +394,8 @@ template <int DH> struct CacheTile<e4m3_t, DH> : StagedValues<DH> {
     wave_sync();
   }
   static constexpr bool kStaged = true;
-  template <int N, int PIECES>
-  __device__ __forceinline__ void values(const f32x4_t (*p)[2], f32x4_t (*o)[Base::ND], char* lds, int lane) const {
-    Base::template accumulate<N, PIECES>(p, o, lds, lane);
+  __device__ __forceinline__ void values(const f32x4_t* p, f32x4_t* o, char* lds, int lane) const {
+    Base::accumulate(p, o, lds, lane);
   }
 };
 
@@ -477,26 +464,21 @@ template <int DH> struct CacheTile<float, DH> {
         }
     return any;
   }
-  template <int N>
-  __device__ __forceinline__ void scores(const Query* q, f32x4_t (*s)[2]) const {
+  __device__ __forceinline__ void scores(const Query& q, f32x4_t* s) const {
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < 2; ++t) {
+      // four sums over a quarter of the channels each: shorter chains, and none waits for another
+      f32x4_t a[4];
 #pragma unroll
-      for (int n = 0; n < N; ++n) {
-        // four sums over a quarter of the channels each: shorter chains, and none waits for another
-        f32x4_t a[4];
+      for (int e = 0; e < 4; ++e) {
+        a[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          a[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int c = 0; c < NC; ++c)
-            a[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[t][c][e], q[n].q[c][e], a[e], 0, 0, 0);
-        }
-        s[n][t] = (a[0] + a[1]) + (a[2] + a[3]);
+        for (int c = 0; c < NC; ++c) a[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[t][c][e], q.q[c][e], a[e], 0, 0, 0);
       }
+      s[t] = (a[0] + a[1]) + (a[2] + a[3]);
+    }
   }
-  template <int N, int PIECES>
-  __device__ __forceinline__ void values(const f32x4_t (*p)[2], f32x4_t (*o)[ND], char*, int) const {
+  __device__ __forceinline__ void values(const f32x4_t* p, f32x4_t* o, char*, int) const {
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -505,10 +487,7 @@ template <int DH> struct CacheTile<float, DH> {
         for (int c = 0; c < NP; ++c)
 #pragma unroll
           for (int e = 0; e < VEC; ++e)
-#pragma unroll
-            for (int n = 0; n < N; ++n)
-              o[n][c * VEC + e] =
-                  __builtin_amdgcn_mfma_f32_16x16x4f32(v[t][i][c][e], p[n][t][i], o[n][c * VEC + e], 0, 0, 0);
+            o[c * VEC + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[t][i][c][e], p[t][i], o[c * VEC + e], 0, 0, 0);
   }
   static __device__ __forceinline__ int channel(int b, int g, int i) {
     return (b / VEC) * 16 * VEC + VEC * (4 * g + i) + b % VEC;

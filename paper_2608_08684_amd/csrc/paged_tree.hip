@@ -78,40 +78,31 @@ template <typename T, typename C, int DH>
 __global__ __launch_bounds__(64 * kDecodeWaves) void tree_narrow_kernel(PagedView cache, PagedTable tab, SeqTable st,
                                                                         TreeArgs a) {
   using Tile = CacheTile<C, DH>;
-  constexpr int NW = kDecodeWaves, SP = DH + 4, N = 1, PIECES = 3;
+  constexpr int NW = kDecodeWaves, SP = DH + 4;
   constexpr bool kFp32 = std::is_same<T, float>::value;
   constexpr int AREA = Tile::LDS * NW > NW * 16 * SP * 4 ? Tile::LDS * NW : NW * 16 * SP * 4;
   __shared__ __attribute__((aligned(16))) char area[AREA];
   __shared__ float sm[NW][16], sl[NW][16];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Share sh(cache, tab, st, a, lane, 16 * N);
+  const Share sh(cache, tab, st, a, lane, 16);
   if (sh.none) return;
-  const int G = cache.n_kv, grp = a.n_heads / G, cols = sh.m * grp, c0 = sh.cb * 16 * N;
+  const int G = cache.n_kv, grp = a.n_heads / G, cols = sh.m * grp, c0 = sh.cb * 16;
   const int start = sh.start, end = sh.end, base = sh.base;
   const int32_t* pages = tab.pages + (int64_t)sh.seq * tab.stride;
   const int shift = cache.page_shift, in_mask = (1 << shift) - 1;
   const int64_t head_at = (int64_t)sh.hk << shift, page_rows = (int64_t)G << shift;
 
   Tile tile;
-  typename Tile::Query query[N];
-  uint64_t word[N];
+  typename Tile::Query query;
   const int col = lane & 15, g = lane >> 4;
+  const int mine = min_i(c0 + col, cols - 1), row = mine / grp;   // this lane's column and draft
+  Tile::load_q(query, (const T*)a.q + (int64_t)(sh.row0 + row) * a.q_rs + (int64_t)(sh.hk * grp + mine - row * grp) * DH,
+               lane);
+  const uint64_t word = a.masks ? a.masks[sh.row0 + row] : (2ull << row) - 1;
+  f32x4_t o[Tile::ND];
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const int c = min_i(c0 + n * 16 + col, cols - 1), j = c / grp;
-    Tile::load_q(query[n], (const T*)a.q + (int64_t)(sh.row0 + j) * a.q_rs + (int64_t)(sh.hk * grp + c - j * grp) * DH,
-                 lane);
-    word[n] = a.masks ? a.masks[sh.row0 + j] : (2ull << j) - 1;
-  }
-  f32x4_t o[N][Tile::ND];
-  float R[N], l[N];
-#pragma unroll
-  for (int n = 0; n < N; ++n) {
-    R[n] = kUnset;
-    l[n] = 0.f;
-#pragma unroll
-    for (int i = 0; i < Tile::ND; ++i) o[n][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
+  for (int i = 0; i < Tile::ND; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  float R = kUnset, l = 0.f;
   // the weights' unit: a power of two above the part's entries and e^kRaise
   const int bits = 32 - __builtin_clz(max_i(end - start, 1)) + 12;
   const float unit = __uint_as_float((uint32_t)(127 - bits) << 23);
@@ -140,19 +131,17 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void tree_narrow_kernel(PagedVie
     return wh;
   };
   // scores of what is not seen, or by the mask not seen by the column, are -inf
-  const auto hide = [&](f32x4_t (*s)[2], int k0, uint32_t seen) {
+  const auto hide = [&](f32x4_t* s, int k0, uint32_t seen) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const int at = k0 + t * 16 + 4 * g - base;   // draft of the lane's first entry of this half
 #pragma unroll
-      for (int n = 0; n < N; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (!(seen >> (t * 16 + 4 * g + i) & 1) || !sees(word[n], at + i)) s[n][t][i] = -INFINITY;
+      for (int i = 0; i < 4; ++i)
+        if (!(seen >> (t * 16 + 4 * g + i) & 1) || !sees(word, at + i)) s[t][i] = -INFINITY;
     }
   };
-  const auto weight = [&](float s, float ref) {
-    return kFp32 ? exp_diff_exact(s * a.scale - ref, unit) : __builtin_amdgcn_exp2f(fmaf(s, c2, -ref));
+  const auto weight = [&](float s) {
+    return kFp32 ? exp_diff_exact(s * a.scale - R, unit) : __builtin_amdgcn_exp2f(fmaf(s, c2, -R));
   };
   // loads run a tile ahead, their pages two, as in the attention of one token
   Where cur{}, nxt{};
@@ -167,8 +156,8 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void tree_narrow_kernel(PagedVie
   bool poison = false;
   for (int k0 = first; k0 < end; k0 += step) {
     const uint32_t seen = cur.seen;
-    f32x4_t s[N][2];
-    tile.template scores<N>(query, s);
+    f32x4_t s[2];
+    tile.scores(query, s);
     tile.load_k(cache, nxt.r0, nxt.r1, lane);
     if (seen != 0xffffffffu) tile.clear_values(seen, lane);
     if (seen != 0xffffffffu || k0 + 32 > base) hide(s, k0, seen);
@@ -180,38 +169,27 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void tree_narrow_kernel(PagedVie
     }
     nxt = where(ahead);
     ahead = pages_of(k0 + 3 * step);
-    float mx[N];
-    bool above = false;
+    float mx = s[0][0];
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      mx[n] = s[n][0][0];
+    for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[i >> 2][i & 3]);
+    if (__ballot(kFp32 ? mx * a.scale > R + kRaise : fmaf(mx, c2, -R) > kRaise * kLog2e - (float)bits)) {
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      const float to = fmaxf(R, kFp32 ? mx * a.scale : fmaf(mx, c2, (float)bits));
+      const float corr = kFp32 ? exp_diff(R - to) : __builtin_amdgcn_exp2f(R - to);
+      R = to;
+      l *= corr;
 #pragma unroll
-      for (int i = 1; i < 8; ++i) mx[n] = fmaxf(mx[n], s[n][i >> 2][i & 3]);
-      above |= kFp32 ? mx[n] * a.scale > R[n] + kRaise : fmaf(mx[n], c2, -R[n]) > kRaise * kLog2e - (float)bits;
+      for (int i = 0; i < Tile::ND; ++i) o[i] *= corr;
     }
-    if (__ballot(above)) {
 #pragma unroll
-      for (int n = 0; n < N; ++n) {
-        float x = fmaxf(mx[n], __shfl_xor(mx[n], 16, 64));
-        x = fmaxf(x, __shfl_xor(x, 32, 64));
-        const float to = fmaxf(R[n], kFp32 ? x * a.scale : fmaf(x, c2, (float)bits));
-        const float corr = kFp32 ? exp_diff(R[n] - to) : __builtin_amdgcn_exp2f(R[n] - to);
-        R[n] = to;
-        l[n] *= corr;
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int i = 0; i < Tile::ND; ++i) o[n][i] *= corr;
+      for (int i = 0; i < 4; ++i) {
+        s[t][i] = weight(s[t][i]);
+        l += s[t][i];
       }
-    }
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s[n][t][i] = weight(s[n][t][i], R[n]);
-          l[n] += s[n][t][i];
-        }
-    tile.template values<N, PIECES>(s, o, area + w * Tile::LDS, lane);
+    tile.values(s, o, area + w * Tile::LDS, lane);
     if constexpr (!Tile::kStaged) tile.load_v(cache, cur.r0, cur.r1, lane);
   }
   if (__ballot(poison)) {
@@ -219,71 +197,62 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void tree_narrow_kernel(PagedVie
       if (k0 + 32 <= base) continue;
       const Where wh = where(pages_of(k0));
       tile.load_k(cache, wh.r0, wh.r1, lane);
-      f32x4_t s[N][2];
-      tile.template scores<N>(query, s);
+      f32x4_t s[2];
+      tile.scores(query, s);
       hide(s, k0, wh.seen);
 #pragma unroll
-      for (int n = 0; n < N; ++n)
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[n][t][i] = weight(s[n][t][i], R[n]) > 0.f ? kHuge : 0.f;
+        for (int i = 0; i < 4; ++i) s[t][i] = weight(s[t][i]) > 0.f ? kHuge : 0.f;
 #pragma unroll 1
       for (int sign = 1; sign >= -1; sign -= 2) {
         tile.load_v(cache, wh.r0, wh.r1, lane);
         tile.clear_values(wh.seen, lane);
         tile.take_out_values(sign);
         if constexpr (Tile::kStaged) tile.stage_v(area + w * Tile::LDS, lane);
+        f32x4_t sum[Tile::ND];   // of their own: an infinity in o would swallow the other one
 #pragma unroll
-        for (int n = 0; n < N; ++n) {   // sums of their own: an infinity in o would swallow the other one
-          f32x4_t add[1][Tile::ND];
+        for (int i = 0; i < Tile::ND; ++i) sum[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        tile.values(s, sum, area + w * Tile::LDS, lane);
 #pragma unroll
-          for (int i = 0; i < Tile::ND; ++i) add[0][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-          tile.template values<1, PIECES>(s + n, add, area + w * Tile::LDS, lane);
-#pragma unroll
-          for (int i = 0; i < Tile::ND; ++i) o[n][i] += add[0][i];
-        }
+        for (int i = 0; i < Tile::ND; ++i) o[i] += sum[i];
       }
     }
   }
   float* so = (float*)area;
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  __syncthreads();   // the tiles are done with: their area takes the waves' outputs
+  if (g == 0) { sm[w][col] = R; sl[w][col] = l; }
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    if (c0 + n * 16 >= cols) return;
-    l[n] += __shfl_xor(l[n], 16, 64);
-    l[n] += __shfl_xor(l[n], 32, 64);
-    __syncthreads();   // the tiles, or the last columns' outputs, are done with
-    if (g == 0) { sm[w][col] = R[n]; sl[w][col] = l[n]; }
+  for (int i = 0; i < Tile::ND; ++i)
 #pragma unroll
-    for (int i = 0; i < Tile::ND; ++i)
+    for (int e = 0; e < 4; ++e) so[(w * 16 + col) * SP + Tile::channel(i, g, e)] = o[i][e];
+  __syncthreads();
+  for (int i = tid; i < 16 * DH; i += 64 * NW) {
+    const int cc = i / DH, x = i % DH, c = c0 + cc;
+    if (c >= cols) break;
+    float M = sm[0][cc];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) so[(w * 16 + col) * SP + Tile::channel(i, g, e)] = o[n][i][e];
-    __syncthreads();
-    for (int i = tid; i < 16 * DH; i += 64 * NW) {
-      const int cc = i / DH, x = i % DH, c = c0 + n * 16 + cc;
-      if (c >= cols) break;
-      float M = sm[0][cc];
+    for (int q = 1; q < NW; ++q) M = fmaxf(M, sm[q][cc]);
+    float L = 0.f, v = 0.f;
 #pragma unroll
-      for (int q = 1; q < NW; ++q) M = fmaxf(M, sm[q][cc]);
-      float L = 0.f, v = 0.f;
-#pragma unroll
-      for (int q = 0; q < NW; ++q) {
-        const float f = kFp32 ? exp_diff(sm[q][cc] - M) : __builtin_amdgcn_exp2f(sm[q][cc] - M);
-        L += sl[q][cc] * f;
-        v += so[(q * 16 + cc) * SP + x] * f;
-      }
-      // nothing seen: 0, with a log-sum-exp of -inf (a NaN sum stays NaN)
-      v = L == 0.f ? 0.f : v / L;
-      const float lse = L == 0.f ? -INFINITY : kFp32 ? M + logf(L / unit) : fmaf(M, 0.6931471805599453f, logf(L));
-      const int j = c / grp, h = sh.hk * grp + c - j * grp;
-      const int64_t at = (int64_t)(sh.row0 + j) * a.n_heads + h;
-      if (sh.parts == 1) {
-        Act<T>::store((T*)a.out + (int64_t)(sh.row0 + j) * a.out_rs + (int64_t)h * DH + x, v);
-        if (a.lse && x == 0) a.lse[at] = lse;
-      } else {
-        a.part_o[(at * a.n_parts + sh.part) * DH + x] = v;
-        if (x == 0) a.part_lse[at * a.n_parts + sh.part] = lse;
-      }
+    for (int q = 0; q < NW; ++q) {
+      const float f = kFp32 ? exp_diff(sm[q][cc] - M) : __builtin_amdgcn_exp2f(sm[q][cc] - M);
+      L += sl[q][cc] * f;
+      v += so[(q * 16 + cc) * SP + x] * f;
+    }
+    // nothing seen: 0, with a log-sum-exp of -inf (a NaN sum stays NaN)
+    v = L == 0.f ? 0.f : v / L;
+    const float lse = L == 0.f ? -INFINITY : kFp32 ? M + logf(L / unit) : fmaf(M, 0.6931471805599453f, logf(L));
+    const int j = c / grp, h = sh.hk * grp + c - j * grp;
+    const int64_t at = (int64_t)(sh.row0 + j) * a.n_heads + h;
+    if (sh.parts == 1) {
+      Act<T>::store((T*)a.out + (int64_t)(sh.row0 + j) * a.out_rs + (int64_t)h * DH + x, v);
+      if (a.lse && x == 0) a.lse[at] = lse;
+    } else {
+      a.part_o[(at * a.n_parts + sh.part) * DH + x] = v;
+      if (x == 0) a.part_lse[at * a.n_parts + sh.part] = lse;
     }
   }
 }
@@ -477,7 +446,8 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void tree_wide_kernel(PagedVi
           s[n][t][i] = __builtin_amdgcn_exp2f(fmaf(s[n][t][i], c2, -R[n]));
           l[n] += s[n][t][i];
         }
-    Values::template pieces<N, 2>(s, part);
+#pragma unroll
+    for (int n = 0; n < N; ++n) Values::template pieces<2>(s[n], part[n]);
   };
   Tile tile;
   bool poison = false;
