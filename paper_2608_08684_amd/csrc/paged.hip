@@ -30,6 +30,10 @@ namespace rk {
 // Bound: memory (each value read once, written once); 17928 rows, 32 / 8 heads of 128:
 // 92 us (4.8 TB/s), a copy of as many bytes 89; 12 fp32 heads of 64: 72 us (4.6).  A step's
 // rows (64 sequences): the latency of one pass, 6 us.
+// 8-bit caches: the lanes that hold a row agree on its largest magnitude, and the row is rounded
+// once, from the rotated fp32 values (a rounding to bf16 in between would move a value that lies
+// next to the middle of two codes to the wrong one).  17928 rows as above: 404 MB, 96 us (4.2
+// TB/s).
 constexpr int kAppendThreads = 256, kAppendRows = 16, kAppendQueryRows = 8;
 
 // cosine and sine of channel pair x at position pos
@@ -711,6 +715,11 @@ __global__ __launch_bounds__(kSelectThreads) void page_select_kernel(PagedView c
 // 32768 50 us (5.1: the join and the first tile's way, lengths to pages to keys, are 9 of
 // them).  8 waves a workgroup, three workgroups per CU, equal runs of tiles for every
 // workgroup whatever the sequences' lengths: all slower or the same.
+// 8-bit caches: a row is half as long, and its codes become bf16 numbers, exactly, on the way to
+// the matrix unit (keys in registers, values before LDS), two conversions a 32-bit word.  64
+// sequences of 4096: 120 us (4.5 TB/s), 32 of 100 .. 8192 66, 2 of up to 32768
+// 24.4, and the join.  Four waves to a SIMD instead of three (fewer registers a wave): 143
+// where 120 stands.
 
 // SEL: attention over selected pages.  kKeys: their keys are in the workspace; kScores:
 // the workgroup forms them; either way its first wave then makes the choice, the same
@@ -720,7 +729,7 @@ enum class Sel { kNone, kKeys, kScores };
 
 template <typename T, typename C, int DH, Sel SEL, int NW = kDecodeWaves>
 __global__ __launch_bounds__(64 * NW) void decode_kernel(PagedView cache, PagedTable tab, DecodeArgs a,
-                                                                   SelectArgs sel) {
+                                                         SelectArgs sel) {
   using Tile = CacheTile<C, DH>;
   constexpr int SP = DH + 4;
   constexpr int AREA0 = Tile::LDS * NW > NW * 16 * SP * 4 ? Tile::LDS * NW : NW * 16 * SP * 4;
@@ -999,6 +1008,9 @@ hipError_t launch_decode(const PagedView& cache, const PagedTable& tab, DecodeAr
   // start are short (32 sequences of 100 .. 8192 entries, 8 KV heads: 118 -> 109 us; 64 equal
   // ones 188 -> 191; more than 64 are taken in their order, a wave has 64 lanes to know them)
   a.longest_first = blocks > 512 && tab.n_seqs <= 64 && !tab.per_head;
+  // 8-bit caches with one workgroup or less to a CU: 8 waves, for as many bytes in flight as bf16
+  // rows have with 4 (192 workgroups of 64 channels 18.5 -> 14.9 us, 240 of 128: 25.0 -> 22.5;
+  // more than one to a CU lose: 480 of 64 channels 15.4 -> 16.3)
 #define RK_DECODE(T, C, DH)                                                                                        \
   do {                                                                                                             \
     constexpr int kMore = std::is_same<C, e4m3_t>::value ? 8 : kDecodeWaves;                                       \
@@ -1053,8 +1065,8 @@ hipError_t launch_decode_selected(const PagedView& cache, const PagedTable& tab,
   const uint32_t blocks = (uint32_t)((int64_t)rows * head_tiles * a.n_parts);
 #define RK_DECODE(T, C, DH)                                                                                           \
   do {                                                                                                                \
-    if (alone) decode_kernel<T, C, DH, Sel::kScores><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, d, sel);           \
-    else decode_kernel<T, C, DH, Sel::kKeys><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, d, sel);                   \
+    if (alone) decode_kernel<T, C, DH, Sel::kScores><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, d, sel);        \
+    else decode_kernel<T, C, DH, Sel::kKeys><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, d, sel);                \
     if (a.n_parts > 1)                                                                                                \
       decode_join_kernel<T, DH><<<tab.n_seqs * a.n_heads, 256, 0, s>>>(lists, d, cache.n_kv, cache.page_shift);       \
   } while (0)

@@ -74,6 +74,10 @@ struct Share {
 __device__ __forceinline__ bool sees(uint64_t word, int draft) { return draft < 0 || (word >> (draft & 63) & 1); }
 
 // --------------------------------------------------------------------------- few columns
+// As the attention of one token, with a draft's mask for each column.  Weights in three bf16 pieces.
+// Bound: memory where entries are many (2 sequences of 8192, 16 columns of 128: 23.6 us), else the
+// latency of lengths -> pages -> tiles -> join through LDS (one fp32 sequence of 257, 5 drafts, three
+// rounds of tiles: 10.7 us).
 template <typename T, typename C, int DH>
 __global__ __launch_bounds__(64 * kDecodeWaves) void tree_narrow_kernel(PagedView cache, PagedTable tab, SeqTable st,
                                                                         TreeArgs a) {
@@ -331,6 +335,17 @@ template <typename C, int DH> struct WideTile {
 // and then multiplies them with the values, and the next 32 entries' keys with its queries
 // (matrix unit).  The waves read all of K and V from LDS; 32 columns a wave keep that below what
 // the products take.
+// Weights enter the product in two bf16 pieces: what is left out, at most 2^-16 of a weight, is
+// 2^-8 of the output's own rounding.  One piece (2^-8 of a weight) took 117 us where two take 135,
+// with outputs off by up to 1.4 times as much.
+// Bound: the vector unit (53% of the cycles: exponentials, pieces, rows widened to bf16) and
+// the matrix unit (37%), which two waves to a SIMD, all that 256 registers leave, hardly overlap: a
+// tile takes a lone workgroup 2.6 us.  16 sequences of 100 .. 8192 in e4m3, 64 drafts of 32 query
+// heads of 128 over 8 KV heads: 144 us (0.45 PFLOP/s of the formula's products); 8 of 500 .. 4096 in
+// bf16, up to 26 drafts: 34 us.  The waves' priority in the matrix part: 167 -> 154 of the first.  Not
+// taken: 8 waves in two groups that alternate between the units (157 where 150 stood), vector and
+// matrix instructions mixed by the schedule (154 -> 280, registers spill), one block of 16 columns
+// a wave for all (179).
 template <typename C, int DH, int N>
 __global__ __launch_bounds__(64 * kDecodeWaves, 2) void tree_wide_kernel(PagedView cache, PagedTable tab, SeqTable st,
                                                                          TreeArgs a) {
