@@ -336,7 +336,7 @@ template <typename C, int DH> struct WideTile {
 // (matrix unit).  The waves read all of K and V from LDS; 32 columns a wave keep that below what
 // the products take.
 // Weights enter the product in two bf16 pieces: what is left out, at most 2^-16 of a weight, is
-// 2^-8 of the output's own rounding.  One piece (2^-8 of a weight) took 117 us where two take 135,
+// 2^-8 of the output's own rounding.  One piece (2^-8 of a weight) took 117 us where two took 135,
 // with outputs off by up to 1.4 times as much.
 // Bound: the vector unit (53% of the cycles: exponentials, pieces, rows widened to bf16) and
 // the matrix unit (37%), which two waves to a SIMD, all that 256 registers leave, hardly overlap: a
@@ -576,7 +576,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void tree_wide_kernel(PagedVi
     l[n] += __shfl_xor(l[n], 32, 64);
     const int c = c0 + n * 16 + col;
     if (c >= cols) continue;
-    const float L = l[n], inv = L == 0.f ? 0.f : 1.f / L;   // nothing seen: 0, with a log-sum-exp of -inf
+    const float L = l[n], inv = L == 0.f ? 0.f : 1.f / (L * kTwoPieces);   // nothing seen: 0, with a log-sum-exp of -inf
     const float lse = L == 0.f ? -INFINITY : fmaf(R[n], 0.6931471805599453f, logf(L));
     const int j = c / grp, h = sh.hk * grp + c - j * grp;
     const int64_t row = (int64_t)(sh.row0 + j) * a.n_heads + h;
