@@ -135,13 +135,19 @@ template <> __device__ __forceinline__ bool take_out<bf16_t>(v4u& v, int sign) {
   bool any = false;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
+    if (sign == 0) {   // an exponent of ones carries into the bit above it
+      const uint32_t over = ((v[w] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+      any |= over != 0;
+      v[w] &= ~((over >> 15) * 0xffffu);
+      continue;
+    }
     uint32_t r = 0;
 #pragma unroll
     for (int at = 0; at < 32; at += 16) {
       const uint32_t x = v[w] >> at & 0xffffu;
       const bool bad = (x & 0x7f80u) == 0x7f80u, mine = bad && ((x & 0x7fu) || (x >> 15) == (sign < 0));
       any |= bad;
-      r |= (sign == 0 ? (bad ? 0u : x) : mine ? (sign < 0 ? 0xc000u : 0x4000u) : 0u) << at;
+      r |= (mine ? (sign < 0 ? 0xc000u : 0x4000u) : 0u) << at;
     }
     v[w] = r;
   }
@@ -151,13 +157,19 @@ template <> __device__ __forceinline__ bool take_out<e4m3_t>(v4u& v, int sign) {
   bool any = false;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
+    if (sign == 0) {
+      const uint32_t over = ((v[w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+      any |= over != 0;
+      v[w] &= ~((over >> 7) * 0xffu);
+      continue;
+    }
     uint32_t r = 0;
 #pragma unroll
     for (int at = 0; at < 32; at += 8) {
       const uint32_t x = v[w] >> at & 0xffu;
       const bool bad = (x & 0x7fu) == 0x7fu;
       any |= bad;
-      r |= (sign == 0 ? (bad ? 0u : x) : bad ? (sign < 0 ? 0xc0u : 0x40u) : 0u) << at;
+      r |= (bad ? (sign < 0 ? 0xc0u : 0x40u) : 0u) << at;
     }
     v[w] = r;
   }

@@ -71,7 +71,12 @@ struct Share {
   }
 };
 
-__device__ __forceinline__ bool sees(uint64_t word, int draft) { return draft < 0 || (word >> (draft & 63) & 1); }
+// A bit for each of 32 entries that a column sees: the text's, then by its mask.  first: the first one's
+// number among the drafts (negative: text).
+__device__ __forceinline__ uint32_t sees(uint64_t word, int first) {
+  if (first >= 0) return (uint32_t)(word >> (first & 63));
+  return first <= -32 ? ~0u : (uint32_t)word << -first | ((1u << -first) - 1u);
+}
 
 // --------------------------------------------------------------------------- few columns
 // As the attention of one token, with a draft's mask for each column.  Weights in three bf16 pieces.
@@ -136,13 +141,11 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void tree_narrow_kernel(PagedVie
   };
   // scores of what is not seen, or by the mask not seen by the column, are -inf
   const auto hide = [&](f32x4_t* s, int k0, uint32_t seen) {
+    const uint32_t on = (seen & sees(word, k0 - base)) >> 4 * g;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int at = k0 + t * 16 + 4 * g - base;   // draft of the lane's first entry of this half
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (!(seen >> (t * 16 + 4 * g + i) & 1) || !sees(word, at + i)) s[t][i] = -INFINITY;
-    }
+      for (int i = 0; i < 4; ++i) s[t][i] = on >> (t * 16 + i) & 1 ? s[t][i] : -INFINITY;
   };
   const auto weight = [&](float s) {
     return kFp32 ? exp_diff_exact(s * a.scale - R, unit) : __builtin_amdgcn_exp2f(fmaf(s, c2, -R));
@@ -419,13 +422,12 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void tree_wide_kernel(PagedVi
   const auto hide = [&](f32x4_t (*s)[2], int k0, uint32_t seen) {
     if (seen == 0xffffffffu && k0 + 32 <= base) return;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int at = k0 + t * 16 + 4 * g - base;
+    for (int n = 0; n < N; ++n) {
+      const uint32_t on = (seen & sees(word[n], k0 - base)) >> 4 * g;
 #pragma unroll
-      for (int n = 0; n < N; ++n)
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (!(seen >> (t * 16 + 4 * g + i) & 1) || !sees(word[n], at + i)) s[n][t][i] = -INFINITY;
+        for (int i = 0; i < 4; ++i) s[n][t][i] = on >> (t * 16 + i) & 1 ? s[n][t][i] : -INFINITY;
     }
   };
   const auto raise = [&](const f32x4_t (*s)[2]) {
