@@ -341,14 +341,16 @@ template <typename C, int DH> struct WideTile {
 // Weights enter the product in two bf16 pieces: what is left out, at most 2^-16 of a weight, is
 // 2^-8 of the output's own rounding.  One piece (2^-8 of a weight) took 117 us where two took 135,
 // with outputs off by up to 1.4 times as much.
-// Bound: the vector unit (53% of the cycles: exponentials, pieces, rows widened to bf16) and
-// the matrix unit (37%), which two waves to a SIMD, all that 256 registers leave, hardly overlap: a
-// tile takes a lone workgroup 2.6 us.  16 sequences of 100 .. 8192 in e4m3, 64 drafts of 32 query
-// heads of 128 over 8 KV heads: 144 us (0.45 PFLOP/s of the formula's products); 8 of 500 .. 4096 in
-// bf16, up to 26 drafts: 34 us.  The waves' priority in the matrix part: 167 -> 154 of the first.  Not
-// taken: 8 waves in two groups that alternate between the units (157 where 150 stood), vector and
-// matrix instructions mixed by the schedule (154 -> 280, registers spill), one block of 16 columns
-// a wave for all (179).
+// Bound: issue.  The vector unit is busy 54% of the cycles (a fifth of that are the matrix
+// instructions' own) and the matrix unit 40%, and they go together badly: a wave's 32 matrix
+// instructions beside another's 128 fmas take 0.67 of the sum of both, two waves that do both in turn
+// 0.8 - 0.86.  256 registers leave two waves to a SIMD.  16 sequences of 100 .. 8192 in e4m3, 64
+// drafts of 32 query heads of 128 over 8 KV heads: 131 us (0.50 PFLOP/s of the formula's products); 8
+// of 500 .. 4096 in bf16, up to 26 drafts: 31 us.  The waves' priority in the matrix part: 167 -> 154 of
+// the first, then.  Not taken: 8 waves in two groups that alternate between the units (157 where 150
+// stood), vector and matrix instructions mixed by the schedule (154 -> 280, registers spill), one block
+// of 16 columns a wave for all (179), keys half a tile ahead of the values for one barrier a tile
+// instead of two (147 -> 152), another priority for every second wave (146 -> 153 .. 158).
 template <typename C, int DH, int N>
 __global__ __launch_bounds__(64 * kDecodeWaves, 2) void tree_wide_kernel(PagedView cache, PagedTable tab, SeqTable st,
                                                                          TreeArgs a) {
@@ -637,17 +639,19 @@ __global__ __launch_bounds__(256) void tree_join_kernel(PagedTable tab, SeqTable
 
 // Columns of a workgroup, for the widest tree of a call, and whether its waves share their tiles.
 // Sharing pays where entries are many or workgroups are: a tile takes a workgroup 2.6 us by
-// itself, and a shared one starts 3 us later (bf16, 8 KV heads of 128: 1 sequence of 360, 148
-// columns: 12.4 us not shared, 24.3 shared; 4 of 1000, 104: 20 and 30; 8 of 2048, 32: 31.5 and
-// 24.6; 2 of 8192, 64: 41 and 29; 60 of 300, 64: 105 and 26).  fp32 has no shared kernel: its
-// products take eight times as long as its loads.
+// itself, and a shared one starts 3 us later.  bf16, 8 KV heads of 128, us not shared | shared: 1
+// sequence of 360, 148 columns 11.4 | 21.8; 4 of 1000, 104: 19.0 | 27.2; 1 of 1500, 256: 18.9 | 27.4; 1 of
+// 4096, 64: 17.8 | 19.4; 8 of 2048, 32: 26.2 | 24.5; 2 of 8192, 64: 34.7 | 27.9; 60 of 300, 64: 63.7 | 25.2.
+// 12 KV heads of 64: 2 of 900, 30 columns 11.1 | 14.6; 4 of 2048, 32: 16.8 | 16.3.  fp32 has no shared
+// kernel: its products take eight times as long as its loads.
 struct Width {
   int columns;
   bool shared;
 };
 Width width_of(const PagedView& cache, int n_seqs, int max_drafts, int n_heads, int64_t max_entries) {
   const int64_t cols = (int64_t)max_drafts * (n_heads / cache.n_kv);
-  const bool few = max_entries <= 1024 && (int64_t)n_seqs * cache.n_kv * ((cols + 15) / 16) <= 256;
+  const int64_t narrow = (int64_t)n_seqs * cache.n_kv * ((cols + 15) / 16);
+  const bool few = narrow <= 256 && (max_entries <= 1024 || narrow * max_entries <= 1600 * cache.head_dim);
   if (cols <= 16 || !cache.bf16 || few) return {16, false};
   return {cols <= 64 ? 64 : 128, true};
 }
@@ -655,11 +659,12 @@ Width width_of(const PagedView& cache, int n_seqs, int max_drafts, int n_heads, 
 }  // namespace
 
 // Parts of a length: two workgroups to a CU, in parts of 256 entries or more (of a workgroup whose
-// waves share their tiles; 512 otherwise, as in the attention of one token); and twice as many
-// of 1024 or more (512 of 64 channels), so that unequal lengths level out: what a part costs,
-// its fp32 outputs written and read again, has to be little beside its entries.
+// waves share their tiles, or up to 24 of 128; 512 otherwise, as in the attention of one token); and
+// twice as many of 1024 or more (512 of 64 channels), so that unequal lengths level out: what a part
+// costs, its fp32 outputs written and read again, has to be little beside its entries.
 //   2 x 8192 entries, 64 columns of 128: 16 parts of 512 29.0, 32 of 256 28.5; 16 columns: 23.6 and 32.1;
-//   4 x 1000, 104 columns: 1 part 54.5, 3 30.1; 16 x 4096, 64 columns: 4 parts 72, 8 84;
+//   1 x 3000, 256 columns: 11 parts of 256 28.2, 23 of 128 25.5; 2 x 4096, 104: 16 of 256 26.8, 32 28.4;
+//   4 x 1000, 104 columns, shared: 1 part 54.5, 3 30.1; 16 x 4096, 64 columns: 4 parts 72, 8 84;
 //   16 x 100 .. 8192, 256 columns: 2 parts 190, 4 150, 8 180 (all of 4096: 146, 157, 185);
 //   16 x 100 .. 2048, 32 columns of 64: 2 parts 29.2, 4 22.2.
 int tree_parts(const PagedView& cache, int n_seqs, int max_drafts, int n_heads, int64_t max_entries) {
@@ -667,9 +672,19 @@ int tree_parts(const PagedView& cache, int n_seqs, int max_drafts, int n_heads, 
   const int64_t cols = (int64_t)max_drafts * (n_heads / cache.n_kv);
   const int64_t rows = (int64_t)n_seqs * cache.n_kv * ((cols + width.columns - 1) / width.columns);
   const int64_t least = std::max(512, 8 * cache.head_dim);
-  const int64_t fill = std::min(512 / rows, max_entries / (width.shared ? 256 : 512));
+  const int64_t fill = std::min(512 / rows, width.shared ? std::max(max_entries / 256, std::min<int64_t>(max_entries / 128, 24))
+                                                         : max_entries / 512);
   const int64_t level = std::min(1024 / rows, max_entries / least);
   return (int)std::max<int64_t>(1, std::min<int64_t>(std::max(fill, level), kMaxTreeParts));
+}
+
+// As many of them as the longest sequence has when each has whole tiles for every wave
+// (part_entries); workgroups for more would end at once, and leave some CUs less to do than others (2 x
+// 4096, 104 columns, 24 parts that are 16: 26.8 us, 28.5 with the empty ones).
+int tree_full_parts(int n_parts, int64_t max_entries) {
+  constexpr int64_t unit = kTile * kDecodeWaves;
+  const int64_t each = ((max_entries + n_parts - 1) / n_parts + unit - 1) / unit * unit;
+  return (int)((max_entries + each - 1) / each);
 }
 
 int64_t tree_blocks(const PagedView& cache, const PagedTable& tab, const SeqTable& st, const TreeArgs& a) {

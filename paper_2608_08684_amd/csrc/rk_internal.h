@@ -300,6 +300,7 @@ struct TreeArgs {
 constexpr int kMaxTreeParts = 64;
 // Parts that the length is split into, for trees of up to max_drafts rows.
 int tree_parts(const PagedView& cache, int n_seqs, int max_drafts, int n_heads, int64_t max_entries);
+int tree_full_parts(int n_parts, int64_t max_entries);
 int64_t tree_blocks(const PagedView& cache, const PagedTable& tab, const SeqTable& st, const TreeArgs& a);   // workgroups
 // st: the drafts' rows, max_len the most of a sequence (at least 1).
 hipError_t launch_tree(const PagedView& cache, const PagedTable& tab, const SeqTable& st, TreeArgs a, hipStream_t s);

@@ -359,7 +359,8 @@ rk_status rk_paged_attention_tree(const rk_paged_cache* cache, const rk_paged_se
   if (ws_bytes < p.total) { set_error("workspace too small (%zu < %zu)", ws_bytes, p.total); return RK_ERR_WORKSPACE; }
   TreeArgs a{};
   a.q = q; a.out = out; a.lse = lse; a.masks = masks; a.q_rs = q_row_stride; a.out_rs = out_row_stride;
-  a.n_heads = n_heads; a.n_parts = p.n_parts;
+  a.n_heads = n_heads;
+  a.n_parts = tree_full_parts(p.n_parts, (int64_t)t.max_pages << v.page_shift);
   a.scale = scale > 0.f ? scale : (float)(1.0 / sqrt((double)v.head_dim));
   a.part_o = (float*)workspace; a.part_lse = (float*)((char*)workspace + p.part_lse);
   if (tree_blocks(v, t, st, a) > kMaxWorkgroups) return bad(RK_ERR_SHAPE, "more heads and drafts than a launch takes");
