@@ -124,6 +124,19 @@ def test_long_lengths_are_split_and_joined(heads, kv_heads, d, page, dtype, coun
     drafts.check(*drafts.run())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("lengths, counts", [
+    ([9000, 300, 4100, 1], [8, 5, 3, 1]),    # 32 columns a KV head over long caches: waves with one block of them
+    ([3000], [64]),                          # 256 columns, parts of 128 entries
+    ([1500], [61]),                          # 244 columns, 16 a workgroup
+    ([4090, 3000], [26, 11]),                # fewer parts than 512 workgroups would be
+])
+def test_lengths_and_widths_between(dtype, lengths, counts):
+    case = make(lengths, 32, 8, 128, 64 if dtype == "e4m3" else 16, dtype, seed=len(lengths))
+    drafts = Drafts(case, counts, seed=4)
+    drafts.check(*drafts.run())
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "e4m3", "f32"])
 def test_many_sequences(dtype):
     n = rk.RK_MAX_BATCH_SEQS
@@ -242,6 +255,46 @@ def test_non_finite_drafts_reach_those_who_see_them(dtype, bad, heads):
     put("k")
     out, lse = drafts.run()
     assert torch.equal(out[~hit], ref[~hit]) and torch.equal(lse[~hit], ref_lse[~hit])
+
+
+@pytest.mark.parametrize("heads, kv_heads, d, page, dtype", [
+    (4, 4, 64, 16, "bf16"), (8, 2, 128, 16, "bf16"), (24, 1, 64, 32, "bf16"), (4, 2, 32, 16, "f32"), (8, 2, 128, 64, "f32"),
+])
+@pytest.mark.parametrize("lengths, counts", [([700, 40], [3, 1]), ([5000, 1300], [40, 24])])
+def test_infinite_values_of_the_text(heads, kv_heads, d, page, dtype, lengths, counts):
+    """Every draft sees them, and a weight is positive however small: their channels are those infinities."""
+    case = make(lengths, heads, kv_heads, d, page, dtype, seed=17)
+    drafts = Drafts(case, counts, seed=17)
+    ref, ref_lse = drafts.run()
+    put = {0: float("inf"), d // 2 + 1: -float("inf"), d - 1: float("inf")}
+    for i, n in enumerate(lengths):
+        for (channel, x), u in zip(put.items(), (0, (n - counts[i]) // 2, n - counts[i] - 1)):
+            case.v[int(case.table[i, u // page]), :, u % page, channel] = x
+    out, lse = drafts.run()
+    for channel, x in put.items():
+        assert (out[:, :, channel] == x).all(), channel
+    rest = [x for x in range(d) if x not in put]
+    assert (out[:, :, rest] == ref[:, :, rest]).all() and (lse == ref_lse).all()
+
+
+@pytest.mark.parametrize("drafts, heads", [(2, 4), (12, 8), (40, 16)])   # 4, 48 and 320 columns a KV head
+@pytest.mark.parametrize("dtype, d", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+def test_infinite_values_of_small_weight(drafts, heads, dtype, d):
+    """A weight of e^-50 of the largest."""
+    case = make([2048] * 4, heads, 2, d, 16, dtype, seed=18)
+    case.k.zero_()
+    for i in range(4):
+        case.k[int(case.table[i, 0]), :, 0, 0] = 5.0
+        for channel, u, x in ((3, 1, float("inf")), (d - 2, 1700, -float("inf"))):
+            case.v[int(case.table[i, u // 16]), :, u % 16, channel] = x
+    rows = Drafts(case, [drafts] * 4, seed=18)
+    rows.q.zero_()
+    rows.q[:, :, 0] = 10.0
+    out, lse = rows.run(scale=1.0)
+    assert (out[:, :, 3] == float("inf")).all() and (out[:, :, d - 2] == -float("inf")).all()
+    assert (lse == 50.0).all()
+    rest = [x for x in range(d) if x not in (3, d - 2)]
+    assert out[:, :, rest].isfinite().all()
 
 
 def test_infinities_of_both_signs():
