@@ -513,7 +513,8 @@ rk_status rk_spearman(const double *x, const double *y, int32_t n, double *rho);
  * of the least power of two, 2^-117 at least, of which its largest finite magnitude is at
  * most 448.  Infinities and NaN become NaN, what would round to 2^128 becomes 1.875 2^127.
  * The values that are left are bf16 numbers, and every call that reads the cache does so as
- * if it held those.                                                                */
+ * if it held those.  (Bytes 10 .. 247 occur.  In a cache that is filled otherwise, other bytes
+ * too, a value is the bf16 number nearest to it, an infinity from 2^128 on.)           */
 typedef struct {
   void *k, *v;
   void *key_bounds;

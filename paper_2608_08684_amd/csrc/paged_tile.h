@@ -129,9 +129,9 @@ __device__ __forceinline__ void from_e4m3(v2u u, uint32_t b, float* x) {
 }
 
 // 16 bytes of values: infinities and NaN become 0 (sign 0), or all others do, and those of that
-// sign and NaN become 2 or -2 (sign 1 or -1); whether there are any.
-template <typename C> __device__ __forceinline__ bool take_out(v4u& v, int sign);
-template <> __device__ __forceinline__ bool take_out<bf16_t>(v4u& v, int sign) {
+// sign and NaN become 2 or -2 (sign 1 or -1); whether there are any.  scale: 8-bit rows' byte.
+template <typename C> __device__ __forceinline__ bool take_out(v4u& v, int sign, uint32_t scale = 127);
+template <> __device__ __forceinline__ bool take_out<bf16_t>(v4u& v, int sign, uint32_t) {
   bool any = false;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
@@ -153,12 +153,15 @@ template <> __device__ __forceinline__ bool take_out<bf16_t>(v4u& v, int sign) {
   }
   return any;
 }
-template <> __device__ __forceinline__ bool take_out<e4m3_t>(v4u& v, int sign) {   // NaN alone: of either sign
+// NaN, and what a scale byte above 246 takes to 2^128 or more, an infinity as bf16: a code c of exponent
+// c >> 3 stands for 2^((c >> 3) - 7 + scale - 127) or more, so c from 8 (262 - scale) on.
+template <> __device__ __forceinline__ bool take_out<e4m3_t>(v4u& v, int sign, uint32_t scale) {
+  const uint32_t carry = (uint32_t)max(1, 8 * ((int)scale - 246));   // takes the least of them to 0x80, NaN's 0x7f too
   bool any = false;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
     if (sign == 0) {
-      const uint32_t over = ((v[w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+      const uint32_t over = ((v[w] & 0x7f7f7f7fu) + carry * 0x01010101u) & 0x80808080u;
       any |= over != 0;
       v[w] &= ~((over >> 7) * 0xffu);
       continue;
@@ -166,16 +169,16 @@ template <> __device__ __forceinline__ bool take_out<e4m3_t>(v4u& v, int sign) {
     uint32_t r = 0;
 #pragma unroll
     for (int at = 0; at < 32; at += 8) {
-      const uint32_t x = v[w] >> at & 0xffu;
-      const bool bad = (x & 0x7fu) == 0x7fu;
+      const uint32_t x = v[w] >> at & 0xffu, code = x & 0x7fu;
+      const bool bad = code + carry >= 0x80u, mine = bad && (code == 0x7fu || (x >> 7) == (sign < 0));
       any |= bad;
-      r |= (bad ? (sign < 0 ? 0xc0u : 0x40u) : 0u) << at;
+      r |= (mine ? (sign < 0 ? 0xc0u : 0x40u) : 0u) << at;
     }
     v[w] = r;
   }
   return any;
 }
-template <> __device__ __forceinline__ bool take_out<float>(v4u& v, int sign) {
+template <> __device__ __forceinline__ bool take_out<float>(v4u& v, int sign, uint32_t) {
   bool any = false;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
@@ -397,7 +400,7 @@ template <int DH> struct CacheTile<e4m3_t, DH> : StagedValues<DH> {
     bool any = false;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      any |= take_out<e4m3_t>(v[i], sign);
+      any |= take_out<e4m3_t>(v[i], sign, vs[i]);
       if (sign != 0) vs[i] = 127;
     }
     return any;

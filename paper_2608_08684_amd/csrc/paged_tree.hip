@@ -308,9 +308,12 @@ template <typename C, int DH> struct WideTile {
     bool any = false;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      any |= take_out<C>(v[i], sign);
-      if constexpr (kScaled)
+      if constexpr (kScaled) {
+        any |= take_out<C>(v[i], sign, vs[i]);
         if (sign != 0) vs[i] = 127;
+      } else {
+        any |= take_out<C>(v[i], sign);
+      }
     }
     return any;
   }
