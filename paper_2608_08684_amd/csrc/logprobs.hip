@@ -162,6 +162,59 @@ __device__ __forceinline__ Sums wave_sums(Sums q) {
   return Sums{m, wave_total(q.s), wave_total(q.t)};
 }
 
+__device__ __forceinline__ double wave_total(double x) {
+#define RK_STEP(ctrl, rows)                                                                                   \
+  {                                                                                                           \
+    const uint64_t u = (uint64_t)__double_as_longlong(x);                                                     \
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)u, ctrl, rows, 0xf, false);             \
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(u >> 32), ctrl, rows, 0xf, false);     \
+    x += __longlong_as_double((long long)((uint64_t)hi << 32 | lo));                                          \
+  }
+  RK_STEP(0x111, 0xf) RK_STEP(0x112, 0xf) RK_STEP(0x114, 0xf) RK_STEP(0x118, 0xf)
+  RK_STEP(0x142, 0xa) RK_STEP(0x143, 0xc)
+#undef RK_STEP
+  const uint64_t u = (uint64_t)__double_as_longlong(x);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)u, 63);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), 63);
+  return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+}
+
+// The same for beams, whose scores are compared with each other: the exponentials are fp32's, what
+// is done with them is done in doubles, at no cost (128 rows of 128256 fp32 logits: 15.3 us either
+// way).  log S is then 1e-8 off in the mean, 7e-8 at most on a language model's logits, where fp32
+// sums left 8e-8 and 4e-7; what remains is the exponentials', so that a row's largest logit, whose
+// exponential is 1, adds nothing to it: with a token of probability 0.9999 it is 1e-12.
+// Exponentials in doubles too, 17 instructions of half rate a logit: 23 us.
+struct BeamSums {
+  float c;
+  float t;
+  double s;
+  __device__ __forceinline__ float ref() const { return c == -INFINITY ? 0.f : c; }
+  __device__ __forceinline__ void raise(float c2) {
+    const float d = fmaxf(c - c2, -1.0e4f), f = __builtin_amdgcn_exp2f(d * kLog2e);
+    t = f * fmaf(d, (float)s, t);
+    s *= (double)f;
+    c = c2;
+  }
+  // S: every exponent above is (1 + e) of what it should be, fp32's log2(e) being 1.9259630e-8
+  // too small, so the sum is off by e T
+  __device__ __forceinline__ double sum() const { return s + 1.9259630e-8 * 0.69314718055994531 * (double)t; }
+  // as the workspace holds them
+  __device__ __forceinline__ float4 packed() const {
+    const uint64_t u = (uint64_t)__double_as_longlong(s);
+    return make_float4(c, t, __uint_as_float((uint32_t)u), __uint_as_float((uint32_t)(u >> 32)));
+  }
+  static __device__ __forceinline__ BeamSums of(float4 f) {
+    const uint64_t u = (uint64_t)__float_as_uint(f.w) << 32 | __float_as_uint(f.z);
+    return {f.x, f.y, __longlong_as_double((long long)u)};
+  }
+};
+__device__ __forceinline__ BeamSums wave_sums(BeamSums q) {
+  const float m = from_order(wave_max(order_bits(q.c)));
+  if (m > -INFINITY) q.raise(m);
+  return BeamSums{m, wave_total(q.t), wave_total(q.s)};
+}
+
 constexpr int kPasses = 4;         // vectors in flight per lane
 constexpr int kTopGroups = 4096;   // groups of a row or part: 65536 vectors
 constexpr int kTopLook = 128;      // groups looked at again
@@ -381,7 +434,8 @@ __device__ __forceinline__ bool beam_open(const BeamArgs& b, int64_t r) {
 template <typename T, int NT, bool TOP, bool BEAM = false>
 __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a, BeamArgs beam) {
   constexpr int N = Logit<T>::N, NW = NT / 64, U = kPasses;
-  __shared__ Sums sums[NW];
+  using RowSums = std::conditional_t<BEAM, BeamSums, Sums>;
+  __shared__ RowSums sums[NW];
   __shared__ int counts[NW];
   __shared__ std::conditional_t<TOP, TopShared<NT>, int> sh;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -400,7 +454,8 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a, BeamArgs bea
   // x >= xt is x > below, the next float down (xt = -inf is counted index by index)
   const int bits = __float_as_int(xt);
   const float below = xt == 0.f ? __int_as_float((int)0x80000001) : __int_as_float(bits < 0 ? bits + 1 : bits - 1);
-  Sums q{-INFINITY, 0.f, 0.f};
+  RowSums q{};                          // sums of nothing
+  q.c = -INFINITY;
   float c = 0.f;                        // q.ref()
   int count = 0;                        // wave-uniform
   uint32_t best_key = 0;
@@ -443,7 +498,8 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a, BeamArgs bea
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         const float d = f[e] - c, p = __builtin_amdgcn_exp2f(d * kLog2e);
-        s += p;
+        if constexpr (BEAM) q.s += (double)p;
+        else s += p;
         t = fmaf(p, fmaxf(d, -1.0e4f), t);
       }
       if (has) {
@@ -461,7 +517,7 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a, BeamArgs bea
         }
       }
     }
-    q.s += s;
+    if constexpr (!BEAM) q.s += s;
     q.t += t;
     if constexpr (TOP) {
       // a group holds logits if its first vector does
@@ -480,21 +536,29 @@ __global__ __launch_bounds__(NT) void logprob_kernel(LogprobArgs a, BeamArgs bea
     if (tid == 0) { sh.n_chosen = 0; sh.n_list = 0; }
   }
   __syncthreads();
-  q = wave_sums(lane < NW ? sums[lane] : Sums{-INFINITY, 0.f, 0.f});
+  RowSums mine{};
+  mine.c = -INFINITY;
+  if (lane < NW) mine = sums[lane];
+  q = wave_sums(mine);
   count = wave_count(lane < NW ? counts[lane] : 0);
   if (BEAM || a.parts > 1) {
-    if (tid == 0) a.part[r * a.parts + part] = make_float4(q.c, q.s, q.t, __int_as_float(count));
+    if (tid == 0) {
+      if constexpr (BEAM) a.part[r * a.parts + part] = q.packed();
+      else a.part[r * a.parts + part] = make_float4(q.c, q.s, q.t, __int_as_float(count));
+    }
     if constexpr (TOP)
       top_logits<T, NT>(x, a.n_top, (x.n_vec + NT * U - 1) / (NT * U) * (NT / 4), sh, [&](int i, uint32_t k, int id) {
         a.part_top[(r * a.parts + part) * a.n_top + i] = (uint64_t)k << 32 | (uint32_t)~(id + first);
       });
     return;
   }
-  const RowResult res(a, r, q, count, has, x_tok);
-  if (tid == 0) res.write(a, r);
-  if constexpr (TOP)
-    top_logits<T, NT>(x, a.n_top, (x.n_vec + NT * U - 1) / (NT * U) * (NT / 4), sh,
-                      [&](int i, uint32_t k, int id) { res.put(a, r, i, k, id); });
+  if constexpr (!BEAM) {
+    const RowResult res(a, r, q, count, has, x_tok);
+    if (tid == 0) res.write(a, r);
+    if constexpr (TOP)
+      top_logits<T, NT>(x, a.n_top, (x.n_vec + NT * U - 1) / (NT * U) * (NT / 4), sh,
+                        [&](int i, uint32_t k, int id) { res.put(a, r, i, k, id); });
+  }
 }
 
 // Joins the parts of a row: their sums, and the first n_top of their n_top best logits each.
@@ -558,19 +622,32 @@ hipError_t launch_logprobs(const LogprobArgs& a, bool bf16, hipStream_t s) {
 // lane l of its first wave holds the head of list l, and n_out times the best head is taken and
 // its list moved on.  More than 64 lists (rows in many parts) are first cut to the 64 with the
 // best heads: a list with n_out better heads beside it gives nothing.  Scores between beams are
-// doubles of the logit, so that the order hangs on nothing but log S; within a beam the logits
-// decide.
+// doubles, log S among them (BeamSums says how good it is); within a beam the logits decide.
 // Bound: latency, a chain of loads, sums and n_out short steps: 6.9 us for the 8 best of 16 lists,
 // 4.7 for the 4 best of 12.  The rows' kernel before it reads every logit once (128 rows of 128256
 // fp32 in two parts: 15.5 us, 4.2 TB/s; 4 rows of 50257 bf16: 8.5).
 // (lists: 256 where rows are split to fill the card, 17 a row of 2^22 fp32 logits)
 constexpr int kMaxLists = 17 * RK_MAX_BEAMS;
 
-// log of a positive finite sum: the exponent's part in double, the rest below 0.7
-__device__ __forceinline__ double log_sum(float s) {
-  const int e = (int)(__float_as_uint(s) >> 23) - 127;
-  const float m = __uint_as_float((__float_as_uint(s) & 0x7fffffu) | 0x3f800000u);
-  return e * 0.69314718055994530942 + (double)logf(m);
+// log of a positive finite sum, 2^e m: logf(m), and what m times e^-that is above 1
+__device__ __forceinline__ double log_sum(double s) {
+  const uint64_t u = (uint64_t)__double_as_longlong(s);
+  const int e = (int)(u >> 52) - 1023;
+  const double m = __longlong_as_double((long long)((u & 0xfffffffffffffull) | 0x3ff0000000000000ull));
+  const double y = (double)logf((float)m), z = -0.5 * y;     // e^z, |z| < 0.35, by its series: squared, 2e-15 off
+  double p = 1.0 / 39916800.0;
+  p = fma(p, z, 1.0 / 3628800.0);
+  p = fma(p, z, 1.0 / 362880.0);
+  p = fma(p, z, 1.0 / 40320.0);
+  p = fma(p, z, 1.0 / 5040.0);
+  p = fma(p, z, 1.0 / 720.0);
+  p = fma(p, z, 1.0 / 120.0);
+  p = fma(p, z, 1.0 / 24.0);
+  p = fma(p, z, 1.0 / 6.0);
+  p = fma(p, z, 0.5);
+  p = fma(p, z, 1.0);
+  p = fma(p, z, 1.0);
+  return e * 0.69314718055994530942 + (y + fma(m * p, p, -1.0));
 }
 
 // A candidate as a whole number that orders like its score, 0 for none; its logit's order with
@@ -615,23 +692,18 @@ __global__ __launch_bounds__(256) void beam_join_kernel(LogprobArgs a, BeamArgs 
   if (lists <= 64)
     for (int i = tid; i < lists * n; i += NT) list[i] = top[i];
   __syncthreads();
-  if (parts == 1) {
-    if (tid < nb) {
-      const float4 f = sums[tid];
-      ref[tid] = Sums{f.x, f.y, f.z}.ref();
-      // without a finite largest logit S is 0 or NaN
-      shift[tid] = f.y > 0.f && f.y < INFINITY ? (double)score[tid] - log_sum(f.y) : -INFINITY;
-    }
-  } else {
+  if (parts > 1) {
     for (int b = w; b < nb; b += NT / 64) {
-      Sums q{-INFINITY, 0.f, 0.f};
-      if (lane < parts) { const float4 f = sums[b * parts + lane]; q = Sums{f.x, f.y, f.z}; }
-      q = wave_sums(q);
-      if (lane == 0) {
-        ref[b] = q.ref();
-        shift[b] = q.s > 0.f && q.s < INFINITY ? (double)score[b] - log_sum(q.s) : -INFINITY;
-      }
+      const BeamSums q = wave_sums(lane < parts ? BeamSums::of(sums[b * parts + lane]) : BeamSums{-INFINITY, 0.f, 0.0});
+      if (lane == 0) sums[b * parts] = q.packed();
     }
+    __syncthreads();
+  }
+  if (tid < nb) {
+    const BeamSums q = BeamSums::of(sums[tid * parts]);
+    ref[tid] = q.ref();
+    // without a finite largest logit S is 0 or NaN
+    shift[tid] = q.s > 0.0 && q.s < INFINITY ? (double)score[tid] - log_sum(q.sum()) : -INFINITY;
   }
   __syncthreads();
   // candidate i of list l, whose key the lists have; the next in order has no better score
