@@ -747,7 +747,8 @@ rk_status rk_token_logprobs(const void *logits, rk_dtype dtype, int64_t n_rows, 
  * "gemm_gate_up", "gemm_down", "lm_lse", "lm_kl", "kl_logits", "lm_logits",
  * "local", "snap_scores", "snap_select", "paged_append", "paged_attention",
  * "paged_read", "paged_tree", "paged_keep", "paged_reorder", "beam_select",
- * "token_logprobs").
+ * "token_logprobs"; of "paged_tree" the one kernel or the other by itself: "paged_tree_narrow",
+ * "paged_tree_shared", whose waves share their tiles).
  * rk_timing_end waits for the recorded events, returns the number of launches
  * and their summed duration in milliseconds, and stops recording.  Host-side
  * state is process-wide; not for concurrent use from several threads.          */

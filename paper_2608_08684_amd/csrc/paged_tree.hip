@@ -705,11 +705,13 @@ hipError_t launch_tree(const PagedView& cache, const PagedTable& tab, const SeqT
 #define RK_TREE(T, C, DH)                                                                                          \
   do {                                                                                                             \
     if constexpr (std::is_same<T, float>::value) {                                                                 \
+      Timed timed("paged_tree_narrow", s);                                                                         \
       tree_narrow_kernel<T, C, DH><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, st, a);                        \
     } else {                                                                                                       \
-      if (!width.shared) tree_narrow_kernel<T, C, DH><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, st, a);  \
-      else if (width.columns == 64) tree_wide_kernel<C, DH, 1><<<blocks, 256, 0, s>>>(cache, tab, st, a);       \
-      else tree_wide_kernel<C, DH, 2><<<blocks, 256, 0, s>>>(cache, tab, st, a);                                \
+      Timed timed(!width.shared ? "paged_tree_narrow" : "paged_tree_shared", s);                                   \
+      if (!width.shared) tree_narrow_kernel<T, C, DH><<<blocks, 64 * kDecodeWaves, 0, s>>>(cache, tab, st, a);     \
+      else if (width.columns == 64) tree_wide_kernel<C, DH, 1><<<blocks, 256, 0, s>>>(cache, tab, st, a);          \
+      else tree_wide_kernel<C, DH, 2><<<blocks, 256, 0, s>>>(cache, tab, st, a);                                   \
     }                                                                                                              \
     if (a.n_parts > 1) {                                                                                           \
       const int groups = 256 / (DH / 4);                                                                           \

@@ -5,7 +5,7 @@ import paper_2608_08684_amd as rk
 
 from e4m3_helpers import Case8, empty_cache, values
 from test_gpu_paged_tree import Drafts, make
-from tree_helpers import SHARED, shared
+from tree_helpers import SHARED, all_shared, shared
 
 pytestmark = pytest.mark.gpu
 
@@ -15,6 +15,16 @@ def beyond(byte):
     return 8 * (262 - byte)
 
 
+def of_form(form, d, seed):
+    if form == "narrow":
+        case = make([70, 90], 8, 2, d, 16, "e4m3", seed=seed)
+        return case, Drafts(case, [10, 30], seed=seed)
+    case, drafts = shared(form, d, "e4m3", seed=seed)
+    with all_shared(1):
+        drafts.run()
+    return case, drafts
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("form", ["narrow", *SHARED])
 @pytest.mark.parametrize("byte, sign", [(247, 0), (247, 0x80), (248, 0), (254, 0), (254, 0x80), (246, 0)])
@@ -22,11 +32,7 @@ def test_values_beyond_bf16_reach_those_who_see_them(form, d, byte, sign):
     """The rows whose mask leaves the draft out do not change by a bit; the others get the infinity, in its channel
     alone.  The largest code that is finite is no infinity."""
     import torch
-    if form == "narrow":
-        case = make([70, 90], 8, 2, d, 16, "e4m3", seed=11)
-        drafts = Drafts(case, [10, 30], seed=11)
-    else:
-        case, drafts = shared(form, d, "e4m3", seed=11)
+    case, drafts = of_form(form, d, seed=11)
     seq, draft, head, channel, other = 0, 2, 1, 7, d - 3
     group = case.H // 2
     u = case.lens[seq] - drafts.counts[seq] + draft
@@ -60,11 +66,7 @@ def test_values_beyond_bf16_reach_those_who_see_them(form, d, byte, sign):
 def test_both_infinities_and_nan(form):
     """A draft with both infinities beside finite values and NaN, each in a channel of its own."""
     import torch
-    if form == "narrow":
-        case = make([70, 90], 8, 2, 64, 16, "e4m3", seed=12)
-        drafts = Drafts(case, [10, 30], seed=12)
-    else:
-        case, drafts = shared(form, 64, "e4m3", seed=12)
+    case, drafts = of_form(form, 64, seed=12)
     draft = 3
     u = case.lens[0] - drafts.counts[0] + draft
     at = (int(case.table[0, u // 16]), 0, u % 16)

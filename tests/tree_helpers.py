@@ -1,6 +1,10 @@
 """Trees of drafts at the kernel whose waves share tiles: from 256 workgroups of 16 columns on, or under a long table."""
 from __future__ import annotations
 
+import contextlib
+
+import paper_2608_08684_amd as rk
+
 from test_gpu_paged_tree import Drafts, make
 
 # (sequences, drafts of the longest tree, query heads to a KV head, columns of a workgroup, table in entries or None)
@@ -32,3 +36,16 @@ def shared(form, d, dtype, masks="tree", page=16, seed=0, lengths=None, counts=N
         kw["width"] = entries // page
     case = make(lengths, 2 * group, 2, d, page, dtype, seed=seed, **kw)
     return case, Drafts(case, counts or counts_of(form), masks, seed=seed)
+
+
+@contextlib.contextmanager
+def all_shared(calls):
+    """Every one of that many attention calls goes to the kernel whose waves share tiles."""
+    rk.timing_begin("paged_tree_shared")
+    done = False
+    try:
+        yield
+        done = True
+    finally:
+        launches, _ = rk.timing_end()
+    assert not done or launches == calls, f"{launches} of {calls} calls"
