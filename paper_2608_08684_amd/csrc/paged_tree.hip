@@ -11,7 +11,8 @@
 //
 // A column keeps a reference R, the sum l of its weights e^(s - R) and its output.  R is
 // moved only when a score has passed it by kRaise: the output's rescale, a multiplication of
-// every accumulator, is then rare.  bf16 and 8-bit caches: R is held times log2(e) and a
+// every accumulator, is then rare.  The other columns of the wave go through it with a factor of
+// 1, so that no bit of a row hangs on what other rows see.  bf16 and 8-bit caches: R is held times log2(e) and a
 // weight's exponent is one fma of the score; what its rounding puts into a weight, 2^-24 of a
 // score, is far below the output's bf16.  R also holds the power of two above the part's entries
 // (the weights' sum stays below 1, and no weighted sum overflows).
@@ -179,10 +180,13 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void tree_narrow_kernel(PagedVie
     float mx = s[0][0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) mx = fmaxf(mx, s[i >> 2][i & 3]);
-    if (__ballot(kFp32 ? mx * a.scale > R + kRaise : fmaf(mx, c2, -R) > kRaise * kLog2e - (float)bits)) {
+    const auto above = [&](float x) {
+      return kFp32 ? x * a.scale > R + kRaise : fmaf(x, c2, -R) > kRaise * kLog2e - (float)bits;
+    };
+    if (__ballot(above(mx))) {
       mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
       mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-      const float to = fmaxf(R, kFp32 ? mx * a.scale : fmaf(mx, c2, (float)bits));
+      const float to = above(mx) ? (kFp32 ? mx * a.scale : fmaf(mx, c2, (float)bits)) : R;
       const float corr = kFp32 ? exp_diff(R - to) : __builtin_amdgcn_exp2f(R - to);
       R = to;
       l *= corr;
@@ -436,21 +440,22 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void tree_wide_kernel(PagedVi
     }
   };
   const auto raise = [&](const f32x4_t (*s)[2]) {
+    const auto above = [&](float x, int n) { return fmaf(x, c2, -R[n]) > kRaise * kLog2e - (float)bits; };
     float mx[N];
-    bool above = false;
+    bool any = false;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       mx[n] = s[n][0][0];
 #pragma unroll
       for (int i = 1; i < 8; ++i) mx[n] = fmaxf(mx[n], s[n][i >> 2][i & 3]);
-      above |= fmaf(mx[n], c2, -R[n]) > kRaise * kLog2e - (float)bits;
+      any |= above(mx[n], n);
     }
-    if (!__ballot(above)) return;
+    if (!__ballot(any)) return;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       float x = fmaxf(mx[n], __shfl_xor(mx[n], 16, 64));
       x = fmaxf(x, __shfl_xor(x, 32, 64));
-      const float to = fmaxf(R[n], fmaf(x, c2, (float)bits));
+      const float to = above(x, n) ? fmaf(x, c2, (float)bits) : R[n];
       const float corr = __builtin_amdgcn_exp2f(R[n] - to);
       R[n] = to;
       l[n] *= corr;
