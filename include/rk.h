@@ -649,7 +649,9 @@ size_t rk_paged_tree_workspace_size(const rk_paged_cache *cache, int32_t n_seqs,
  *            the drafts 0 .. j.
  *   q, out, scale, lse [rows, n_heads]: as for rk_paged_attention, a row for each draft.
  * A row that sees nothing gets zeros and a log-sum-exp of -inf; what is said of infinite and
- * NaN Values, tables and lengths there holds here (weights below e^-50 may count as 0).   */
+ * NaN Values, tables and lengths there holds here (weights below e^-50 may count as 0).  The
+ * work is laid out for sequences as long as the table is wide (max_pages): short ones under a
+ * table with room for long ones take up to half as long again.                     */
 rk_status rk_paged_attention_tree(const rk_paged_cache *cache, const rk_paged_seqs *seqs, const int64_t *offsets,
                                   const uint64_t *masks, const void *q, int64_t q_row_stride, int32_t n_heads,
                                   float scale, void *out, int64_t out_row_stride, float *lse, void *workspace,

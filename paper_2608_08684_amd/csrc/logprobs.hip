@@ -180,8 +180,8 @@ __device__ __forceinline__ double wave_total(double x) {
 }
 
 // The same for beams, whose scores are compared with each other: the exponentials are fp32's, what
-// is done with them is done in doubles, at no cost (128 rows of 128256 fp32 logits: 15.3 us either
-// way).  log S is then 1e-8 off in the mean, 7e-8 at most on a language model's logits, where fp32
+// is done with them is done in doubles (128 rows of 128256 fp32 logits: 14.7 us either way; the
+// joining kernel takes 0.4 us more).  log S is then 1e-8 off in the mean, 7e-8 at most on a language model's logits, where fp32
 // sums left 8e-8 and 4e-7; what remains is the exponentials', so that a row's largest logit, whose
 // exponential is 1, adds nothing to it: with a token of probability 0.9999 it is 1e-12.
 // Exponentials in doubles too, 17 instructions of half rate a logit: 23 us.
@@ -623,9 +623,9 @@ hipError_t launch_logprobs(const LogprobArgs& a, bool bf16, hipStream_t s) {
 // its list moved on.  More than 64 lists (rows in many parts) are first cut to the 64 with the
 // best heads: a list with n_out better heads beside it gives nothing.  Scores between beams are
 // doubles, log S among them (BeamSums says how good it is); within a beam the logits decide.
-// Bound: latency, a chain of loads, sums and n_out short steps: 6.9 us for the 8 best of 16 lists,
-// 4.7 for the 4 best of 12.  The rows' kernel before it reads every logit once (128 rows of 128256
-// fp32 in two parts: 15.5 us, 4.2 TB/s; 4 rows of 50257 bf16: 8.5).
+// Bound: latency, a chain of loads, sums and n_out short steps: 7.4 us for the 8 best of 16 lists,
+// 4.9 for the 4 best of 12.  The rows' kernel before it reads every logit once (128 rows of 128256
+// fp32 in two parts: 14.7 us, 4.5 TB/s, in part out of the cache; 4 rows of 50257 bf16: 8.0).
 // (lists: 256 where rows are split to fill the card, 17 a row of 2^22 fp32 logits)
 constexpr int kMaxLists = 17 * RK_MAX_BEAMS;
 

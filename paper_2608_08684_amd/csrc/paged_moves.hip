@@ -21,7 +21,9 @@ __device__ __forceinline__ int64_t entry_row(const PagedView& cache, const Paged
 // --------------------------------------------------------------------------- read
 // A workgroup takes up to 16 rows, fewer while CUs are idle: where they lie, then their
 // 16-byte pieces, keys first, U loads in flight a thread.  17928 8-bit rows of 8 heads of 128 to
-// bf16: 26.8 us (110 MB, 4.1 TB/s); 64 rows 3.3 us, the way from lengths to pages to rows.
+// bf16: 25.7 us (110 MB, 4.3 TB/s); 64 rows 3.1 us, the way from lengths to pages to rows.  The same rows
+// again and again, in part out of the cache: 22.2, bf16 ones 25.9 (147 MB), 12 heads of 64 in fp32 37.2
+// (220 MB); 64 rows of either 2.8 and 3.0.
 constexpr int kReadRows = 16, kMoveThreads = 256;
 
 template <typename T, typename C, int DH>
@@ -79,8 +81,9 @@ __global__ __launch_bounds__(kMoveThreads) void read_kernel(PagedView cache, Pag
 // A workgroup takes the path of one sequence and KV head, its keys or its values: all rows go
 // to LDS before any is written, so a row's new place may be another's old one.  The keys'
 // workgroup then forms the bounds of the pages, a channel a thread, in the order of the path.
-// Bound: latency, lengths -> pages -> rows -> bounds: 4.8 us for 32 sequences of up to 26 drafts
-// with bounds, 3.8 for 8 of 64 fp32 rows without.
+// Bound: latency, lengths -> pages -> rows -> bounds: 4.7 us for 32 sequences of up to 26 drafts
+// with bounds, 3.6 for 8 of 64 fp32 rows of 64 channels without.  A thread's loads hang on where its rows
+// go, so each is waited for before the next: 8 x 63 fp32 rows of 128 channels, 8 loads a thread, 6.1 us.
 template <typename T, typename C, int DH>
 __global__ __launch_bounds__(kMoveThreads) void keep_kernel(PagedView cache, PagedTable tab, SeqTable st,
                                                             const int32_t* kept, int64_t kept_stride, int n_kept) {
@@ -159,8 +162,10 @@ __global__ __launch_bounds__(kMoveThreads) void keep_kernel(PagedView cache, Pag
 // reads it from the pages of all of a group's parents before it writes any: the beams'
 // pages may be each other's sources.  The table's workgroups do the same with its columns.
 // Both read the table of before, so they share a launch unless the table is changed in place.
-// 16 groups of 8 beams, 52 entries of 8 KV heads of 128 in the page: up to 54 MB, 15.7 us; 4 beams,
-// 12 heads of 64: 3.9.
+// 16 groups of 8 beams, 52 entries of 8 KV heads of 128 in the page: up to 54 MB, 14.8 us; 4 beams,
+// 12 heads of 64: 3.7.  Bound: a thread's loads hang on there being a copy, and for up to 8 beams each is
+// waited for before the next (beyond, they go out together); 5 .. 8 beams take 240 registers, two
+// waves to a SIMD.
 template <typename T, typename C, int DH, int NB>
 __global__ __launch_bounds__(kMoveThreads) void reorder_kernel(PagedView cache, PagedTable tab, ReorderArgs a,
                                                                int chunks, int table_chunks) {

@@ -83,7 +83,7 @@ __device__ __forceinline__ uint32_t sees(uint64_t word, int first) {
 // As the attention of one token, with a draft's mask for each column.  Weights in three bf16 pieces.
 // Bound: memory where entries are many (2 sequences of 8192, 16 columns of 128: 23.6 us), else the
 // latency of lengths -> pages -> tiles -> join through LDS (one fp32 sequence of 257, 5 drafts, three
-// rounds of tiles: 10.7 us).
+// rounds of tiles: 9.7 us).
 template <typename T, typename C, int DH>
 __global__ __launch_bounds__(64 * kDecodeWaves) void tree_narrow_kernel(PagedView cache, PagedTable tab, SeqTable st,
                                                                         TreeArgs a) {
@@ -352,9 +352,10 @@ template <typename C, int DH> struct WideTile {
 // instructions' own) and the matrix unit 40%, and they go together badly: a wave's 32 matrix
 // instructions beside another's 128 fmas take 0.67 of the sum of both, two waves that do both in turn
 // 0.8 - 0.86.  256 registers leave two waves to a SIMD.  16 sequences of 100 .. 8192 in e4m3, 64
-// drafts of 32 query heads of 128 over 8 KV heads: 131 us (0.50 PFLOP/s of the formula's products); 8
-// of 500 .. 4096 in bf16, up to 26 drafts: 31 us.  The waves' priority in the matrix part: 167 -> 154 of
-// the first, then.  Not taken: 8 waves in two groups that alternate between the units (157 where 150
+// drafts of 32 query heads of 128 over 8 KV heads: 110 us and 13.7 of the join (0.53 PFLOP/s of the
+// formula's products in 124); 8 of 500 .. 4096 in bf16, up to 26 drafts: 28.5 and 5.9.  (Of calls one
+// after the other: the first twenty after a pause take 134.)  Trials, with what stood then beside
+// them: the waves' priority in the matrix part 167 -> 154.  Not taken: 8 waves in two groups that alternate between the units (157 where 150
 // stood), vector and matrix instructions mixed by the schedule (154 -> 280, registers spill), one block
 // of 16 columns a wave for all (179), keys half a tile ahead of the values for one barrier a tile
 // instead of two (147 -> 152), another priority for every second wave (146 -> 153 .. 158).
@@ -652,6 +653,12 @@ __global__ __launch_bounds__(256) void tree_join_kernel(PagedTable tab, SeqTable
 // 4096, 64: 17.8 | 19.4; 8 of 2048, 32: 26.2 | 24.5; 2 of 8192, 64: 34.7 | 27.9; 60 of 300, 64: 63.7 | 25.2.
 // 12 KV heads of 64: 2 of 900, 30 columns 11.1 | 14.6; 4 of 2048, 32: 16.8 | 16.3.  fp32 has no shared
 // kernel: its products take eight times as long as its loads.
+// The lengths lie on the device, so the choice, and that of the parts below, goes by the table's width.  A
+// call with its join under a table as wide as its longest sequence needs | 4 | 16 times as wide:
+// 1 of 360, 148 columns of 128: 10.6 | 12.9 | 16.0 (shared); 4 of 1000, 104: 17.6 | 22.5 | 22.6 (shared
+// from 4 on); 32 of 300, 32: 22.5 | 22.4 | 28.3; 8 of 500 .. 4096, 104: 34.6 | 36.7 | 36.7; 16 of 100 ..
+// 8192 in e4m3, 256: 125 | 127 | 126; 2 of 900, 30 of 64: 10.4 | 11.3 | 11.4 (shared); one fp32 sequence
+// of 257: 9.8 | 11.0 | 9.9.
 struct Width {
   int columns;
   bool shared;
