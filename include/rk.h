@@ -694,7 +694,7 @@ size_t rk_beam_select_workspace_size(int32_t n_groups, int32_t n_beams, int32_t 
  * beam the logits, ties to the lower token.  Of a logsumexp the exponentials alone are fp32's: it
  * is off by some 1e-8, at most by 2^-23 sum_v p_v (max x - x_v) and a few 2^-22 of the probability
  * below the row's largest logit.  Beams nearer to each other than that may come in either
- * order, the same one in every call.  n_beams <= RK_MAX_BEAMS, 1 <= n_out <= RK_MAX_TOP; rows and
+ * order, the same one whenever the call is repeated.  n_beams <= RK_MAX_BEAMS, 1 <= n_out <= RK_MAX_TOP; rows and
  * vocab as for rk_token_logprobs.                               */
 rk_status rk_beam_select(const void *logits, rk_dtype dtype, int32_t n_groups, int32_t n_beams, int32_t vocab,
                          int64_t row_stride, const float *scores, const uint8_t *ended, int32_t end_token,

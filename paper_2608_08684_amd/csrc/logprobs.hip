@@ -181,10 +181,10 @@ __device__ __forceinline__ double wave_total(double x) {
 
 // The same for beams, whose scores are compared with each other: the exponentials are fp32's, what
 // is done with them is done in doubles (128 rows of 128256 fp32 logits: 14.7 us either way; the
-// joining kernel takes 0.4 us more).  log S is then 1e-8 off in the mean, 7e-8 at most on a language model's logits, where fp32
-// sums left 8e-8 and 4e-7; what remains is the exponentials', so that a row's largest logit, whose
-// exponential is 1, adds nothing to it: with a token of probability 0.9999 it is 1e-12.
-// Exponentials in doubles too, 17 instructions of half rate a logit: 23 us.
+// joining kernel takes 0.4 us more).  log S is then 1e-8 off in the mean, 7e-8 at most on a language
+// model's logits, where fp32 sums left 8e-8 and 4e-7.  What remains is the exponentials', so that a
+// row's largest logit, whose exponential is 1, adds nothing to it: with a token of probability
+// 0.9999 it is 1e-12.  Exponentials in doubles too, 17 instructions of half rate a logit: 23 us.
 struct BeamSums {
   float c;
   float t;

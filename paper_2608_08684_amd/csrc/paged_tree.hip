@@ -12,10 +12,10 @@
 // A column keeps a reference R, the sum l of its weights e^(s - R) and its output.  R is
 // moved only when a score has passed it by kRaise: the output's rescale, a multiplication of
 // every accumulator, is then rare.  The other columns of the wave go through it with a factor of
-// 1, so that no bit of a row hangs on what other rows see.  bf16 and 8-bit caches: R is held times log2(e) and a
-// weight's exponent is one fma of the score; what its rounding puts into a weight, 2^-24 of a
-// score, is far below the output's bf16.  R also holds the power of two above the part's entries
-// (the weights' sum stays below 1, and no weighted sum overflows).
+// 1, so that no bit of a row hangs on what other rows see.  bf16 and 8-bit caches: R is held times
+// log2(e) and a weight's exponent is one fma of the score; what its rounding puts into a weight,
+// 2^-24 of a score, is far below the output's bf16.  R also holds the power of two above the part's
+// entries (the weights' sum stays below 1, and no weighted sum overflows).
 //
 // A value that is infinite or NaN must not reach the columns whose mask leaves its draft out,
 // but 0 times it would: in the tiles that hold drafts such values are taken out of the
@@ -354,11 +354,12 @@ template <typename C, int DH> struct WideTile {
 // 0.8 - 0.86.  256 registers leave two waves to a SIMD.  16 sequences of 100 .. 8192 in e4m3, 64
 // drafts of 32 query heads of 128 over 8 KV heads: 110 us and 13.7 of the join (0.53 PFLOP/s of the
 // formula's products in 124); 8 of 500 .. 4096 in bf16, up to 26 drafts: 28.5 and 5.9.  (Of calls one
-// after the other: the first twenty after a pause take 134.)  Trials, with what stood then beside
-// them: the waves' priority in the matrix part 167 -> 154.  Not taken: 8 waves in two groups that alternate between the units (157 where 150
-// stood), vector and matrix instructions mixed by the schedule (154 -> 280, registers spill), one block
-// of 16 columns a wave for all (179), keys half a tile ahead of the values for one barrier a tile
-// instead of two (147 -> 152), another priority for every second wave (146 -> 153 .. 158).
+// after the other; the first twenty after a pause take 134 and 31.)  Trials, with what stood then
+// beside them: the waves' priority in the matrix part 167 -> 154.  Not taken: 8 waves in two groups
+// that alternate between the units (157 where 150 stood), vector and matrix instructions mixed by
+// the schedule (154 -> 280, registers spill), one block of 16 columns a wave for all (179), keys half
+// a tile ahead of the values for one barrier a tile instead of two (147 -> 152), another priority for
+// every second wave (146 -> 153 .. 158).
 template <typename C, int DH, int N>
 __global__ __launch_bounds__(64 * kDecodeWaves, 2) void tree_wide_kernel(PagedView cache, PagedTable tab, SeqTable st,
                                                                          TreeArgs a) {

@@ -1,4 +1,4 @@
-"""What holds at the edges of a tree's attention, at the kernel whose waves share tiles: workgroups of 64 and of 128 columns,
+"""What holds at the edges of a tree's attention, at the kernel whose waves share tiles: workgroups of 64 and 128 columns,
 lengths in one part and in several.  Every test makes sure that it is that kernel."""
 import pytest
 
